@@ -157,7 +157,8 @@ def strip_comments(src: str) -> str:
 
 def kernel_sources_sha1():
     """Hash of the code (comments and layout left out) of every HIP source and header of the
-    library: a stored counter reading is valid only for the kernels it was taken from."""
+    recurrence (the operators in csrc/head are none of this benchmark's kernels): a stored counter
+    reading is valid only for the kernels it was taken from."""
     import glob
     import hashlib
     h = hashlib.sha1()

@@ -21,7 +21,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstacklstm.so")
 BUILD = os.path.join(HERE, "_build")
-SOURCES = ["api.hip", "scan.hip", "plan.hip", "prep.hip", "contract.hip", "level_fwd.hip", "level_bwd.hip"]
+SOURCES = ["api.hip", "scan.hip", "plan.hip", "prep.hip", "contract.hip", "level_fwd.hip", "level_bwd.hip",
+           "head/norm.hip", "head/linear.hip", "head/distill.hip", "head/beam.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # packed fp32 instructions stay off: only scalar fp32 ALU code is generated
@@ -114,15 +115,16 @@ def mfma_branch_hazards(asm: str) -> list:
 
 
 def _compile(src: str):
-    obj = os.path.join(BUILD, src.replace(".hip", ".o"))
+    name = os.path.basename(src)
+    obj = os.path.join(BUILD, name.replace(".hip", ".o"))
     cmd = [HIPCC, *FLAGS, "-save-temps", "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True, cwd=BUILD)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError(f"hipcc failed for {src}")
-    stem = src[:-len(".hip")]
+    stem = name[:-len(".hip")]
     for f in os.listdir(BUILD):   # keep the device assembly and the objects only
-        if f.startswith(stem + "-") and not f.endswith("-gfx950.s") or f.startswith(src + "-"):
+        if f.startswith(stem + "-") and not f.endswith("-gfx950.s") or f.startswith(name + "-"):
             os.remove(os.path.join(BUILD, f))
     with open(os.path.join(BUILD, f"{stem}-hip-amdgcn-amd-amdhsa-gfx950.s")) as fh:
         hazards = mfma_branch_hazards(fh.read())

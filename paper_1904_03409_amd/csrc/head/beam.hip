@@ -1,0 +1,555 @@
+// One step of a beam search: the K best of K x V continuations of every search, then the stacks of states
+// copied to the beams that go on.
+//   total = (x - lse(x)) + score, falling; ties to the lower place k V + v
+// Selection is bound by one read of the logits. A row (beam) waits in registers between its softmax sums and its
+// selection. What is chosen has to be exact, ties included, so totals are compared as whole keys (ordered bits of
+// the total, then the place). To touch few elements with them: the row's threads form 64 groups; the K-th largest of
+// the groups' largest elements is a bound that at least K elements reach and few others do. Those go to a list
+// in LDS and are ranked there. Where equal logits or their layout make the list too long, the K best are
+// taken one after the other.
+// Rows that are too long for registers, or too few to fill the chip, are cut into chunks with a pass for the
+// sums before (k_beam_part). Small vocabularies take one workgroup to a search (k_beam_small).
+#include <algorithm>
+
+#include "../../../include/stacklstm_head.h"
+#include "head.h"
+
+namespace {
+
+typedef unsigned long long u64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxBeams = 64, kList = 1024;
+constexpr int kPartVecs = 4;                           // vectors a thread in a chunk of 256 threads
+constexpr int kSmall = 8192;                           // totals of a search that fit one workgroup's LDS
+
+struct BeamArgs {
+  int B, K, V, eos, chunks;
+  const void* x;
+  int64_t ldx;
+  const uint8_t *legal, *done;
+  const float* score;
+  float* part;                                         // [rows][chunks][2]: maximum, sum
+  u64* cand;                                           // [rows][chunks][K] keys, place = token
+  float* score_next;
+  int32_t *parent, *token;
+  uint8_t* done_next;
+};
+
+// Bits in the order of the floats (-0 as 0), and back.
+__device__ __forceinline__ uint32_t order_bits(float v) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_order(uint32_t o) {
+  return __uint_as_float(o ^ ((uint32_t)~((int32_t)o >> 31) | 0x80000000u));
+}
+// 0: no continuation (-inf and NaN)
+__device__ __forceinline__ u64 make_key(float total, uint32_t place) {
+  return total > -INFINITY ? (u64)order_bits(total) << 32 | (0xffffffffu - place) : 0;
+}
+__device__ __forceinline__ float key_total(u64 k) { return from_order((uint32_t)(k >> 32)); }
+__device__ __forceinline__ uint32_t key_place(u64 k) { return 0xffffffffu - (uint32_t)k; }
+
+template <int N>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  auto move = [](uint32_t v, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  if constexpr (N >= 2) v = max(v, move(v, std::integral_constant<int, 0xb1>()));
+  if constexpr (N >= 4) v = max(v, move(v, std::integral_constant<int, 0x4e>()));
+  if constexpr (N >= 8) v = max(v, move(v, std::integral_constant<int, 0x141>()));
+  if constexpr (N >= 16) v = max(v, move(v, std::integral_constant<int, 0x140>()));
+  return v;
+}
+
+struct TopkLds {
+  u64 list[kList], out[kMaxBeams], red[16];
+  uint32_t grp[64], thr;
+  int count;
+};
+
+// The K-th largest of the 64 groups' largest values (in order bits; 0: the group has none), in every thread.
+// mine: this thread's. All NT threads call.
+template <int NT>
+__device__ __forceinline__ uint32_t topk_bound(uint32_t mine, int K, TopkLds& s) {
+  constexpr int G = NT / 64;                           // threads of a group
+  mine = lanes_max<G>(mine);
+  const int t = threadIdx.x;
+  if (t % G == 0) s.grp[t / G] = mine;
+  if (t == 0) s.count = 0;
+  if (t < kMaxBeams) s.out[t] = 0;
+  __syncthreads();
+  if (t < 64) {
+    const uint32_t v = s.grp[t];
+    int above = 0;
+#pragma unroll 16
+    for (int j = 0; j < 64; ++j) {
+      const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)v, j);
+      above += o > v || (o == v && j < t);
+    }
+    if (above == K - 1) s.thr = v;
+  }
+  __syncthreads();
+  return s.thr;
+}
+__device__ __forceinline__ void topk_put(u64 key, TopkLds& s) {
+  const int i = atomicAdd(&s.count, 1);
+  if (i < kList) s.list[i] = key;
+}
+// The K best of the listed keys (all different) to s.out, falling, zeros behind the last. each(f): calls f with every
+// key of this thread, listed or not, for lists that did not fit.
+template <int NT, typename Each>
+__device__ __forceinline__ void topk_rank(int K, TopkLds& s, Each each) {
+  __syncthreads();
+  const int n = s.count, t = threadIdx.x;
+  if (n <= kList) {
+    for (int i = t; i < n; i += NT) {
+      const u64 k = s.list[i];
+      int above = 0;
+      for (int j = 0; j < n; ++j) above += s.list[j] > k;
+      if (above < K) s.out[above] = k;
+    }
+    __syncthreads();
+    return;
+  }
+  u64 last = ~(u64)0;
+  for (int r = 0; r < K; ++r) {
+    u64 best = 0;
+    each([&](u64 k) {
+      if (k < last && k > best) best = k;
+    });
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const u64 o = __shfl_xor(best, d);
+      best = o > best ? o : best;
+    }
+    if ((t & 63) == 0) s.red[t >> 6] = best;
+    __syncthreads();
+    for (int w = 0; w < NT / 64; ++w) best = s.red[w] > best ? s.red[w] : best;
+    if (t == 0) s.out[r] = best;
+    __syncthreads();
+    last = best;
+    if (!best) break;                                  // (every thread has the same)
+  }
+}
+
+// Where place n of a search's K goes.
+__device__ __forceinline__ void beam_out(const BeamArgs& a, int b, int n, u64 key) {
+  const int64_t o = (int64_t)b * a.K + n;
+  int parent = n, token = -1;
+  bool done = true;
+  float total = -INFINITY;
+  if (key) {
+    const uint32_t place = key_place(key);
+    total = key_total(key);
+    parent = (int)(place / (uint32_t)a.V);
+    const bool was = a.done && a.done[(int64_t)b * a.K + parent];
+    if (!was) {
+      token = (int)(place % (uint32_t)a.V);
+      done = token == a.eos;
+    }
+  }
+  a.score_next[o] = total;
+  a.parent[o] = parent;
+  a.token[o] = token;
+  a.done_next[o] = done;
+}
+
+// Vector c of a row of logits, -inf where the row ends and where a token is not allowed.
+template <typename T>
+__device__ __forceinline__ u32x4 load_logits(const BeamArgs& a, int64_t row, int c) {
+  constexpr int V = vec<T>::N;
+  constexpr uint32_t low = kPadLow<T>;
+  u32x4 r = load_vec((const T*)a.x + row * a.ldx, c, a.V, low);
+  if (a.legal) {
+    const uint8_t* l = a.legal + row * a.V + (int64_t)c * V;
+    bool ok[V];
+    if ((c + 1) * V <= a.V) {
+      typedef uint32_t u32_any __attribute__((aligned(1)));
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) {
+        const uint32_t w = *(const u32_any*)(l + 4 * q);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ok[4 * q + k] = (w >> (8 * k)) & 0xffu;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) ok[k] = c * V + k < a.V && l[k];
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if constexpr (V == 4) {
+        r[k] = ok[k] ? r[k] : low;
+      } else {
+        const uint32_t keep = k & 1 ? 0x0000ffffu : 0xffff0000u;
+        r[k / 2] = ok[k] ? r[k / 2] : (r[k / 2] & keep) | (low & ~keep);
+      }
+    }
+  }
+  return r;
+}
+
+// Whether a beam goes on with tokens; if not, its chunk's keys are written (a finished beam's one).
+__device__ __forceinline__ bool beam_runs(const BeamArgs& a, int64_t row, int ch, float score) {
+  const bool done = a.done && a.done[row];
+  if (!done && score > -INFINITY) return true;
+  u64* out = a.cand + ((size_t)row * a.chunks + ch) * a.K;
+  for (int j = threadIdx.x; j < a.K; j += blockDim.x) out[j] = done && ch == 0 && j == 0 ? make_key(score, 0) : 0;
+  return false;
+}
+
+}  // namespace
+
+// A row, or with JOIN a chunk of one: the best K continuations by it.
+template <typename T, int NT, int NV, bool JOIN>
+__global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
+  constexpr int V = vec<T>::N;
+  __shared__ TopkLds s;
+  __shared__ float red[2][16];
+  const int64_t row = JOIN ? blockIdx.x / a.chunks : blockIdx.x;
+  const int ch = JOIN ? blockIdx.x % a.chunks : 0, t = threadIdx.x, c0 = ch * NT * NV + t;
+  const float score = a.score[row];
+  if (!beam_runs(a, row, ch, score)) return;
+  u32x4 raw[NV];
+  float mine = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) raw[i] = load_logits<T>(a, row, c0 + i * NT);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float v[V];
+    vec<T>::unpack(raw[i], v);
+#pragma unroll
+    for (int k = 0; k < V; ++k) mine = fmaxf(mine, v[k]);
+  }
+  float m, sum = 0.f;
+  if constexpr (JOIN) {
+    const float* q = a.part + (size_t)row * a.chunks * 2;
+    m = -INFINITY;
+    for (int i = t; i < a.chunks; i += NT) m = fmaxf(m, q[2 * i]);
+    m = group_reduce<NT>(m, op_max(), red[0]);
+    for (int i = t; i < a.chunks; i += NT) {
+      // (a chunk of -inf alone has the sum 0 and no share)
+      const float mi = q[2 * i], si = q[2 * i + 1];
+      sum += mi == -INFINITY ? si : si * __builtin_amdgcn_exp2f((mi - m) * kLog2e);
+    }
+  } else {
+    m = group_reduce<NT>(mine, op_max(), red[0]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      opaque_vec(raw[i]);
+      float v[V];
+      vec<T>::unpack(raw[i], v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum += __builtin_amdgcn_exp2f((v[k] - m) * kLog2e);
+    }
+  }
+  const float lse = m + logf(group_reduce<NT>(sum, op_sum(), red[1]));
+  const uint32_t bound = topk_bound<NT>(mine > -INFINITY ? order_bits(mine) : 0u, a.K, s);
+  // Totals rise with x, but two different x may have one total, where the lower place wins: elements a few
+  // roundings below the bound are looked at as well.
+  const float xb = bound ? from_order(bound) : -INFINITY;
+  const float tb = bound ? (xb - lse) + score : -INFINITY;
+  const float lo = bound ? xb - 1e-6f * (fabsf(xb) + fabsf(lse) + fabsf(score)) : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    opaque_vec(raw[i]);
+    float v[V], most = -INFINITY;
+    vec<T>::unpack(raw[i], v);
+#pragma unroll
+    for (int k = 0; k < V; ++k) most = fmaxf(most, v[k]);
+    if (most >= lo) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float total = (v[k] - lse) + score;
+        if (total >= tb && total > -INFINITY) topk_put(make_key(total, (c0 + i * NT) * V + k), s);
+      }
+    }
+  }
+  topk_rank<NT>(a.K, s, [&](auto f) {
+#pragma unroll 1
+    for (int i = 0; i < NV; ++i) {
+      // (read again: a loop over registers would take them all at once)
+      const u32x4 w = load_logits<T>(a, row, c0 + i * NT);
+      float v[V];
+      vec<T>::unpack(w, v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) f(make_key((v[k] - lse) + score, (c0 + i * NT) * V + k));
+    }
+  });
+  u64* out = a.cand + ((size_t)row * a.chunks + ch) * a.K;
+  for (int j = t; j < a.K; j += NT) out[j] = s.out[j];
+}
+
+// A chunk's maximum and sum.
+template <typename T>
+__global__ void __launch_bounds__(256) k_beam_part(BeamArgs a) {
+  constexpr int V = vec<T>::N;
+  __shared__ float red[2][4];
+  const int64_t row = blockIdx.x / a.chunks;
+  const int ch = blockIdx.x % a.chunks, t = threadIdx.x, c0 = ch * 256 * kPartVecs + t;
+  if ((a.done && a.done[row]) || !(a.score[row] > -INFINITY)) return;
+  u32x4 raw[kPartVecs];
+  float m = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPartVecs; ++i) raw[i] = load_logits<T>(a, row, c0 + i * 256);
+#pragma unroll
+  for (int i = 0; i < kPartVecs; ++i) {
+    float v[V];
+    vec<T>::unpack(raw[i], v);
+#pragma unroll
+    for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
+  }
+  m = group_reduce<256>(m, op_max(), red[0]);
+  const float m0 = m > -INFINITY ? m : 0.f;
+#pragma unroll
+  for (int i = 0; i < kPartVecs; ++i) {
+    float v[V];
+    vec<T>::unpack(raw[i], v);
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum += __builtin_amdgcn_exp2f((v[k] - m0) * kLog2e);
+  }
+  sum = group_reduce<256>(sum, op_sum(), red[1]);
+  if (t == 0) {
+    a.part[(size_t)blockIdx.x * 2] = m;
+    a.part[(size_t)blockIdx.x * 2 + 1] = sum;
+  }
+}
+
+// The K best of a search's candidates.
+__global__ void __launch_bounds__(256) k_beam_merge(BeamArgs a) {
+  __shared__ TopkLds s;
+  const int b = blockIdx.x, t = threadIdx.x, per = a.chunks * a.K;
+  const int64_t n = (int64_t)a.K * per;
+  const u64* cand = a.cand + (size_t)b * n;
+  auto get = [&](int64_t i) -> u64 {
+    const u64 k = cand[i];
+    // the place in the search: the same total, K V continuations
+    return k ? (k & 0xffffffff00000000ull) | (0xffffffffu - (key_place(k) + (uint32_t)(i / per) * (uint32_t)a.V)) : 0;
+  };
+  uint32_t mine = 0;
+  for (int64_t i = t; i < n; i += 256) mine = max(mine, (uint32_t)(cand[i] >> 32));
+  const uint32_t bound = topk_bound<256>(mine, a.K, s);
+  for (int64_t i = t; i < n; i += 256) {
+    const u64 k = get(i);
+    if (k && (uint32_t)(k >> 32) >= bound) topk_put(k, s);
+  }
+  topk_rank<256>(a.K, s, [&](auto f) {
+    for (int64_t i = t; i < n; i += 256) f(get(i));
+  });
+  if (t < a.K) beam_out(a, b, t, s.out[t]);
+}
+
+// A whole search of at most kSmall continuations: a wave to a row for the softmax sums, totals in LDS.
+template <typename T>
+__global__ void __launch_bounds__(256) k_beam_small(BeamArgs a) {
+  __shared__ TopkLds s;
+  __shared__ float tot[kSmall];
+  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, n = a.K * a.V;
+  for (int k = t >> 6; k < a.K; k += 4) {
+    const int64_t row = (int64_t)b * a.K + k;
+    const T* x = (const T*)a.x + row * a.ldx;
+    const uint8_t* legal = a.legal ? a.legal + row * a.V : nullptr;
+    float* to = tot + k * a.V;
+    const float score = a.score[row];
+    const bool done = a.done && a.done[row];
+    float m = -INFINITY, sum = 0.f;
+    for (int v = lane; v < a.V; v += 64) {
+      const float e = !legal || legal[v] ? to_f32(x[v]) : -INFINITY;
+      to[v] = e;
+      m = fmaxf(m, e);
+    }
+    m = lanes<64>(m, op_max());
+    for (int v = lane; v < a.V; v += 64) sum += __builtin_amdgcn_exp2f((to[v] - m) * kLog2e);
+    const float lse = m + logf(lanes<64>(sum, op_sum()));
+    for (int v = lane; v < a.V; v += 64) to[v] = done ? (v ? -INFINITY : score) : (to[v] - lse) + score;
+  }
+  __syncthreads();
+  uint32_t mine = 0;
+  for (int i = t; i < n; i += 256) {
+    const float v = tot[i];
+    if (v > -INFINITY) mine = max(mine, order_bits(v));
+  }
+  const uint32_t bound = topk_bound<256>(mine, a.K, s);
+  for (int i = t; i < n; i += 256) {
+    const u64 k = make_key(tot[i], i);
+    if (k && (uint32_t)(k >> 32) >= bound) topk_put(k, s);
+  }
+  topk_rank<256>(a.K, s, [&](auto f) {
+    for (int i = t; i < n; i += 256) f(make_key(tot[i], i));
+  });
+  if (t < a.K) beam_out(a, b, t, s.out[t]);
+}
+
+namespace {
+
+// Rows of state: 16 KB pieces to a workgroup, or for short rows 16 lanes to a row.
+constexpr int kPiece = 16384, kShort = 256;
+constexpr int64_t kMostBytes = (int64_t)1 << 31;       // of a row of state
+struct CopyState {
+  const char* src;
+  char* dst;
+  const int32_t* live;
+  int64_t slot_bytes;
+  int32_t slots, pieces;                               // pieces 0: short rows, 16 to a workgroup
+  uint32_t first;                                      // first workgroup
+};
+struct ReorderArgs {
+  int K, count;
+  int64_t rows;
+  const int32_t* parent;
+  CopyState st[SLSTM_BEAM_MAX_STATES];
+};
+typedef u32x4 u32x4_byte __attribute__((aligned(1)));
+
+}  // namespace
+
+// Bound by memory: the live slots of the parents are read and written once.
+__global__ void __launch_bounds__(256) k_beam_reorder(ReorderArgs a) {
+  int q = 0;
+  while (q + 1 < a.count && blockIdx.x >= a.st[q + 1].first) ++q;
+  const CopyState& st = a.st[q];
+  const uint32_t id = blockIdx.x - st.first;
+  const bool wide = st.pieces > 0;
+  const int64_t row = wide ? id / st.pieces : (int64_t)id * 16 + (threadIdx.x >> 4);
+  if (row >= a.rows) return;
+  const int p = a.parent[row];
+  if (p < 0 || p >= a.K) return;
+  const int64_t from = row / a.K * a.K + p;
+  int live = st.slots;
+  if (st.live) live = min(max(st.live[from], 0), st.slots);
+  const int64_t bytes = live * st.slot_bytes, pitch = st.slots * st.slot_bytes;
+  const int64_t lo = wide ? (int64_t)(id % st.pieces) * kPiece : 0, hi = wide ? min(bytes, lo + kPiece) : bytes;
+  const char* s = st.src + from * pitch;
+  char* d = st.dst + row * pitch;
+  const int t = wide ? threadIdx.x : threadIdx.x & 15, nt = wide ? 256 : 16;
+  if (wide) {
+    u32x4 v[kPiece / 4096];
+#pragma unroll
+    for (int i = 0; i < kPiece / 4096; ++i) {
+      const int64_t o = lo + (i * 256 + t) * 16;
+      if (o + 16 <= hi) v[i] = *(const u32x4_byte*)(s + o);
+    }
+#pragma unroll
+    for (int i = 0; i < kPiece / 4096; ++i) {
+      const int64_t o = lo + (i * 256 + t) * 16;
+      if (o + 16 <= hi) *(u32x4_byte*)(d + o) = v[i];
+    }
+  } else {
+    for (int64_t o = t * 16; o + 16 <= hi; o += nt * 16) *(u32x4_byte*)(d + o) = *(const u32x4_byte*)(s + o);
+  }
+  if (hi > lo) {
+    const int64_t tail = lo + ((hi - lo) & ~(int64_t)15);
+    if (tail + t < hi) d[tail + t] = s[tail + t];
+  }
+}
+
+namespace {
+
+int beam_vecs(const slstm_beam_dims* d) { return d->type == SLSTM_F32 ? (d->V + 3) / 4 : (d->V + 7) / 8; }
+int beam_chunks(const slstm_beam_dims* d) { return (beam_vecs(d) + 256 * kPartVecs - 1) / (256 * kPartVecs); }
+bool beam_ok(const slstm_beam_dims* d) {
+  return d && d->B >= 0 && d->K >= 1 && d->K <= kMaxBeams && d->V >= 1 && d->V <= (1 << 22) &&
+         (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->eos >= -1 && stride_ok(d->ld_logits, d->V) &&
+         (int64_t)d->B * d->K * beam_chunks(d) <= 0x7fffffff;
+}
+bool beam_small(const slstm_beam_dims* d) { return (int64_t)d->K * d->V <= kSmall; }
+// As the rows of a loss: 8192 vectors in registers; rows of four chunks or more are cut where there is not one of
+// them for every compute unit.
+bool beam_cut(const slstm_beam_dims* d) {
+  return beam_vecs(d) > 8192 || (beam_chunks(d) >= 4 && (int64_t)d->B * d->K < 256);
+}
+size_t beam_part_bytes(const slstm_beam_dims* d) { return ((size_t)d->B * d->K * beam_chunks(d) * 8 + 255) & ~(size_t)255; }
+
+template <typename T>
+void beam_rows(const slstm_beam_dims* d, const BeamArgs& a, hipStream_t st) {
+  const unsigned rows = (unsigned)((int64_t)d->B * d->K);
+  const int n = beam_vecs(d);
+  if (beam_cut(d)) {
+    hipLaunchKernelGGL(k_beam_part<T>, dim3(rows * a.chunks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_beam_rows<T, 256, kPartVecs, true>), dim3(rows * a.chunks), dim3(256), 0, st, a);
+  } else if (n <= 1024) {
+    hipLaunchKernelGGL((k_beam_rows<T, 256, 4, false>), dim3(rows), dim3(256), 0, st, a);
+  } else if (n <= 2048) {
+    hipLaunchKernelGGL((k_beam_rows<T, 256, 8, false>), dim3(rows), dim3(256), 0, st, a);
+  } else if (n <= 4096) {
+    hipLaunchKernelGGL((k_beam_rows<T, 512, 8, false>), dim3(rows), dim3(512), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((k_beam_rows<T, 1024, 8, false>), dim3(rows), dim3(1024), 0, st, a);
+  }
+}
+
+}  // namespace
+
+extern "C" size_t stacklstm_beam_workspace_bytes(const slstm_beam_dims* d) {
+  if (!beam_ok(d)) return 0;
+  if (beam_small(d) || d->B == 0) return 4;
+  const bool cut = beam_cut(d);
+  return (cut ? beam_part_bytes(d) : 0) + (size_t)d->B * d->K * (cut ? beam_chunks(d) : 1) * d->K * 8;
+}
+
+extern "C" int stacklstm_beam_select(const slstm_beam_dims* d, const void* logits, const uint8_t* legal, const float* score,
+                                     const uint8_t* done, float* score_next, int32_t* parent, int32_t* token,
+                                     uint8_t* done_next, void* workspace, size_t ws_bytes, void* stream) {
+  if (!beam_ok(d)) return SLSTM_EINVAL;
+  if (d->B == 0) return SLSTM_OK;
+  if (!logits || !score || !score_next || !parent || !token || !done_next) return SLSTM_EINVAL;
+  BeamArgs a = {};
+  a.B = d->B, a.K = d->K, a.V = d->V, a.eos = d->eos;
+  a.x = logits, a.ldx = row_stride(d->ld_logits, d->V), a.legal = legal, a.done = done, a.score = score;
+  a.score_next = score_next, a.parent = parent, a.token = token, a.done_next = done_next;
+  const hipStream_t st = as_stream(stream);
+  if (beam_small(d)) {
+    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_beam_small<float>, dim3(d->B), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(k_beam_small<bf16_t>, dim3(d->B), dim3(256), 0, st, a);
+  } else {
+    if (!workspace || ((uintptr_t)workspace & 7u)) return SLSTM_EINVAL;
+    if (ws_bytes < stacklstm_beam_workspace_bytes(d)) return SLSTM_EWORKSPACE;
+    const bool cut = beam_cut(d);
+    a.chunks = cut ? beam_chunks(d) : 1;
+    a.part = (float*)workspace;
+    a.cand = (u64*)((char*)workspace + (cut ? beam_part_bytes(d) : 0));
+    if (d->type == SLSTM_F32) beam_rows<float>(d, a, st);
+    else beam_rows<bf16_t>(d, a, st);
+    hipLaunchKernelGGL(k_beam_merge, dim3(d->B), dim3(256), 0, st, a);
+  }
+  return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+}
+
+extern "C" int stacklstm_beam_reorder(const slstm_beam_dims* d, const int32_t* parent, const slstm_beam_state* states,
+                                      int32_t count, void* stream) {
+  if (!d || d->B < 0 || d->K < 1 || d->K > kMaxBeams || (int64_t)d->B * d->K > 0x7fffffff) return SLSTM_EINVAL;
+  if (count < 0 || count > SLSTM_BEAM_MAX_STATES) return SLSTM_EINVAL;
+  if (count == 0 || d->B == 0) return SLSTM_OK;
+  if (!parent || !states) return SLSTM_EINVAL;
+  ReorderArgs a = {};
+  a.K = d->K, a.count = count, a.rows = (int64_t)d->B * d->K, a.parent = parent;
+  int64_t blocks = 0;
+  for (int i = 0; i < count; ++i) {
+    const slstm_beam_state& s = states[i];
+    if (!s.src || !s.dst || s.slot_bytes < 1 || s.slots < 1 || s.reserved || s.slot_bytes > kMostBytes / s.slots)
+      return SLSTM_EINVAL;
+    const int64_t pitch = s.slot_bytes * s.slots;
+    const char* d0 = (const char*)s.dst;
+    // nothing is read from where a state is written
+    auto meets = [&](const void* p, int64_t bytes) {
+      const char* s0 = (const char*)p;
+      return p && d0 < s0 + bytes && s0 < d0 + pitch * a.rows;
+    };
+    if (meets(parent, a.rows * 4)) return SLSTM_EINVAL;
+    for (int j = 0; j < count; ++j) {
+      const slstm_beam_state& o = states[j];
+      if (o.slots < 1 || o.slot_bytes < 1 || o.slot_bytes > kMostBytes / o.slots) return SLSTM_EINVAL;
+      if (meets(o.src, o.slot_bytes * o.slots * a.rows) || meets(o.live, a.rows * 4)) return SLSTM_EINVAL;
+    }
+    CopyState& c = a.st[i];
+    c.src = (const char*)s.src, c.dst = (char*)s.dst, c.live = s.live, c.slot_bytes = s.slot_bytes, c.slots = s.slots;
+    const int64_t pieces = pitch <= kShort ? 0 : (pitch + kPiece - 1) / kPiece;
+    const int64_t n = pieces ? pieces * a.rows : (a.rows + 15) / 16;
+    if (pieces > 0x7fffffff || blocks + n > 0x7fffffff) return SLSTM_EINVAL;
+    c.pieces = (int32_t)pieces;
+    c.first = (uint32_t)blocks;
+    blocks += n;
+  }
+  hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), a);
+  return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+}

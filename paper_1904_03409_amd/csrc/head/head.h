@@ -1,0 +1,144 @@
+// Shared device helpers of the operators behind the recurrence (include/stacklstm_head.h).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../common.h"
+
+// Rows are read and written in vectors of 16 bytes from the row's first element on, whatever the
+// row's alignment (global memory instructions need none on gfx950); the last vector of a row whose
+// width is no whole number of vectors goes element by element.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+template <typename T> struct vec;
+template <> struct vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(u32x4 r, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&v)[4]) {
+    return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
+};
+template <> struct vec<bf16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(u32x4 r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(r[i] << 16);
+      v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+  }
+  // nearest even, the one rounding of a 16-bit output
+  static __device__ __forceinline__ u32x4 pack(const float (&v)[8]) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r[i] = (uint32_t)f32_to_bf16_bits(v[2 * i]) | (uint32_t)f32_to_bf16_bits(v[2 * i + 1]) << 16;
+    return r;
+  }
+};
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(bf16_t v) { return bf16_bits_to_f32(v); }
+__device__ __forceinline__ void from_f32(float& d, float v) { d = v; }
+__device__ __forceinline__ void from_f32(bf16_t& d, float v) { d = f32_to_bf16_bits(v); }
+
+// Vector i of a row of W elements, `pad` (the bits of 32 bits' worth of elements) past the row's end.
+constexpr uint32_t kPadZero = 0u;
+template <typename T> constexpr uint32_t kPadLow = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // -inf
+template <typename T>
+__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W, uint32_t pad = kPadZero) {
+  constexpr int V = vec<T>::N;
+  if ((i + 1) * V <= W) return *(const u32x4_any*)(row + i * V);
+  u32x4 r = {pad, pad, pad, pad};
+  if constexpr (V == 4) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (i * V + k < W) r[k] = __float_as_uint(row[i * V + k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 7; ++k)
+      if (i * V + k < W) {
+        const uint32_t e = row[i * V + k];
+        r[k / 2] = k & 1 ? (r[k / 2] & 0xffffu) | e << 16 : (r[k / 2] & 0xffff0000u) | e;
+      }
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(T* row, int i, int W, const float (&v)[vec<T>::N]) {
+  constexpr int V = vec<T>::N;
+  if ((i + 1) * V <= W) {
+    *(u32x4_any*)(row + i * V) = vec<T>::pack(v);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < V - 1; ++k)
+    if (i * V + k < W) from_f32(row[i * V + k], v[k]);
+}
+
+// Packed values that are unpacked again behind this point, instead of being kept unpacked in registers.
+__device__ __forceinline__ void opaque_vec(u32x4& v) { asm volatile("" : "+v"(v)); }
+// Order between a wave's LDS stores and its other lanes' loads of them.
+__device__ __forceinline__ void wave_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Reductions over groups of N neighbouring lanes (N a power of two up to 64), the result in every
+// lane: DPP moves inside a row of 16 lanes, row and half swaps above it; no LDS.
+struct op_sum { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct op_max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <typename Op>
+__device__ __forceinline__ float row_swap(float v, Op op) {        // lane ^ 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <typename Op>
+__device__ __forceinline__ float half_swap(float v, Op op) {       // lane ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <int N, typename Op>
+__device__ __forceinline__ float lanes(float v, Op op) {
+  if constexpr (N >= 2) v = op(v, dpp_move<0xb1>(v));              // quad_perm 1, 0, 3, 2
+  if constexpr (N >= 4) v = op(v, dpp_move<0x4e>(v));              // quad_perm 2, 3, 0, 1
+  if constexpr (N >= 8) v = op(v, dpp_move<0x141>(v));             // row_half_mirror
+  if constexpr (N >= 16) v = op(v, dpp_move<0x140>(v));            // row_mirror
+  if constexpr (N >= 32) v = row_swap(v, op);
+  if constexpr (N >= 64) v = half_swap(v, op);
+  return v;
+}
+// The other way round: over the lanes that have the same place in their group of N, the groups of a wave joined.
+template <int N, typename Op>
+__device__ __forceinline__ float across(float v, Op op) {
+  if constexpr (N <= 8) v = op(v, __shfl_xor(v, 8));
+  if constexpr (N <= 16) v = row_swap(v, op);
+  if constexpr (N <= 32) v = half_swap(v, op);
+  return v;
+}
+// Over a workgroup of NT threads (N <= 64: over the lane's group of N), the result in every thread. `red`:
+// NT / 64 floats of LDS that no other reduction in flight uses; one barrier.
+template <int NT, typename Op>
+__device__ __forceinline__ float group_reduce(float v, Op op, float* red) {
+  v = lanes<(NT < 64 ? NT : 64)>(v, op);
+  if constexpr (NT > 64) {
+    constexpr int W = NT / 64;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lanes<W>(red[threadIdx.x & (W - 1)], op);
+  }
+  return v;
+}
+
+// Host side: a row stride as given (0: dense), and whether one may be.
+static inline int64_t row_stride(int64_t ld, int64_t width) { return ld ? ld : width; }
+static inline bool stride_ok(int64_t ld, int64_t width) { return ld == 0 || (ld >= width && ld <= ((int64_t)1 << 40)); }
+static inline hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
