@@ -5,8 +5,9 @@
 // W of dx) or with k as the row ("tall": W of y, both operands of dW). A flat operand's slice is kept in LDS by rows
 // of 128 bytes and read 16 bytes a lane; a tall one's by its rows of k, and is read transposed (16-bit) or element by
 // element (fp32). 16-byte granules are permuted within a row so that fragment reads spread over the banks.
-// Slices reach LDS by DMA where every operand is 16-bit and aligned, a few slices ahead; otherwise through
-// registers, one slice ahead, with the rows' ends cut off there.
+// Slices reach LDS by DMA, a few slices ahead. That takes operands of whole 16-byte granules: those at odd places or
+// of odd widths are first copied to padded rows in the work space (k_linear_pad; dz is written there anyhow). For few rows,
+// where a copy of W would cost more than it gives, slices go through registers, with the rows' ends cut off there.
 // Where the tiles do not fill the chip the sum over k is split, and k_linear_join adds the parts and applies the
 // epilogue.
 #include <algorithm>
@@ -27,12 +28,16 @@ struct GemmArgs {
   float* part;                                         // [splits][M][N], NULL: none
 };
 
+// sigma(2 sqrt(2/pi) (z + 0.044715 z^3)): 1 / (1 + 2^(z (k + k3 z^2)))
+__device__ __forceinline__ float gelu_gate(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * (z * z * -0.10294324f - 2.3022082f)));
+}
 __device__ __forceinline__ float act_fwd(float z, int act) {
   switch (act) {
     case SLSTM_ACT_RELU: return z > 0.f ? z : z != z ? z : 0.f;
     case SLSTM_ACT_TANH: return tanhf_(z);
     case SLSTM_ACT_SILU: return z * sigmoidf_(z);
-    case SLSTM_ACT_GELU: return z * sigmoidf_(1.5957691216057308f * (z + 0.044715f * z * z * z));
+    case SLSTM_ACT_GELU: return z * gelu_gate(z);
     default: return z;
   }
 }
@@ -49,24 +54,21 @@ __device__ __forceinline__ float act_bwd(float z, int act) {
       return s * (1.f + z * (1.f - s));
     }
     case SLSTM_ACT_GELU: {
-      const float s = sigmoidf_(1.5957691216057308f * (z + 0.044715f * z * z * z));
+      const float s = gelu_gate(z);
       return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * z * z);
     }
     default: return 1.f;
   }
 }
 
-// One row piece of the epilogue: v[] at column n of row m.
+// One row piece of the epilogue: v[] at column n of row m, with its bias and residual.
 template <typename T>
-__device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int n, float (&v)[vec<T>::N]) {
+__device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int n, float (&v)[vec<T>::N], const float (&b)[vec<T>::N],
+                                       u32x4 res) {
   constexpr int V = vec<T>::N;
   const int left = g.N - n;
-  if (g.bias) {
-    float b[V];
-    vec<T>::unpack(load_vec((const T*)g.bias + n, 0, left), b);
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] += b[k];
-  }
+  for (int k = 0; k < V; ++k) v[k] += b[k];
   if (g.z) store_vec((T*)g.z + m * g.N + n, 0, left, v);
   if (g.act != SLSTM_ACT_NONE) {
 #pragma unroll
@@ -74,22 +76,33 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int n, floa
   }
   if (g.res) {
     float r[V];
-    vec<T>::unpack(load_vec((const T*)g.res + m * g.ldr + n, 0, left), r);
+    vec<T>::unpack(res, r);
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] += r[k];
   }
   store_vec((T*)g.y + m * g.ldy + n, 0, left, v);
 }
+template <typename T>
+__device__ __forceinline__ void load_bias(const GemmArgs& g, int n, float (&b)[vec<T>::N]) {
+  vec<T>::unpack(g.bias && n < g.N ? load_vec((const T*)g.bias + n, 0, g.N - n) : u32x4{0u, 0u, 0u, 0u}, b);
+}
+template <typename T>
+__device__ __forceinline__ u32x4 load_res(const GemmArgs& g, int64_t m, int n) {
+  return g.res ? load_vec((const T*)g.res + m * g.ldr + n, 0, g.N - n) : u32x4{0u, 0u, 0u, 0u};
+}
 
-// Sizes of a block tile. A slice is 128 bytes of k: 64 (16-bit) or 32 (fp32).
+// Sizes of a block tile. A slice of k is 128 bytes of each flat row, whole cache lines (64 bytes at a time took twice the
+// requests: the product below at 1150 TFLOP/s instead of 1212); a step of it 64 bytes (32 k of 16 bits, 16 of fp32): one
+// (four) matrix instructions of a pair of fragments.
+constexpr int kSteps = 2;
 template <typename T, int BM, int BN>
 struct Tile {
-  static constexpr int BK = 128 / (int)sizeof(T), NT = BM == 256 ? 512 : 256, WN = BM == 256 ? 4 : 2, WM = NT / 64 / WN;
+  static constexpr int BK = 128 / (int)sizeof(T);
+  static constexpr int NT = BM == 256 ? 512 : 256, WN = BM == 256 ? 4 : 2, WM = NT / 64 / WN;
   static constexpr int MI = BM / WM / 16, NJ = BN / WN / 16;
-  static constexpr int ABYTES = BM * 128, BBYTES = BN * 128, STAGE = ABYTES + BBYTES;
-  static constexpr int IA = BM * 8 / NT, IB = BN * 8 / NT;       // granules of a thread
+  static constexpr int ABYTES = BM * 128, BBYTES = BN * 128;
+  static constexpr int IA = ABYTES / 16 / NT, IB = BBYTES / 16 / NT;       // granules of a thread
 };
-constexpr int gemm_lds(int stage, int stages) { return stage * stages; }
 
 // Place of granule c of a slice's row r (flat: r a row of the operand, tall: r a k).
 template <typename T, bool TALL, int ROWS>
@@ -107,222 +120,341 @@ __device__ __forceinline__ void place(int L, int& r, int& c) {
   c = (L % G) ^ swz<T, TALL, ROWS>(r);
 }
 
-}  // namespace
+// A lane's 16 bytes of k of one 16-row tile and step.
+template <typename T> struct frag_of { typedef f32x4 type; };
+template <> struct frag_of<bf16_t> { typedef bf16x8 type; };
+template <typename T, bool TALL, int ROWS>
+__device__ __forceinline__ typename frag_of<T>::type load_frag(const unsigned char* p, int tile, int step, int l16, int lq) {
+  const int r = 16 * tile + l16;
+  if constexpr (!TALL) {
+    return *(const typename frag_of<T>::type*)(p + (r * 8 + ((4 * step + lq) ^ swz<T, TALL, ROWS>(r))) * 16);
+  } else if constexpr (sizeof(T) == 2) {
+    // transposed: the lane gives the address of k row 8 lq + l16 / 4 and columns 4 (l16 % 4) of the tile, and gets
+    // column l16, four k
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    constexpr int G = ROWS / 8;
+    const int k = 8 * lq + (l16 >> 2);
+    const unsigned char* q = p + (step * 32 + k) * G * 16 + ((2 * tile + ((l16 & 3) >> 1)) ^ swz<T, TALL, ROWS>(k)) * 16 + (l16 & 1) * 8;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * G * 16));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    f32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int k = 16 * step + 4 * lq + q;
+      v[q] = *(const float*)(p + (k * (ROWS / 4) + ((r >> 2) ^ swz<T, TALL, ROWS>(k))) * 16 + (r & 3) * 4);
+    }
+    return v;
+  }
+}
+// The products of row tile i of a step. C^T = B^T A^T: a lane holds row l16 and columns 4 lq .. 4 lq + 3 of a tile. (fp32:
+// a lane's four k go to four instructions, for both operands alike.)
+template <typename T, int NJ>
+__device__ __forceinline__ void mma(const typename frag_of<T>::type& a, const typename frag_of<T>::type (&b)[NJ], f32x4 (&acc)[NJ]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[j] = mfma_bf16_16x16x32(b[j], a, acc[j]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][q], a[q], acc[j], 0, 0, 0);
+  }
+}
 
-template <typename T, bool AT, bool BT, int BM, int BN, bool DMA, int NS>
-__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g) {
-  typedef Tile<T, BM, BN> S;
-  constexpr int V = vec<T>::N, BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ;
-  static_assert(!DMA || sizeof(T) == 2, "DMA of 16-bit operands");
-  extern __shared__ __align__(16) unsigned char sm[];
+// Which tile and which part of k a workgroup has.
+struct Where {
+  int split, m0, n0, kbeg, kend, nr, nc;
+};
+template <int BM, int BN>
+__device__ __forceinline__ Where where(const GemmArgs& g) {
+  Where w;
   const int NTL = (g.N + BN - 1) / BN, MTL = (g.M + BM - 1) / BM, tiles = NTL * MTL, all = tiles * g.splits;
   int lid = (int)blockIdx.x;
   // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of tiles, in groups of 8 row tiles to a
   // column tile, so that what its L2 holds is used again
-  {
-    const int full = all & ~7;
-    if (lid < full) lid = (lid & 7) * (full >> 3) + (lid >> 3);
-  }
-  const int zs = lid / tiles;
-  lid -= zs * tiles;
+  const int full = all & ~7;
+  if (lid < full) lid = (lid & 7) * (full >> 3) + (lid >> 3);
+  w.split = uni(lid / tiles);
+  lid -= w.split * tiles;
   constexpr int GM = 8;
   const int gi = lid / (GM * NTL), gm = min(GM, MTL - gi * GM), rem = lid - gi * GM * NTL;
-  const int m0 = (gi * GM + rem % gm) * BM, n0 = (rem / gm) * BN;
-  const int kbeg = min(g.K, zs * g.chunk), kend = min(g.K, kbeg + g.chunk);
-  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
-  const int nr = min(BM, g.M - m0), nc = min(BN, g.N - n0);
-  const T* A = (const T*)g.A + (AT ? m0 : (int64_t)m0 * g.lda);
-  const T* B = (const T*)g.B + (BT ? n0 : (int64_t)n0 * g.ldb);
+  w.m0 = uni((gi * GM + rem % gm) * BM);               // (scalar registers: descriptors are made of them)
+  w.n0 = uni((rem / gm) * BN);
+  w.kbeg = min(g.K, w.split * g.chunk);
+  w.kend = min(g.K, w.kbeg + g.chunk);
+  w.nr = min(BM, g.M - w.m0);
+  w.nc = min(BN, g.N - w.n0);
+  return w;
+}
 
-  // DMA of the slice at k0 (past kend: nothing is read; the count of a wave's DMAs stays the same)
-  [[maybe_unused]] auto dma = [&](int k0, int buf, int part, int parts) {
-    unsigned char* st = sm + buf * S::STAGE;
-    auto one = [&](auto tall, auto rows, const T* p, int64_t ld, int n, unsigned char* to, int i) {
-      constexpr bool TALL = decltype(tall)::value;
-      constexpr int ROWS = decltype(rows)::value;
-      int r, c;
-      place<T, TALL, ROWS>((i * (NT / 64) + wave) * 64 + lane, r, c);
-      const int left = kend - k0;
-      const bool in = TALL ? r < left && c * V < n : r < n && c * V < left;
-      const T* base = TALL ? p + (int64_t)k0 * ld : p + k0;
-      const rsrc_t rs = make_rsrc(base, left > 0 ? (size_t)((TALL ? min(BK, left) - 1 : n - 1) * ld + (TALL ? n : min(BK, left))) * 2 : 0);
-      bdma16(rs, in ? (uint32_t)(r * (int)ld + c * V) * 2u : kOOB, 0u, lds_addr(to + (i * (NT / 64) + wave) * 1024));
-    };
+// A wave turns 16 rows of its tile at a time into row pieces of 16 bytes a lane. The residual's loads all go out first
+// (one after the other they took half the time of a tile: 256 x 256 of k = 1024 with gelu, z and residual 61 us, without
+// its epilogue 32). ws: 16 x (16 NJ + 4) floats of LDS of this wave.
+template <typename T, int MI, int NJ>
+__device__ __forceinline__ void epilogue(const GemmArgs& g, const Where& w, const f32x4 (&acc)[MI][NJ], int wm, int wn, int lane,
+                                         float* ws) {
+  constexpr int V = vec<T>::N, CW = 16 * NJ, LD = CW + 4, VR = 64 * V / CW, EP = 16 / VR;
+  const int l16 = lane & 15, lq = lane >> 4, er = lane / (CW / V), ec = (lane % (CW / V)) * V, n = w.n0 + CW * wn + ec;
+  u32x4 res[MI][EP];
+  float bias[V];
+  if (!g.part) {
+    load_bias<T>(g, n, bias);
 #pragma unroll
-    for (int i = 0; i < S::IA; ++i)
-      if (i % parts == part) one(std::integral_constant<bool, AT>(), std::integral_constant<int, BM>(), A, g.lda, nr, st, i);
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int i = 0; i < S::IB; ++i)
-      if ((S::IA + i) % parts == part)
-        one(std::integral_constant<bool, BT>(), std::integral_constant<int, BN>(), B, g.ldb, nc, st + S::ABYTES, i);
-  };
-  // the same through registers
-  [[maybe_unused]] u32x4 ra[S::IA], rb[S::IB];
-  [[maybe_unused]] auto fetch = [&](int k0) {
-    const int left = kend - k0;
-#pragma unroll
-    for (int i = 0; i < S::IA; ++i) {
-      int r, c;
-      place<T, AT, BM>(i * NT + tid, r, c);
-      const bool in = left > 0 && r < (AT ? left : nr);
-      ra[i] = in ? load_vec(A + (AT ? (int64_t)(k0 + r) * g.lda : (int64_t)r * g.lda + k0), c, AT ? nr : left) : u32x4{0u, 0u, 0u, 0u};
-    }
-#pragma unroll
-    for (int i = 0; i < S::IB; ++i) {
-      int r, c;
-      place<T, BT, BN>(i * NT + tid, r, c);
-      const bool in = left > 0 && r < (BT ? left : nc);
-      rb[i] = in ? load_vec(B + (BT ? (int64_t)(k0 + r) * g.ldb : (int64_t)r * g.ldb + k0), c, BT ? nc : left) : u32x4{0u, 0u, 0u, 0u};
-    }
-  };
-  [[maybe_unused]] auto put = [&](int buf) {
-    unsigned char* st = sm + buf * S::STAGE;
-#pragma unroll
-    for (int i = 0; i < S::IA; ++i) *(u32x4*)(st + (i * NT + tid) * 16) = ra[i];
-#pragma unroll
-    for (int i = 0; i < S::IB; ++i) *(u32x4*)(st + S::ABYTES + (i * NT + tid) * 16) = rb[i];
-  };
-
-  f32x4 acc[MI][NJ];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  // products of a staged slice; between(i): behind those of row tile i of the first half
-  auto products = [&](const unsigned char* st, auto between) {
-    if constexpr (sizeof(T) == 2) {
-      typedef short s16x4 __attribute__((ext_vector_type(4)));
-      // a lane's 8 k of tile `tile`: from one row, or transposed: the lane gives the address of k row
-      // 8 lq + l16 / 4 and columns 4 (l16 % 4) of the tile, and gets column l16, four k
-      auto frag = [&](auto tall, auto rows, const unsigned char* p, int tile, int kc) {
-        constexpr bool TALL = decltype(tall)::value;
-        constexpr int ROWS = decltype(rows)::value;
-        if constexpr (!TALL) {
-          const int r = 16 * tile + l16;
-          return *(const bf16x8*)(p + (r * 8 + ((4 * kc + lq) ^ swz<T, TALL, ROWS>(r))) * 16);
-        } else {
-          constexpr int G = ROWS / 8;
-          const int k = 8 * lq + (l16 >> 2);
-          const unsigned char* q = p + (kc * 32 + k) * G * 16 + ((2 * tile + ((l16 & 3) >> 1)) ^ swz<T, TALL, ROWS>(k)) * 16 + (l16 & 1) * 8;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * G * 16));
-          return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-      };
-#pragma unroll
-      for (int kc = 0; kc < 2; ++kc) {
-        bf16x8 a[MI], b[NJ];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) a[i] = frag(std::integral_constant<bool, AT>(), std::integral_constant<int, BM>(), st, MI * wm + i, kc);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-          b[j] = frag(std::integral_constant<bool, BT>(), std::integral_constant<int, BN>(), st + S::ABYTES, NJ * wn + j, kc);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[i][j] = mfma_bf16_16x16x32(b[j], a[i], acc[i][j]);
-          if (kc == 0) between(i);
-        }
+      for (int e = 0; e < EP; ++e) {
+        const int m = 16 * (MI * wm + i) + e * VR + er;
+        res[i][e] = m < w.nr && n < g.N ? load_res<T>(g, w.m0 + m, n) : u32x4{0u, 0u, 0u, 0u};
       }
-    } else {
-      // a lane's four k (4 lq .. 4 lq + 3 of 16) go to four instructions, for both operands alike
-      auto frag = [&](auto tall, auto rows, const unsigned char* p, int tile, int kc) {
-        constexpr bool TALL = decltype(tall)::value;
-        constexpr int ROWS = decltype(rows)::value;
-        const int r = 16 * tile + l16;
-        if constexpr (!TALL) {
-          return *(const f32x4*)(p + (r * 8 + ((4 * kc + lq) ^ swz<T, TALL, ROWS>(r))) * 16);
-        } else {
-          f32x4 v;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int k = 16 * kc + 4 * lq + q;
-            v[q] = *(const float*)(p + (k * (ROWS / 4) + ((r >> 2) ^ swz<T, TALL, ROWS>(k))) * 16 + (r & 3) * 4);
-          }
-          return v;
-        }
-      };
-#pragma unroll
-      for (int kc = 0; kc < 2; ++kc) {
-        f32x4 a[MI], b[NJ];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) a[i] = frag(std::integral_constant<bool, AT>(), std::integral_constant<int, BM>(), st, MI * wm + i, kc);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-          b[j] = frag(std::integral_constant<bool, BT>(), std::integral_constant<int, BN>(), st + S::ABYTES, NJ * wn + j, kc);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][q], a[i][q], acc[i][j], 0, 0, 0);
-          if (kc == 0) between(i);
-        }
-      }
-    }
-  };
-
-  if constexpr (DMA) {
-    constexpr int PER = S::IA + S::IB;
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s) dma(kbeg + s * BK, s, 0, 1);
-    int buf = 0;
-    for (int k0 = kbeg; k0 < kend; k0 += BK) {
-      wait_vm<(NS - 2) * PER>();
-      __syncthreads();                                 // this slice landed, the stage before it is free
-      const int next = buf == 0 ? NS - 1 : buf - 1;
-      products(sm + buf * S::STAGE, [&](int i) { dma(k0 + (NS - 1) * BK, next, i, MI); });
-      buf = buf + 1 == NS ? 0 : buf + 1;
-    }
-    wait_vm<0>();
-  } else {
-    static_assert(NS == 2, "two stages");
-    fetch(kbeg);
-    int buf = 0;
-    for (int k0 = kbeg; k0 < kend; k0 += BK, buf ^= 1) {
-      put(buf);
-      __syncthreads();
-      if (k0 + BK < kend) fetch(k0 + BK);
-      products(sm + buf * S::STAGE, [](int) {});
-    }
   }
-  __syncthreads();                                     // the stages are free
-
-  // a wave turns 16 rows of its tile at a time into row pieces of 16 bytes a lane
-  constexpr int CW = 16 * NJ, LD = CW + 4, VR = 64 * V / CW;
-  float* ws = reinterpret_cast<float*>(sm) + wave * (16 * LD);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) *(f32x4*)&ws[l16 * LD + j * 16 + 4 * lq] = acc[i][j];
     wave_lds();
 #pragma unroll
-    for (int e = 0; e < 16 / VR; ++e) {
-      const int r = e * VR + lane / (CW / V), c = (lane % (CW / V)) * V;
-      const int m = 16 * (MI * wm + i) + r, n = n0 + CW * wn + c;
-      if (m >= nr || n >= g.N) continue;
+    for (int e = 0; e < EP; ++e) {
+      const int r = e * VR + er, m = 16 * (MI * wm + i) + r;
+      if (m >= w.nr || n >= g.N) continue;
       float v[V];
 #pragma unroll
       for (int k = 0; k < V; k += 4) {
-        const f32x4 q = *(const f32x4*)&ws[r * LD + c + k];
+        const f32x4 q = *(const f32x4*)&ws[r * LD + ec + k];
 #pragma unroll
         for (int h = 0; h < 4; ++h) v[k + h] = q[h];
       }
       if (g.part) {
-        float* o = g.part + ((int64_t)zs * g.M + m0 + m) * g.N + n;
+        float* o = g.part + ((int64_t)w.split * g.M + w.m0 + m) * g.N + n;
 #pragma unroll
         for (int k = 0; k < V; k += 4) {
-          const float w[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
-          store_vec(o, k / 4, g.N - n, w);
+          const float p[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
+          store_vec(o, k / 4, g.N - n, p);
         }
       } else {
-        finish<T>(g, m0 + m, n, v);
+        finish<T>(g, w.m0 + m, n, v, bias, res[i][e]);
       }
     }
     wave_lds();
   }
+}
+
+// The DMA of an operand's slices: a lane's offsets are the same in every slice. Flat: the slice's start goes into the scalar
+// offset, and a lane past the end of k reads nothing; tall: into the descriptor's base, whose end stops rows past it.
+template <typename T, bool TALL, int ROWS, int NT, int I>
+struct Mover {
+  uint32_t off[I];
+  int col[I];                                          // flat: first k of the lane's granule
+  const T* base;
+  int64_t ld;
+  rsrc_t rs;
+  int n;
+  __device__ __forceinline__ void start(const T* p, int64_t ld_, int n_, int k, int wave, int lane) {
+    constexpr int V = vec<T>::N;
+    base = p, ld = ld_, n = n_;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      int r, c;
+      place<T, TALL, ROWS>((i * (NT / 64) + wave) * 64 + lane, r, c);
+      col[i] = c * V;
+      off[i] = (TALL ? c * V < n : r < n) ? (uint32_t)(r * (int)ld + c * V) * (uint32_t)sizeof(T) : kOOB;
+    }
+    // (rows are whole granules in memory: a padded one's last is there)
+    if (!TALL) rs = make_rsrc(base, (size_t)((n - 1) * ld + (k + V - 1) / V * V) * sizeof(T));
+  }
+  // slice at k0 of a k that ends at kend
+  __device__ __forceinline__ void slice(int k0, int kend) {
+    constexpr int V = vec<T>::N, BK = 128 / (int)sizeof(T);
+    if (TALL) {
+      const int rows = uni(max(0, min(BK, kend - k0)));
+      // (no row: a descriptor of no bytes)
+      rs = make_rsrc(base + (int64_t)k0 * ld, (size_t)(rows * ld - (rows > 0 ? ld - (n + V - 1) / V * V : 0)) * sizeof(T));
+    }
+  }
+  __device__ __forceinline__ void go(int i, int k0, int kend, unsigned char* to, int wave) {
+    uint32_t o = off[i], so = 0;
+    if (!TALL) {
+      o = k0 + col[i] < kend ? o : kOOB;
+      so = __builtin_amdgcn_readfirstlane((uint32_t)k0 * (uint32_t)sizeof(T));
+      asm volatile("" : "+s"(so));                     // (in a register: the instruction takes no literal there)
+    }
+    bdma16(rs, o, so, lds_addr(to + (i * (NT / 64) + wave) * 1024));
+  }
+};
+
+}  // namespace
+
+// Operands of whole granules, by DMA into SA and SB stages of LDS. A row tile's fragment of the next step is read as soon as
+// its products of this step are issued, so reads from LDS go along with the products; the columns' fragments have two sets.
+// In a slice's last step the waves meet: the next slice has landed, everybody has read what it needs of this one, and its
+// stages take later slices. The operand that comes from memory (the other one is read again and again from L2) is further
+// ahead: three stages of it and two of the other fill a CU's LDS at 256 x 256.
+// 2 x 65536 x 1024 x 4096 flop of 16 bits, random values, dx: with fragments read at the start of each slice, two stages, 1090
+// TFLOP/s.
+template <typename T, bool AT, bool BT, int BM, int BN, int SA, int SB>
+__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g) {
+  typedef Tile<T, BM, BN> S;
+  typedef typename frag_of<T>::type frag;
+  constexpr int BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ, MEET = MI >= 4 ? 1 : 0;
+  static_assert(SA - SB <= 1 && SB - SA <= 1 && SA >= 2 && SB >= 2, "stages");
+  extern __shared__ __align__(16) unsigned char sm[];
+  const Where w = where<BM, BN>(g);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
+  Mover<T, AT, BM, NT, S::IA> ma;
+  Mover<T, BT, BN, NT, S::IB> mb;
+  ma.start((const T*)g.A + (AT ? w.m0 : (int64_t)w.m0 * g.lda), g.lda, w.nr, g.K, wave, lane);
+  mb.start((const T*)g.B + (BT ? w.n0 : (int64_t)w.n0 * g.ldb), g.ldb, w.nc, g.K, wave, lane);
+  auto stage_a = [&](int i) { return sm + i * S::ABYTES; };
+  auto stage_b = [&](int i) { return sm + SA * S::ABYTES + i * S::BBYTES; };
+  auto move_a = [&](int i, int k0, int buf) { ma.go(i, k0, w.kend, stage_a(buf), wave); };
+  auto move_b = [&](int i, int k0, int buf) { mb.go(i, k0, w.kend, stage_b(buf), wave); };
+  f32x4 acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < (SA > SB ? SA : SB); ++s) {
+    const int k = w.kbeg + s * BK;
+    if (s < SA) {
+      ma.slice(k, w.kend);
+#pragma unroll
+      for (int i = 0; i < S::IA; ++i) move_a(i, k, s);
+    }
+    if (s < SB) {
+      mb.slice(k, w.kend);
+#pragma unroll
+      for (int i = 0; i < S::IB; ++i) move_b(i, k, s);
+    }
+  }
+  frag a[MI], b[2][NJ];
+  auto read_a = [&](const unsigned char* st, int step, int i) { a[i] = load_frag<T, AT, BM>(st, MI * wm + i, step, l16, lq); };
+  auto read_b = [&](const unsigned char* st, int step, frag (&f)[NJ]) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) f[j] = load_frag<T, BT, BN>(st, NJ * wn + j, step, l16, lq);
+  };
+  wait_vm<(SA - 1) * S::IA + (SB - 1) * S::IB>();
+  __syncthreads();                                     // the first slice landed
+  // (in the loop's order: a wait at its head holds for both ways in)
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  read_b(stage_b(0), 0, b[0]);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    read_a(stage_a(0), 0, i);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  int ia = 0, ib = 0;                                  // stages of the slice at k0
+  for (int k0 = w.kbeg; k0 < w.kend; k0 += BK) {
+    const int na = ia + 1 == SA ? 0 : ia + 1, nb = ib + 1 == SB ? 0 : ib + 1;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const bool last = s + 1 == kSteps;
+      const unsigned char *pa = stage_a(last ? na : ia), *pb = stage_b(last ? nb : ib);
+      const int step = last ? 0 : s + 1;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        mma<T, NJ>(a[i], b[s & 1], acc[i]);
+        if (i == MEET) {
+          if (last) {
+            wait_vm<(SA - 2) * S::IA + (SB - 2) * S::IB>();
+            __syncthreads();
+            ma.slice(k0 + SA * BK, w.kend);
+            mb.slice(k0 + SB * BK, w.kend);
+          }
+          read_b(pb, step, b[(s & 1) ^ 1]);
+#pragma unroll
+          for (int h = 0; h <= MEET; ++h) read_a(pa, step, h);
+        } else if (i > MEET) {
+          read_a(pa, step, i);
+        }
+        // DMAs, a few behind each row tile: the nearer slice's first
+        if (last && i >= MEET) {
+          constexpr int PER = S::IA + S::IB, PARTS = MI - MEET;
+          const int p0 = (i - MEET) * PER / PARTS, p1 = (i - MEET + 1) * PER / PARTS;
+#pragma unroll
+          for (int p = 0; p < PER; ++p) {
+            if (p < p0 || p >= p1) continue;
+            if (SA >= SB) {
+              if (p < S::IB) move_b(p, k0 + SB * BK, ib);
+              else move_a(p - S::IB, k0 + SA * BK, ia);
+            } else {
+              if (p < S::IA) move_a(p, k0 + SA * BK, ia);
+              else move_b(p - S::IA, k0 + SB * BK, ib);
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    ia = na;
+    ib = nb;
+  }
+  wait_vm<0>();
+  __syncthreads();                                     // the stages are free
+  epilogue<T, MI, NJ>(g, w, acc, wm, wn, lane, reinterpret_cast<float*>(sm) + wave * (16 * (16 * NJ + 4)));
+}
+
+// Operands at any place, through registers, one slice ahead; two stages.
+template <typename T, bool AT, bool BT, int BM, int BN>
+__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArgs g) {
+  typedef Tile<T, BM, BN> S;
+  typedef typename frag_of<T>::type frag;
+  constexpr int BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ;
+  extern __shared__ __align__(16) unsigned char sm[];
+  const Where w = where<BM, BN>(g);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
+  const T* A = (const T*)g.A + (AT ? w.m0 : (int64_t)w.m0 * g.lda);
+  const T* B = (const T*)g.B + (BT ? w.n0 : (int64_t)w.n0 * g.ldb);
+  u32x4 ra[S::IA], rb[S::IB];
+  auto fetch = [&](int k0) {
+    const int left = w.kend - k0;
+#pragma unroll
+    for (int i = 0; i < S::IA; ++i) {
+      int r, c;
+      place<T, AT, BM>(i * NT + tid, r, c);
+      const bool in = left > 0 && r < (AT ? left : w.nr);
+      ra[i] = in ? load_vec(A + (AT ? (int64_t)(k0 + r) * g.lda : (int64_t)r * g.lda + k0), c, AT ? w.nr : left) : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < S::IB; ++i) {
+      int r, c;
+      place<T, BT, BN>(i * NT + tid, r, c);
+      const bool in = left > 0 && r < (BT ? left : w.nc);
+      rb[i] = in ? load_vec(B + (BT ? (int64_t)(k0 + r) * g.ldb : (int64_t)r * g.ldb + k0), c, BT ? w.nc : left) : u32x4{0u, 0u, 0u, 0u};
+    }
+  };
+  f32x4 acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  fetch(w.kbeg);
+  int buf = 0;
+  for (int k0 = w.kbeg; k0 < w.kend; k0 += BK, buf ^= 1) {
+    unsigned char* st = sm + buf * (S::ABYTES + S::BBYTES);
+#pragma unroll
+    for (int i = 0; i < S::IA; ++i) *(u32x4*)(st + (i * NT + tid) * 16) = ra[i];
+#pragma unroll
+    for (int i = 0; i < S::IB; ++i) *(u32x4*)(st + S::ABYTES + (i * NT + tid) * 16) = rb[i];
+    __syncthreads();
+    if (k0 + BK < w.kend) fetch(k0 + BK);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      frag a[MI], b[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) b[j] = load_frag<T, BT, BN>(st + S::ABYTES, NJ * wn + j, s, l16, lq);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) a[i] = load_frag<T, AT, BM>(st, MI * wm + i, s, l16, lq);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) mma<T, NJ>(a[i], b, acc[i]);
+    }
+  }
+  __syncthreads();                                     // the stages are free
+  epilogue<T, MI, NJ>(g, w, acc, wm, wn, lane, reinterpret_cast<float*>(sm) + wave * (16 * (16 * NJ + 4)));
 }
 
 // The parts of a split product added in order, and the epilogue.
@@ -337,6 +469,10 @@ __global__ void __launch_bounds__(256) k_linear_join(GemmArgs g) {
     float v[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] = 0.f;
+    float b[V];
+    load_bias<T>(g, n, b);
+    const u32x4 res = load_res<T>(g, m, n);
+#pragma unroll 8
     for (int s = 0; s < g.splits; ++s) {
       const float* p = g.part + ((int64_t)s * g.M + m) * g.N + n;
 #pragma unroll
@@ -347,7 +483,7 @@ __global__ void __launch_bounds__(256) k_linear_join(GemmArgs g) {
         for (int h = 0; h < 4; ++h) v[k + h] += w[h];
       }
     }
-    finish<T>(g, m, n, v);
+    finish<T>(g, m, n, v, b, res);
   }
 }
 
@@ -384,7 +520,7 @@ __global__ void __launch_bounds__(256) k_linear_dz(DzArgs a) {
       }
 #pragma unroll
       for (int k = 0; k < V; ++k) s[k] += d[k];
-      if (a.dz) store_vec((T*)a.dz + m * a.ldz, c, a.N, d);
+      if (a.dz) store_vec((T*)a.dz + m * a.ldz, c, (int)a.ldz, d);       // (zeros to the end of the padded row)
     }
   }
   if (!a.part) return;
@@ -398,6 +534,34 @@ __global__ void __launch_bounds__(256) k_linear_dz(DzArgs a) {
 #pragma unroll
     for (int r = 0; r < 8; ++r) v += red[r][i];
     a.part[(int64_t)blockIdx.y * a.N + n] = v;
+  }
+}
+
+namespace {
+struct PadArgs {
+  struct {
+    const void* src;
+    void* dst;
+    int64_t rows, ld;
+    int cols;
+  } op[2];
+  uint32_t first;                                      // first workgroup of the second
+};
+}  // namespace
+
+// Rows copied to rows of whole granules, zeros behind their ends; 16 rows to a workgroup.
+template <typename T>
+__global__ void __launch_bounds__(256) k_linear_pad(PadArgs a) {
+  constexpr int V = vec<T>::N;
+  const bool second = blockIdx.x >= a.first;
+  const auto& o = a.op[second];
+  const int nv = (o.cols + V - 1) / V;
+  const int64_t r0 = (int64_t)(blockIdx.x - (second ? a.first : 0)) * 16, n = min((int64_t)16, o.rows - r0) * nv;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < n; i += 256) {
+    const int64_t r = r0 + (uint32_t)i / (uint32_t)nv;
+    const int c = (int)((uint32_t)i % (uint32_t)nv);
+    *(u32x4*)((T*)o.dst + (r * nv + c) * V) = load_vec((const T*)o.src + r * o.ld, c, o.cols);
   }
 }
 
@@ -421,29 +585,34 @@ __global__ void __launch_bounds__(256) k_linear_db(const float* part, int P, int
 namespace {
 
 bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-// How a product runs: block tile, parts of k, and whether its operands go to LDS by DMA.
+// How a product runs: block tile, parts of k.
 struct Plan {
   int tile, splits, chunk;
-  bool dma;
 };
-// The largest tile that fills three quarters of the 256 CUs, k split where that helps (a part takes at least
-// eight slices); 256 x 256 only by DMA, and no tile of which more than half would be past the end.
-Plan gemm_plan(int64_t M, int64_t N, int64_t K, int type, bool dma) {
-  const int BK = type == SLSTM_F32 ? 32 : 64;
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(64, K / (8 * BK)));
-  Plan p = {64, 1, 0, dma};
-  int64_t tiles = 0;
-  for (int t = dma ? 256 : 128; t >= 64; t /= 2) {
-    tiles = ((M + t - 1) / t) * ((N + t - 1) / t);
-    p.tile = t;
-    if (std::min(M, N) > t / 2 && tiles * most >= 192) break;
+// The tile and the split with the least estimated time. A CU has ceil(tiles / 256) tiles to do, a tile's time goes with its
+// products at the tile's share of the matrix rate (measured on large products; a smaller tile reads more operands to
+// a product), and split parts are written and read once more.
+Plan gemm_plan(int64_t M, int64_t N, int64_t K, int type, bool wide) {
+  const bool f32 = type == SLSTM_F32;
+  const int BK = f32 ? 32 : 64;
+  const int64_t slices = std::max<int64_t>(1, (K + BK - 1) / BK);
+  Plan best = {64, 1, (int)(slices * BK)};
+  double least = 1e300;
+  for (int t = wide && !f32 ? 256 : 128; t >= 64; t /= 2) {
+    const double rate = f32 ? (t == 128 ? 0.6 : 0.55) : t == 256 ? 4.2 : t == 128 ? 2.4 : 1.3;   // TFLOP/s a CU
+    const int64_t tiles = ((M + t - 1) / t) * ((N + t - 1) / t);
+    for (int64_t s = 1; s <= 64 && (s == 1 || (slices / s >= 4 && tiles * s <= 2048)); ++s) {
+      const int64_t per = (slices + s - 1) / s;
+      if ((slices + per - 1) / per != s) continue;
+      const double us = ((tiles * s + 255) / 256) * (2e-6 * t * t * (per + 2) * BK / rate) +
+                        (s > 1 ? 3 + (s + 1) * (double)M * N * 4 / 4e6 : 0);
+      if (us < least) {
+        least = us;
+        best = {t, (int)s, (int)(per * BK)};
+      }
+    }
   }
-  const int64_t want = p.tile == 256 ? 256 : 512;
-  if (tiles * 2 <= want) p.splits = (int)std::max<int64_t>(1, std::min(most, want / std::max<int64_t>(1, tiles)));
-  const int64_t slices = (K + BK - 1) / BK, per = (slices + p.splits - 1) / p.splits;
-  p.chunk = (int)(std::max<int64_t>(1, per) * BK);
-  p.splits = (int)std::max<int64_t>(1, (slices + per - 1) / std::max<int64_t>(1, per));
-  return p;
+  return best;
 }
 size_t part_bytes(const Plan& p, int64_t M, int64_t N) {
   return p.splits > 1 ? ((size_t)p.splits * M * N * 4 + 255) & ~(size_t)255 : 0;
@@ -454,38 +623,87 @@ size_t gemm_bytes(int64_t M, int64_t N, int64_t K, int type) {
   return type == SLSTM_F32 ? a : std::max(a, part_bytes(gemm_plan(M, N, K, type, true), M, N));
 }
 
-template <typename T, bool AT, bool BT, int TILE, bool DMA, int NS>
-hipError_t gemm_launch(const GemmArgs& g, hipStream_t st) {
-  auto kern = k_linear<T, AT, BT, TILE, TILE, DMA, NS>;
-  typedef Tile<T, TILE, TILE> S;
-  constexpr int lds = gemm_lds(S::STAGE, NS);
-  const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int threads, int lds, hipStream_t st) {
+  const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  const int64_t tiles = (((int64_t)g.M + TILE - 1) / TILE) * (((int64_t)g.N + TILE - 1) / TILE) * g.splits;
-  hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(S::NT), lds, st, g);
-  return hipGetLastError();
+  const int64_t tiles = (((int64_t)g.M + tile - 1) / tile) * (((int64_t)g.N + tile - 1) / tile) * g.splits;
+  GemmArgs a = g;
+  void* args[] = {&a};
+  return hipLaunchKernel(kern, dim3((unsigned)tiles), dim3(threads), args, lds, st);
 }
-// One product with its epilogue; g has the operands, the sizes and the outputs.
+template <typename T, bool AT, bool BT, int TILE, int SA, int SB>
+hipError_t launch_dma(const GemmArgs& g, hipStream_t st) {
+  typedef Tile<T, TILE, TILE> S;
+  return tile_launch((const void*)k_linear<T, AT, BT, TILE, TILE, SA, SB>, g, TILE, S::NT, S::ABYTES * SA + S::BBYTES * SB, st);
+}
+template <typename T, bool AT, bool BT, int TILE>
+hipError_t launch_any(const GemmArgs& g, hipStream_t st) {
+  typedef Tile<T, TILE, TILE> S;
+  return tile_launch((const void*)k_linear_any<T, AT, BT, TILE, TILE>, g, TILE, S::NT, (S::ABYTES + S::BBYTES) * 2, st);
+}
+
+// A matrix of rows as a product reads it. whole: its rows are whole granules at aligned places, in reach of a
+// descriptor's 32-bit offsets (in a padded copy: with zeros behind the row's end).
+struct Operand {
+  const void* p;
+  int64_t ld;
+  bool whole;
+};
+int granule(int type) { return type == SLSTM_F32 ? 4 : 8; }
+size_t esize(int type) { return type == SLSTM_F32 ? 4 : 2; }
+int64_t padded(int64_t cols, int type) { return (cols + granule(type) - 1) / granule(type) * granule(type); }
+constexpr int64_t kReach = 1 << 21;
+bool dims_whole(int64_t cols, int64_t ld, int type) { return cols % granule(type) == 0 && ld % granule(type) == 0 && ld <= kReach; }
+Operand as_is(const void* p, int64_t cols, int64_t ld, int type) { return {p, ld, al16(p) && dims_whole(cols, ld, type)}; }
+// Whether matrices at odd places are copied for this many rows of x, and a copy's bytes (by the dims alone).
+bool copies(int64_t M) { return M > 128; }
+bool needs_copy(int64_t M, int64_t cols, int64_t ld, int type) {
+  return copies(M) && !dims_whole(cols, ld, type) && padded(cols, type) <= kReach;
+}
+size_t copy_bytes(int64_t rows, int64_t cols, int type) { return ((size_t)rows * padded(cols, type) * esize(type) + 255) & ~(size_t)255; }
+
+// Copies of up to two matrices in one launch.
+struct Copies {
+  PadArgs a = {};
+  int n = 0;
+  int64_t blocks = 0;
+  Operand add(const void* src, int64_t rows, int64_t cols, int64_t ld, void* dst, int type) {
+    a.op[n].src = src, a.op[n].dst = dst, a.op[n].rows = rows, a.op[n].ld = ld, a.op[n].cols = (int)cols;
+    if (n == 0) a.first = 0xffffffffu;
+    else a.first = (uint32_t)blocks;
+    ++n;
+    blocks += (rows + 15) / 16;
+    return {dst, padded(cols, type), true};
+  }
+  hipError_t run(int type, hipStream_t st) const {
+    if (blocks == 0) return hipSuccess;
+    if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_pad<float>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(k_linear_pad<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
+};
+
+// One product with its epilogue; g has the sizes and the outputs.
 template <bool AT, bool BT>
-hipError_t gemm(GemmArgs g, int type, float* part, hipStream_t st) {
-  // DMA: 16-bit operands whose rows are whole granules at aligned places
-  const bool dma = type == SLSTM_BF16 && al16(g.A) && al16(g.B) && g.lda % 8 == 0 && g.ldb % 8 == 0 &&
-                   (AT ? g.M : g.K) % 8 == 0 && (BT ? g.N : g.K) % 8 == 0 && g.lda <= (1 << 22) && g.ldb <= (1 << 22);
+hipError_t gemm(GemmArgs g, const Operand& A, const Operand& B, int type, float* part, hipStream_t st) {
+  const bool dma = A.whole && B.whole;
+  g.A = A.p, g.lda = A.ld, g.B = B.p, g.ldb = B.ld;
   const Plan p = gemm_plan(g.M, g.N, g.K, type, dma);
   g.splits = p.splits;
   g.chunk = p.chunk;
   g.part = p.splits > 1 ? part : nullptr;
   hipError_t e;
-  if (type == SLSTM_F32)
-    e = p.tile == 128 ? gemm_launch<float, AT, BT, 128, false, 2>(g, st) : gemm_launch<float, AT, BT, 64, false, 2>(g, st);
-  else if (!dma)
-    e = p.tile == 128 ? gemm_launch<bf16_t, AT, BT, 128, false, 2>(g, st) : gemm_launch<bf16_t, AT, BT, 64, false, 2>(g, st);
-  else if (p.tile == 256)
-    e = gemm_launch<bf16_t, AT, BT, 256, true, 2>(g, st);
-  else
-    e = p.tile == 128 ? gemm_launch<bf16_t, AT, BT, 128, true, 2>(g, st) : gemm_launch<bf16_t, AT, BT, 64, true, 4>(g, st);
+  const bool big = p.tile == 128;
+  if (type == SLSTM_F32) {
+    if (dma) e = big ? launch_dma<float, AT, BT, 128, 3, 2>(g, st) : launch_dma<float, AT, BT, 64, 3, 3>(g, st);
+    else e = big ? launch_any<float, AT, BT, 128>(g, st) : launch_any<float, AT, BT, 64>(g, st);
+  } else {
+    if (!dma) e = big ? launch_any<bf16_t, AT, BT, 128>(g, st) : launch_any<bf16_t, AT, BT, 64>(g, st);
+    else if (p.tile == 256) e = launch_dma<bf16_t, AT, BT, 256, 3, 2>(g, st);
+    else e = big ? launch_dma<bf16_t, AT, BT, 128, 3, 2>(g, st) : launch_dma<bf16_t, AT, BT, 64, 3, 3>(g, st);
+  }
   if (e != hipSuccess || p.splits == 1) return e;
-  const int V = type == SLSTM_F32 ? 4 : 8;
+  const int V = granule(type);
   const int64_t n = (int64_t)g.M * ((g.N + V - 1) / V);
   const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 4096));
   if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_join<float>, grid, dim3(256), 0, st, g);
@@ -505,35 +723,50 @@ bool linear_ok(const slstm_linear_dims* d) {
   const int64_t most = 0x7fffffff;
   return tiles(d->M, d->N) <= most && tiles(d->M, d->K) <= most && tiles(d->K, d->N) <= most;
 }
-int esize(const slstm_linear_dims* d) { return d->type == SLSTM_F32 ? 4 : 2; }
 // Blocks of rows of k_linear_dz: about 2048 workgroups, none for fewer than 64 rows.
 struct DzPlan {
   int strips, blocks, rows;
 };
 DzPlan dz_plan(const slstm_linear_dims* d) {
   DzPlan p;
-  const int V = 16 / esize(d);
+  const int V = granule(d->type);
   p.strips = (d->N + 32 * V - 1) / (32 * V);
   const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(d->M + 63) / 64, 2048 / p.strips, 256}));
   p.rows = (int)(((d->M + want - 1) / want + 7) / 8 * 8);
   p.blocks = (int)std::max<int64_t>(1, (d->M + std::max(1, p.rows) - 1) / std::max(1, p.rows));
   return p;
 }
-size_t dz_stride(const slstm_linear_dims* d) { return ((size_t)d->N + 7) / 8 * 8; }
-size_t dz_bytes(const slstm_linear_dims* d) {
-  return d->act == SLSTM_ACT_NONE ? 0 : ((size_t)d->M * dz_stride(d) * esize(d) + 255) & ~(size_t)255;
+// Work space of a forward: copies of x and W, parts; of a backward: dz (or a copy of dy), copies of W and x, sums of
+// columns, parts.
+struct Spaces {
+  size_t dz, x, W, db, part, total;
+};
+Spaces fwd_spaces(const slstm_linear_dims* d) {
+  Spaces s = {};
+  s.x = 0;
+  s.W = s.x + (needs_copy(d->M, d->K, row_stride(d->ld_x, d->K), d->type) ? copy_bytes(d->M, d->K, d->type) : 0);
+  s.part = s.W + (needs_copy(d->M, d->N, row_stride(d->ld_w, d->N), d->type) ? copy_bytes(d->K, d->N, d->type) : 0);
+  s.total = s.part + gemm_bytes(d->M, d->N, d->K, d->type);
+  return s;
 }
-size_t db_bytes(const slstm_linear_dims* d) { return ((size_t)dz_plan(d).blocks * d->N * 4 + 255) & ~(size_t)255; }
+Spaces bwd_spaces(const slstm_linear_dims* d) {
+  Spaces s = {};
+  const bool dz = d->act != SLSTM_ACT_NONE || needs_copy(d->M, d->N, row_stride(d->ld_dy, d->N), d->type);
+  s.x = dz ? copy_bytes(d->M, d->N, d->type) : 0;
+  s.W = s.x + (needs_copy(d->M, d->K, row_stride(d->ld_x, d->K), d->type) ? copy_bytes(d->M, d->K, d->type) : 0);
+  s.db = s.W + (needs_copy(d->M, d->N, row_stride(d->ld_w, d->N), d->type) ? copy_bytes(d->K, d->N, d->type) : 0);
+  s.part = s.db + (((size_t)dz_plan(d).blocks * d->N * 4 + 255) & ~(size_t)255);
+  s.total = s.part + std::max(gemm_bytes(d->M, d->K, d->N, d->type), gemm_bytes(d->K, d->N, d->M, d->type));
+  return s;
+}
 
 }  // namespace
 
 extern "C" size_t stacklstm_linear_fwd_workspace_bytes(const slstm_linear_dims* d) {
-  if (!linear_ok(d)) return 0;
-  return std::max<size_t>(4, gemm_bytes(d->M, d->N, d->K, d->type));
+  return linear_ok(d) ? std::max<size_t>(4, fwd_spaces(d).total) : 0;
 }
 extern "C" size_t stacklstm_linear_bwd_workspace_bytes(const slstm_linear_dims* d) {
-  if (!linear_ok(d)) return 0;
-  return dz_bytes(d) + db_bytes(d) + std::max(gemm_bytes(d->M, d->K, d->N, d->type), gemm_bytes(d->K, d->N, d->M, d->type));
+  return linear_ok(d) ? std::max<size_t>(4, bwd_spaces(d).total) : 0;
 }
 
 extern "C" int stacklstm_linear_fwd(const slstm_linear_dims* d, const void* x, const void* W, const void* b, const void* res,
@@ -542,13 +775,21 @@ extern "C" int stacklstm_linear_fwd(const slstm_linear_dims* d, const void* x, c
   if (d->M == 0) return SLSTM_OK;
   if (!x || !W || !y || !workspace || !al16(workspace)) return SLSTM_EINVAL;
   if (res == y && row_stride(d->ld_res, d->N) != row_stride(d->ld_y, d->N)) return SLSTM_EINVAL;
-  if (ws_bytes < stacklstm_linear_fwd_workspace_bytes(d)) return SLSTM_EWORKSPACE;
+  const Spaces s = fwd_spaces(d);
+  if (ws_bytes < s.total) return SLSTM_EWORKSPACE;
+  const hipStream_t st = as_stream(stream);
+  char* ws = (char*)workspace;
+  const int64_t ldx = row_stride(d->ld_x, d->K), ldw = row_stride(d->ld_w, d->N);
+  Copies cp;
+  const Operand ox = s.W > s.x ? cp.add(x, d->M, d->K, ldx, ws + s.x, d->type) : as_is(x, d->K, ldx, d->type);
+  const Operand ow = s.part > s.W ? cp.add(W, d->K, d->N, ldw, ws + s.W, d->type) : as_is(W, d->N, ldw, d->type);
+  hipError_t e = cp.run(d->type, st);
   GemmArgs g = {};
-  g.M = (int)d->M, g.N = d->N, g.K = d->K, g.A = x, g.B = W;
-  g.lda = row_stride(d->ld_x, d->K), g.ldb = row_stride(d->ld_w, d->N);
+  g.M = (int)d->M, g.N = d->N, g.K = d->K;
   g.bias = b, g.res = res, g.y = y, g.z = z, g.act = d->act;
   g.ldy = row_stride(d->ld_y, d->N), g.ldr = row_stride(d->ld_res, d->N);
-  return gemm<false, true>(g, d->type, (float*)workspace, as_stream(stream)) == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+  if (e == hipSuccess) e = gemm<false, true>(g, ox, ow, d->type, (float*)(ws + s.part), st);
+  return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }
 
 extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, const void* W, const void* z, const void* dy,
@@ -557,40 +798,46 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
   const bool act = d->act != SLSTM_ACT_NONE;
   if (!workspace || !al16(workspace)) return SLSTM_EINVAL;
   if (d->M > 0 && (!dy || (act && !z) || (dW && !x) || (dx && !W))) return SLSTM_EINVAL;
-  if (ws_bytes < stacklstm_linear_bwd_workspace_bytes(d)) return SLSTM_EWORKSPACE;
+  const Spaces s = bwd_spaces(d);
+  if (ws_bytes < s.total) return SLSTM_EWORKSPACE;
+  if (d->M == 0) dx = nullptr;
   const hipStream_t st = as_stream(stream);
   char* ws = (char*)workspace;
-  float* dbp = (float*)(ws + dz_bytes(d));
-  float* part = (float*)(ws + dz_bytes(d) + db_bytes(d));
-  const void* dz = act ? ws : dy;
-  const int64_t ldz = act ? (int64_t)dz_stride(d) : row_stride(d->ld_dy, d->N);
+  const int64_t ldx = row_stride(d->ld_x, d->K), ldw = row_stride(d->ld_w, d->N), ldd = row_stride(d->ld_dy, d->N);
+  const bool product = dx || dW, own = s.x > s.dz && product && d->M > 0;
+  Operand oz = as_is(dy, d->N, ldd, d->type);
+  if (own) oz = {ws + s.dz, padded(d->N, d->type), padded(d->N, d->type) <= kReach};
   hipError_t e = hipSuccess;
-  if (db || (act && (dx || dW) && d->M > 0)) {
+  if (db || own) {
     const DzPlan p = dz_plan(d);
     DzArgs a = {};
     a.M = (int)d->M, a.N = d->N, a.act = d->act, a.rows = p.rows, a.dy = dy, a.z = act ? z : nullptr;
-    a.ldd = row_stride(d->ld_dy, d->N), a.ldz = ldz, a.dz = act && (dx || dW) ? ws : nullptr, a.part = db ? dbp : nullptr;
+    a.ldd = ldd, a.ldz = padded(d->N, d->type), a.dz = own ? ws + s.dz : nullptr, a.part = db ? (float*)(ws + s.db) : nullptr;
     const dim3 grid(p.strips, p.blocks);
     if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_dz<float>, grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL(k_linear_dz<bf16_t>, grid, dim3(256), 0, st, a);
     if (db) {
       const dim3 cols((d->N + 7) / 8);
-      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(256), 0, st, dbp, p.blocks, d->N, (float*)db);
-      else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(256), 0, st, dbp, p.blocks, d->N, (bf16_t*)db);
+      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(256), 0, st, a.part, p.blocks, d->N, (float*)db);
+      else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(256), 0, st, a.part, p.blocks, d->N, (bf16_t*)db);
     }
     e = hipGetLastError();
   }
-  if (e == hipSuccess && dx && d->M > 0) {
+  Copies cp;
+  Operand ox = {}, ow = {};
+  if (dW) ox = s.W > s.x ? cp.add(x, d->M, d->K, ldx, ws + s.x, d->type) : as_is(x, d->K, ldx, d->type);
+  if (dx) ow = s.db > s.W ? cp.add(W, d->K, d->N, ldw, ws + s.W, d->type) : as_is(W, d->N, ldw, d->type);
+  if (e == hipSuccess) e = cp.run(d->type, st);
+  float* part = (float*)(ws + s.part);
+  if (e == hipSuccess && dx) {
     GemmArgs g = {};
-    g.M = (int)d->M, g.N = d->K, g.K = d->N, g.A = dz, g.B = W, g.lda = ldz, g.ldb = row_stride(d->ld_w, d->N);
-    g.y = dx, g.ldy = d->K;
-    e = gemm<false, false>(g, d->type, part, st);
+    g.M = (int)d->M, g.N = d->K, g.K = d->N, g.y = dx, g.ldy = d->K;
+    e = gemm<false, false>(g, oz, ow, d->type, part, st);
   }
   if (e == hipSuccess && dW) {
     GemmArgs g = {};
-    g.M = d->K, g.N = d->N, g.K = (int)d->M, g.A = x, g.B = dz, g.lda = row_stride(d->ld_x, d->K), g.ldb = ldz;
-    g.y = dW, g.ldy = d->N;
-    e = gemm<true, true>(g, d->type, part, st);
+    g.M = d->K, g.N = d->N, g.K = (int)d->M, g.y = dW, g.ldy = d->N;
+    e = gemm<true, true>(g, ox, oz, d->type, part, st);
   }
   return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }
