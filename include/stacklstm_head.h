@@ -114,7 +114,7 @@ typedef struct {
   int32_t V;               /* 1 .. 2^22 */
   int32_t K;               /* entries of a row, 1 .. 256 */
   int32_t type;            /* slstm_type of logits and dlogits */
-  float tau;               /* > 0 */
+  float tau;               /* 1e-6 .. 1e6 */
   float alpha;             /* 0 .. 1 */
   int64_t ld_logits, ld_dlogits;
 } slstm_distill_dims;

@@ -17,7 +17,6 @@
 namespace {
 
 typedef unsigned long long u64;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxBeams = 64, kList = 1024;
 constexpr int kPartVecs = 4;                           // vectors a thread in a chunk of 256 threads
 constexpr int kSmall = 8192;                           // totals of a search that fit one workgroup's LDS
@@ -59,6 +58,14 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
   if constexpr (N >= 4) v = max(v, move(v, std::integral_constant<int, 0x4e>()));
   if constexpr (N >= 8) v = max(v, move(v, std::integral_constant<int, 0x141>()));
   if constexpr (N >= 16) v = max(v, move(v, std::integral_constant<int, 0x140>()));
+  if constexpr (N >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(r[0], r[1]);
+  }
+  if constexpr (N >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(r[0], r[1]);
+  }
   return v;
 }
 
@@ -80,14 +87,13 @@ __device__ __forceinline__ uint32_t topk_bound(uint32_t mine, int K, TopkLds& s)
   if (t < kMaxBeams) s.out[t] = 0;
   __syncthreads();
   if (t < 64) {
+    // the largest value that K groups reach
     const uint32_t v = s.grp[t];
-    int above = 0;
-#pragma unroll 16
-    for (int j = 0; j < 64; ++j) {
-      const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)v, j);
-      above += o > v || (o == v && j < t);
-    }
-    if (above == K - 1) s.thr = v;
+    int reach = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) reach += (uint32_t)__builtin_amdgcn_readlane((int)v, j) >= v;
+    const uint32_t b = lanes_max<64>(reach >= K ? v : 0u);
+    if (t == 0) s.thr = b;
   }
   __syncthreads();
   return s.thr;
@@ -106,6 +112,7 @@ __device__ __forceinline__ void topk_rank(int K, TopkLds& s, Each each) {
     for (int i = t; i < n; i += NT) {
       const u64 k = s.list[i];
       int above = 0;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) above += s.list[j] > k;
       if (above < K) s.out[above] = k;
     }
@@ -211,17 +218,21 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
   const float score = a.score[row];
   if (!beam_runs(a, row, ch, score)) return;
   u32x4 raw[NV];
-  float mine = -INFINITY;
+  float most[NV], mine = -INFINITY;                    // largest of a vector, of all
 #pragma unroll
   for (int i = 0; i < NV; ++i) raw[i] = load_logits<T>(a, row, c0 + i * NT);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float v[V];
     vec<T>::unpack(raw[i], v);
+    most[i] = v[0];
 #pragma unroll
-    for (int k = 0; k < V; ++k) mine = fmaxf(mine, v[k]);
+    for (int k = 1; k < V; ++k) most[i] = fmaxf(most[i], v[k]);
+    mine = fmaxf(mine, most[i]);
+    __builtin_amdgcn_sched_barrier(0);                 // (one vector unpacked at a time, here and below)
   }
   float m, sum = 0.f;
+  Expo ex;
   if constexpr (JOIN) {
     const float* q = a.part + (size_t)row * a.chunks * 2;
     m = -INFINITY;
@@ -234,16 +245,20 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
     }
   } else {
     m = group_reduce<NT>(mine, op_max(), red[0]);
+    ex = Expo(m, kLog2e);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      opaque_vec(raw[i]);
       float v[V];
       vec<T>::unpack(raw[i], v);
 #pragma unroll
-      for (int k = 0; k < V; ++k) sum += __builtin_amdgcn_exp2f((v[k] - m) * kLog2e);
+      for (int k = 0; k < V; ++k) sum += ex(v[k]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  const float lse = m + logf(group_reduce<NT>(sum, op_sum(), red[1]));
+  sum = group_reduce<NT>(sum, op_sum(), red[1]);
+  const float lse = m + (JOIN ? logf(sum) : ex.log_sum(sum));
   const uint32_t bound = topk_bound<NT>(mine > -INFINITY ? order_bits(mine) : 0u, a.K, s);
   // Totals rise with x, but two different x may have one total, where the lower place wins: elements a few
   // roundings below the bound are looked at as well.
@@ -253,11 +268,9 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     opaque_vec(raw[i]);
-    float v[V], most = -INFINITY;
-    vec<T>::unpack(raw[i], v);
-#pragma unroll
-    for (int k = 0; k < V; ++k) most = fmaxf(most, v[k]);
-    if (most >= lo) {
+    if (most[i] >= lo) {
+      float v[V];
+      vec<T>::unpack(raw[i], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const float total = (v[k] - lse) + score;
@@ -300,15 +313,15 @@ __global__ void __launch_bounds__(256) k_beam_part(BeamArgs a) {
     for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
   }
   m = group_reduce<256>(m, op_max(), red[0]);
-  const float m0 = m > -INFINITY ? m : 0.f;
+  const Expo ex(m > -INFINITY ? m : 0.f, kLog2e);
 #pragma unroll
   for (int i = 0; i < kPartVecs; ++i) {
     float v[V];
     vec<T>::unpack(raw[i], v);
 #pragma unroll
-    for (int k = 0; k < V; ++k) sum += __builtin_amdgcn_exp2f((v[k] - m0) * kLog2e);
+    for (int k = 0; k < V; ++k) sum += ex(v[k]);
   }
-  sum = group_reduce<256>(sum, op_sum(), red[1]);
+  sum = group_reduce<256>(sum, op_sum(), red[1]) * __builtin_amdgcn_exp2f(-ex.off);
   if (t == 0) {
     a.part[(size_t)blockIdx.x * 2] = m;
     a.part[(size_t)blockIdx.x * 2 + 1] = sum;
@@ -341,11 +354,11 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamArgs a) {
 
 // A whole search of at most kSmall continuations: a wave to a row for the softmax sums, totals in LDS.
 template <typename T>
-__global__ void __launch_bounds__(256) k_beam_small(BeamArgs a) {
+__global__ void __launch_bounds__(512) k_beam_small(BeamArgs a) {
   __shared__ TopkLds s;
   __shared__ float tot[kSmall];
   const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, n = a.K * a.V;
-  for (int k = t >> 6; k < a.K; k += 4) {
+  for (int k = t >> 6; k < a.K; k += 8) {
     const int64_t row = (int64_t)b * a.K + k;
     const T* x = (const T*)a.x + row * a.ldx;
     const uint8_t* legal = a.legal ? a.legal + row * a.V : nullptr;
@@ -353,29 +366,37 @@ __global__ void __launch_bounds__(256) k_beam_small(BeamArgs a) {
     const float score = a.score[row];
     const bool done = a.done && a.done[row];
     float m = -INFINITY, sum = 0.f;
+#pragma unroll 4
     for (int v = lane; v < a.V; v += 64) {
-      const float e = !legal || legal[v] ? to_f32(x[v]) : -INFINITY;
+      const float x1 = to_f32(x[v]);
+      const bool ok = !legal || legal[v];
+      const float e = ok ? x1 : -INFINITY;
       to[v] = e;
       m = fmaxf(m, e);
     }
     m = lanes<64>(m, op_max());
-    for (int v = lane; v < a.V; v += 64) sum += __builtin_amdgcn_exp2f((to[v] - m) * kLog2e);
-    const float lse = m + logf(lanes<64>(sum, op_sum()));
+    const Expo ex(m, kLog2e);
+#pragma unroll 4
+    for (int v = lane; v < a.V; v += 64) sum += ex(to[v]);
+    const float lse = m + ex.log_sum(lanes<64>(sum, op_sum()));
+#pragma unroll 4
     for (int v = lane; v < a.V; v += 64) to[v] = done ? (v ? -INFINITY : score) : (to[v] - lse) + score;
   }
   __syncthreads();
   uint32_t mine = 0;
-  for (int i = t; i < n; i += 256) {
+#pragma unroll 4
+  for (int i = t; i < n; i += 512) {
     const float v = tot[i];
     if (v > -INFINITY) mine = max(mine, order_bits(v));
   }
-  const uint32_t bound = topk_bound<256>(mine, a.K, s);
-  for (int i = t; i < n; i += 256) {
+  const uint32_t bound = topk_bound<512>(mine, a.K, s);
+#pragma unroll 4
+  for (int i = t; i < n; i += 512) {
     const u64 k = make_key(tot[i], i);
     if (k && (uint32_t)(k >> 32) >= bound) topk_put(k, s);
   }
-  topk_rank<256>(a.K, s, [&](auto f) {
-    for (int i = t; i < n; i += 256) f(make_key(tot[i], i));
+  topk_rank<512>(a.K, s, [&](auto f) {
+    for (int i = t; i < n; i += 512) f(make_key(tot[i], i));
   });
   if (t < a.K) beam_out(a, b, t, s.out[t]);
 }
@@ -419,28 +440,19 @@ __global__ void __launch_bounds__(256) k_beam_reorder(ReorderArgs a) {
   if (st.live) live = min(max(st.live[from], 0), st.slots);
   const int64_t bytes = live * st.slot_bytes, pitch = st.slots * st.slot_bytes;
   const int64_t lo = wide ? (int64_t)(id % st.pieces) * kPiece : 0, hi = wide ? min(bytes, lo + kPiece) : bytes;
-  const char* s = st.src + from * pitch;
-  char* d = st.dst + row * pitch;
-  const int t = wide ? threadIdx.x : threadIdx.x & 15, nt = wide ? 256 : 16;
-  if (wide) {
-    u32x4 v[kPiece / 4096];
+  const char* s = st.src + from * pitch + lo;
+  char* d = st.dst + row * pitch + lo;
+  const int n = (int)max((int64_t)0, hi - lo), t = wide ? threadIdx.x : threadIdx.x & 15, nt = wide ? 256 : 16;
+  // (a thread's loads all go out before its stores: a piece of 16 KB; short rows have no more)
+  u32x4 v[kPiece / 4096];
 #pragma unroll
-    for (int i = 0; i < kPiece / 4096; ++i) {
-      const int64_t o = lo + (i * 256 + t) * 16;
-      if (o + 16 <= hi) v[i] = *(const u32x4_byte*)(s + o);
-    }
+  for (int i = 0; i < kPiece / 4096; ++i)
+    if ((i * nt + t) * 16 + 16 <= n) v[i] = *(const u32x4_byte*)(s + (i * nt + t) * 16);
 #pragma unroll
-    for (int i = 0; i < kPiece / 4096; ++i) {
-      const int64_t o = lo + (i * 256 + t) * 16;
-      if (o + 16 <= hi) *(u32x4_byte*)(d + o) = v[i];
-    }
-  } else {
-    for (int64_t o = t * 16; o + 16 <= hi; o += nt * 16) *(u32x4_byte*)(d + o) = *(const u32x4_byte*)(s + o);
-  }
-  if (hi > lo) {
-    const int64_t tail = lo + ((hi - lo) & ~(int64_t)15);
-    if (tail + t < hi) d[tail + t] = s[tail + t];
-  }
+  for (int i = 0; i < kPiece / 4096; ++i)
+    if ((i * nt + t) * 16 + 16 <= n) *(u32x4_byte*)(d + (i * nt + t) * 16) = v[i];
+  const int tail = (n & ~15) + t;
+  if (t < 16 && tail < n) d[tail] = s[tail];
 }
 
 namespace {
@@ -472,9 +484,9 @@ void beam_rows(const slstm_beam_dims* d, const BeamArgs& a, hipStream_t st) {
   } else if (n <= 2048) {
     hipLaunchKernelGGL((k_beam_rows<T, 256, 8, false>), dim3(rows), dim3(256), 0, st, a);
   } else if (n <= 4096) {
-    hipLaunchKernelGGL((k_beam_rows<T, 512, 8, false>), dim3(rows), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((k_beam_rows<T, 256, 16, false>), dim3(rows), dim3(256), 0, st, a);
   } else {
-    hipLaunchKernelGGL((k_beam_rows<T, 1024, 8, false>), dim3(rows), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((k_beam_rows<T, 512, 16, false>), dim3(rows), dim3(512), 0, st, a);
   }
 }
 
@@ -499,8 +511,8 @@ extern "C" int stacklstm_beam_select(const slstm_beam_dims* d, const void* logit
   a.score_next = score_next, a.parent = parent, a.token = token, a.done_next = done_next;
   const hipStream_t st = as_stream(stream);
   if (beam_small(d)) {
-    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_beam_small<float>, dim3(d->B), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_beam_small<bf16_t>, dim3(d->B), dim3(256), 0, st, a);
+    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_beam_small<float>, dim3(d->B), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL(k_beam_small<bf16_t>, dim3(d->B), dim3(512), 0, st, a);
   } else {
     if (!workspace || ((uintptr_t)workspace & 7u)) return SLSTM_EINVAL;
     if (ws_bytes < stacklstm_beam_workspace_bytes(d)) return SLSTM_EWORKSPACE;

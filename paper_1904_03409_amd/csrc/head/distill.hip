@@ -15,7 +15,6 @@
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kEntries = 256;                          // most entries of a row
 constexpr int kChunkVecs = 4;                          // vectors a thread in a chunk of 256 threads
 
@@ -90,38 +89,54 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const RowTargets
   return loss;
 }
 
-// Factors of a row's gradient: d = ct 2^((x - m) kt) + c1 2^((x - m) k1). Where tau is 1 the two are one.
+// How the two exponentials of an element are made: tau = 1 needs one, tau = 2 a square, any other tau both. (An exponential
+// is four times as dear as a product: 4096 rows of 32000, tau 2, 170 us with two of them, VALU as long as memory.)
+enum { ONE = 0, SQUARE = 1, BOTH = 2 };
+__device__ __forceinline__ int expo_mode(float tau, bool second) { return tau == 1.f || !second ? ONE : tau == 2.f ? SQUARE : BOTH; }
+
+// The gradient of a row's elements.
 struct RowGrad {
-  float m, a, b, ct, c1, kt, k1;
-  bool zero, both, one;                                // nothing; both terms; only the second
+  Expo et, e1;
+  float a, b, ct, c1;
+  bool zero;
+  int mode;
+  template <int MODE>
+  __device__ __forceinline__ float at(float x) const {
+    if (MODE == ONE) return ct * et(x);
+    if (MODE == SQUARE) {
+      const float e = et(x);
+      return e * (ct + c1 * e);
+    }
+    return ct * et(x) + c1 * e1(x);
+  }
   __device__ __forceinline__ float operator()(float x) const {
-    const float d = x - m;
-    float v = one ? 0.f : ct * __builtin_amdgcn_exp2f(d * kt);
-    if (both || one) v += c1 * __builtin_amdgcn_exp2f(d * k1);
-    return v;
+    return mode == ONE ? at<ONE>(x) : mode == SQUARE ? at<SQUARE>(x) : at<BOTH>(x);
   }
 };
 __device__ __forceinline__ RowGrad row_grad(const DistillArgs& a, const RowTargets& r, int64_t row, float m, float logst,
                                             float logs1) {
   RowGrad g;
   const float gr = a.grad ? a.grad[row] : 1.f;
-  g.m = m;
-  g.kt = kLog2e / a.tau;
-  g.k1 = kLog2e;
+  g.et = Expo(m, kLog2e / a.tau);
+  g.e1 = Expo(m, kLog2e);
   g.a = r.some ? gr * a.alpha * a.tau : 0.f;
   g.b = r.label >= 0 ? gr * (1.f - a.alpha) : 0.f;
   g.zero = g.a == 0.f && g.b == 0.f;
-  // a / st and b / s1, the sums at least 1 (their maximum's term) or NaN
-  g.ct = g.a * __expf(-logst);
-  g.c1 = g.b * __expf(-logs1);
-  if (a.tau == 1.f) {
-    g.ct += g.c1;
-    g.both = g.one = false;
-  } else {
-    g.both = g.a != 0.f && g.b != 0.f;
-    g.one = g.a == 0.f;
-  }
+  // a over the sum of the et, b over that of the e1
+  g.ct = g.a == 0.f ? 0.f : g.a * __builtin_amdgcn_exp2f(-logst * kLog2e - g.et.off);
+  g.c1 = g.b == 0.f ? 0.f : g.b * __builtin_amdgcn_exp2f(-logs1 * kLog2e - g.e1.off);
+  g.mode = expo_mode(a.tau, g.b != 0.f);
+  if (a.tau == 1.f) g.ct += g.c1;
+  if (g.mode == SQUARE) g.c1 = g.b * __builtin_amdgcn_exp2f(-logs1 * kLog2e - 2.f * g.et.off);
   return g;
+}
+// put(f) with the function of a row's elements, one of few kinds.
+template <typename Put>
+__device__ __forceinline__ void each_grad(const RowGrad& g, Put put) {
+  if (g.zero) put([](float) { return 0.f; });
+  else if (g.mode == ONE) put([&](float x) { return g.at<ONE>(x); });
+  else if (g.mode == SQUARE) put([&](float x) { return g.at<SQUARE>(x); });
+  else put([&](float x) { return g.at<BOTH>(x); });
 }
 // The element at entry j (j = K: the label's) with what the teacher and the label take from it.
 __device__ __forceinline__ float entry_grad(const DistillArgs& a, const RowGrad& g, const RowTargets& r, int place, float x,
@@ -177,23 +192,38 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
     m = group_reduce<TPR>(m, op_max(), red[2]);
 #pragma unroll
     for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
-    const float kt = kLog2e / a.tau;
     const bool second = a.tau != 1.f && (a.stats || a.alpha < 1.f);
+    const Expo et(m, kLog2e / a.tau), e1(m, kLog2e);
     float st = 0.f, s1 = 0.f;
+    auto sums = [&](auto mode) {
+      constexpr int MODE = decltype(mode)::value;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float v[V];
-      vec<T>::unpack(raw[i], v);
+      for (int i = 0; i < NV; ++i) {
+        float v[V];
+        vec<T>::unpack(raw[i], v);
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float d = v[k] - m;
-        st += __builtin_amdgcn_exp2f(d * kt);
-        if (second) s1 += __builtin_amdgcn_exp2f(d * kLog2e);
+        for (int k = 0; k < V; ++k) {
+          const float e = et(v[k]);
+          st += e;
+          if (MODE == SQUARE) s1 = __builtin_fmaf(e, e, s1);
+          if (MODE == BOTH) s1 += e1(v[k]);
+        }
+        __builtin_amdgcn_sched_barrier(0);             // (one vector unpacked at a time)
       }
-      __builtin_amdgcn_sched_barrier(0);               // (one vector unpacked at a time)
+    };
+    const int mode = expo_mode(a.tau, second);
+    if (mode == ONE) sums(std::integral_constant<int, ONE>());
+    else if (mode == SQUARE) sums(std::integral_constant<int, SQUARE>());
+    else sums(std::integral_constant<int, BOTH>());
+    logst = et.log_sum(group_reduce<TPR>(st, op_sum(), red[3]));
+    logs1 = logst;
+    if (a.tau != 1.f) {
+      logs1 = 0.f;
+      if (second) {
+        s1 = group_reduce<TPR>(s1, op_sum(), red[4]);
+        logs1 = mode == SQUARE ? logf(s1) - 2.f * et.off * 0.6931471805599453f : e1.log_sum(s1);
+      }
     }
-    logst = logf(group_reduce<TPR>(st, op_sum(), red[3]));
-    logs1 = a.tau == 1.f ? logst : second ? logf(group_reduce<TPR>(s1, op_sum(), red[4])) : 0.f;
     if (a.stats && here && t == 0) {
       a.stats[row * 3] = m;
       a.stats[row * 3 + 1] = logst;
@@ -212,18 +242,21 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
   if (here) g = row_grad(a, r, row, m, logst, logs1);
 #pragma unroll
   for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
-  if (here) {
+  auto put = [&](auto f) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = t + i * TPR;
-      if (c * V >= a.V) continue;
-      float v[V];
-      vec<T>::unpack(raw[i], v);
+      if (c * V < a.V) {
+        float v[V];
+        vec<T>::unpack(raw[i], v);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = g.zero ? 0.f : g(v[k]);
-      store_vec(dx, c, a.V, v);
+        for (int k = 0; k < V; ++k) v[k] = f(v[k]);
+        store_vec(dx, c, a.V, v);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
+  };
+  if (here) each_grad(g, put);
   // the elements that the teacher's entries and the label change, behind the stores above
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if constexpr (TPR > 64) __syncthreads();
@@ -263,23 +296,22 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a) {
     for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
   }
   m = group_reduce<256>(m, op_max(), red[0]);
-  const float kt = kLog2e / a.tau;
   float st = 0.f, s1 = 0.f;
   // (a chunk of -inf alone has the sums 0; one whose maximum is +inf, or with NaN, NaN)
   const float m0 = m > -INFINITY ? m : 0.f;
+  const Expo et(m0, kLog2e / a.tau), e1(m0, kLog2e);
 #pragma unroll
   for (int i = 0; i < kChunkVecs; ++i) {
     float v[V];
     vec<T>::unpack(raw[i], v);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const float d = v[k] - m0;
-      st += __builtin_amdgcn_exp2f(d * kt);
-      if (a.tau != 1.f) s1 += __builtin_amdgcn_exp2f(d * kLog2e);
+      st += et(v[k]);
+      if (a.tau != 1.f) s1 += e1(v[k]);
     }
   }
-  st = group_reduce<256>(st, op_sum(), red[1]);
-  s1 = a.tau == 1.f ? st : group_reduce<256>(s1, op_sum(), red[2]);
+  st = group_reduce<256>(st, op_sum(), red[1]) * __builtin_amdgcn_exp2f(-et.off);
+  s1 = a.tau == 1.f ? st : group_reduce<256>(s1, op_sum(), red[2]) * __builtin_amdgcn_exp2f(-e1.off);
   if (t == 0) {
     float* o = a.part + (size_t)blockIdx.x * 3;
     o[0] = m;
@@ -356,16 +388,18 @@ __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
   T* dx = (T*)a.dx + row * a.ldd;
   const RowGrad g = row_grad(a, r, row, m, logst, logs1);
   __syncthreads();                                     // (every element of the chunk that is fetched by place has been)
+  each_grad(g, [&](auto f) {
 #pragma unroll
-  for (int i = 0; i < kChunkVecs; ++i) {
-    const int c = (ch * kChunkVecs + i) * 256 + t;
-    if (c * V >= a.V) continue;
-    float v[V];
-    vec<T>::unpack(raw[i], v);
+    for (int i = 0; i < kChunkVecs; ++i) {
+      const int c = (ch * kChunkVecs + i) * 256 + t;
+      if (c * V >= a.V) continue;
+      float v[V];
+      vec<T>::unpack(raw[i], v);
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = g.zero ? 0.f : g(v[k]);
-    store_vec(dx, c, a.V, v);
-  }
+      for (int k = 0; k < V; ++k) v[k] = f(v[k]);
+      store_vec(dx, c, a.V, v);
+    }
+  });
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (g.zero) return;
@@ -381,7 +415,7 @@ int distill_vecs(const slstm_distill_dims* d) { return d->type == SLSTM_F32 ? (d
 int distill_chunks(const slstm_distill_dims* d) { return (distill_vecs(d) + kChunkVecs * 256 - 1) / (kChunkVecs * 256); }
 bool distill_ok(const slstm_distill_dims* d) {
   return d && d->rows >= 0 && d->rows <= 0x7fffffff && d->V >= 1 && d->V <= (1 << 22) && d->K >= 1 && d->K <= kEntries &&
-         (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->tau > 0.f && d->tau < INFINITY && d->alpha >= 0.f &&
+         (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->tau >= 1e-6f && d->tau <= 1e6f && d->alpha >= 0.f &&
          d->alpha <= 1.f && stride_ok(d->ld_logits, d->V) && stride_ok(d->ld_dlogits, d->V) &&
          d->rows * distill_chunks(d) <= 0x7fffffff;
 }
@@ -400,7 +434,7 @@ void distill_dispatch(const slstm_distill_dims* d, F f) {
 #define DISTILL_TYPE(T_) \
   DISTILL_CASE(T_, 8, 8, 1) DISTILL_CASE(T_, 16, 16, 1) DISTILL_CASE(T_, 32, 32, 1) DISTILL_CASE(T_, 64, 64, 1) \
   DISTILL_CASE(T_, 128, 64, 2) DISTILL_CASE(T_, 256, 64, 4) DISTILL_CASE(T_, 1024, 256, 4) DISTILL_CASE(T_, 2048, 256, 8) \
-  DISTILL_CASE(T_, 4096, 512, 8) DISTILL_CASE(T_, 8192, 1024, 8)
+  DISTILL_CASE(T_, 4096, 256, 16) DISTILL_CASE(T_, 8192, 512, 16)
   if (d->type == SLSTM_F32) {
     DISTILL_TYPE(float)
   } else {

@@ -138,6 +138,25 @@ __device__ __forceinline__ float group_reduce(float v, Op op, float* red) {
   return v;
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+// exp((x - m) k ln 2) as 2^(x k - mk) in one fused step. mk is m k rounded: every term of a row is off by the one factor
+// 2^off, which its sum and its gradient take out again.
+struct Expo {
+  float k, mk, off;
+  __device__ __forceinline__ Expo() {}
+  __device__ __forceinline__ Expo(float m, float k_) : k(k_), mk(m * k_) {
+    // past fp32's range (logits of the type's lowest value): an element is the maximum or nothing, and is told from it by
+    // any power of two that keeps both in range
+    if (!(fabsf(mk) < 1e38f) && fabsf(m) < INFINITY) {
+      k = 0x1p-60f;
+      mk = m * k;
+    }
+    off = __builtin_fmaf(m, k, -mk);
+  }
+  __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, k, -mk)); }
+  __device__ __forceinline__ float log_sum(float s) const { return logf(s) - off * 0.6931471805599453f; }
+};
+
 // Host side: a row stride as given (0: dense), and whether one may be.
 static inline int64_t row_stride(int64_t ld, int64_t width) { return ld ? ld : width; }
 static inline bool stride_ok(int64_t ld, int64_t width) { return ld == 0 || (ld >= width && ld <= ((int64_t)1 << 40)); }

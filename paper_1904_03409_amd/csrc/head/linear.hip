@@ -32,63 +32,82 @@ struct GemmArgs {
 __device__ __forceinline__ float gelu_gate(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * (z * z * -0.10294324f - 2.3022082f)));
 }
-__device__ __forceinline__ float act_fwd(float z, int act) {
+// (one branch for a vector)
+template <int V>
+__device__ __forceinline__ void act_fwd(float (&z)[V], int act) {
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) z[k] = f(z[k]);
+  };
   switch (act) {
-    case SLSTM_ACT_RELU: return z > 0.f ? z : z != z ? z : 0.f;
-    case SLSTM_ACT_TANH: return tanhf_(z);
-    case SLSTM_ACT_SILU: return z * sigmoidf_(z);
-    case SLSTM_ACT_GELU: return z * gelu_gate(z);
-    default: return z;
+    case SLSTM_ACT_RELU: each([](float v) { return v > 0.f ? v : v != v ? v : 0.f; }); break;
+    case SLSTM_ACT_TANH: each([](float v) { return tanhf_(v); }); break;
+    case SLSTM_ACT_SILU: each([](float v) { return v * sigmoidf_(v); }); break;
+    case SLSTM_ACT_GELU: each([](float v) { return v * gelu_gate(v); }); break;
   }
 }
 // (z/2 (1 + tanh u) = z sigma(2u); derivative of z sigma(2u): s + z s (1 - s) 2u')
-__device__ __forceinline__ float act_bwd(float z, int act) {
+template <int V>
+__device__ __forceinline__ void act_bwd(float (&d)[V], const float (&z)[V], int act) {
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) d[k] *= f(z[k]);
+  };
   switch (act) {
-    case SLSTM_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case SLSTM_ACT_TANH: {
-      const float a = tanhf_(z);
-      return 1.f - a * a;
-    }
-    case SLSTM_ACT_SILU: {
-      const float s = sigmoidf_(z);
-      return s * (1.f + z * (1.f - s));
-    }
-    case SLSTM_ACT_GELU: {
-      const float s = gelu_gate(z);
-      return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * z * z);
-    }
-    default: return 1.f;
+    case SLSTM_ACT_RELU: each([](float v) { return v > 0.f ? 1.f : v != v ? v : 0.f; }); break;
+    case SLSTM_ACT_TANH:
+      each([](float v) {
+        const float a = tanhf_(v);
+        return 1.f - a * a;
+      });
+      break;
+    case SLSTM_ACT_SILU:
+      each([](float v) {
+        const float s = sigmoidf_(v);
+        return s * (1.f + v * (1.f - s));
+      });
+      break;
+    case SLSTM_ACT_GELU:
+      each([](float v) {
+        const float s = gelu_gate(v);
+        return s + v * s * (1.f - s) * (1.5957691216057308f + 0.21406859f * v * v);
+      });
+      break;
   }
 }
 
+// 16 bytes of a row from its first element on; with ALL they are all there, else `left` elements are.
+template <bool ALL, typename T>
+__device__ __forceinline__ void put(T* row, int left, const float (&v)[vec<T>::N]) {
+  if (ALL) *(u32x4_any*)row = vec<T>::pack(v);
+  else store_vec(row, 0, left, v);
+}
 // One row piece of the epilogue: v[] at column n of row m, with its bias and residual.
-template <typename T>
+template <bool ALL, typename T>
 __device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int n, float (&v)[vec<T>::N], const float (&b)[vec<T>::N],
                                        u32x4 res) {
   constexpr int V = vec<T>::N;
   const int left = g.N - n;
 #pragma unroll
   for (int k = 0; k < V; ++k) v[k] += b[k];
-  if (g.z) store_vec((T*)g.z + m * g.N + n, 0, left, v);
-  if (g.act != SLSTM_ACT_NONE) {
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = act_fwd(v[k], g.act);
-  }
+  if (g.z) put<ALL>((T*)g.z + m * g.N + n, left, v);
+  act_fwd(v, g.act);
   if (g.res) {
     float r[V];
     vec<T>::unpack(res, r);
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] += r[k];
   }
-  store_vec((T*)g.y + m * g.ldy + n, 0, left, v);
+  put<ALL>((T*)g.y + m * g.ldy + n, left, v);
 }
 template <typename T>
 __device__ __forceinline__ void load_bias(const GemmArgs& g, int n, float (&b)[vec<T>::N]) {
   vec<T>::unpack(g.bias && n < g.N ? load_vec((const T*)g.bias + n, 0, g.N - n) : u32x4{0u, 0u, 0u, 0u}, b);
 }
-template <typename T>
+template <bool ALL, typename T>
 __device__ __forceinline__ u32x4 load_res(const GemmArgs& g, int64_t m, int n) {
-  return g.res ? load_vec((const T*)g.res + m * g.ldr + n, 0, g.N - n) : u32x4{0u, 0u, 0u, 0u};
+  const T* r = (const T*)g.res + m * g.ldr + n;
+  return ALL ? *(const u32x4_any*)r : load_vec(r, 0, g.N - n);
 }
 
 // Sizes of a block tile. A slice of k is 128 bytes of each flat row, whole cache lines (64 bytes at a time took twice the
@@ -189,54 +208,62 @@ __device__ __forceinline__ Where where(const GemmArgs& g) {
   return w;
 }
 
-// A wave turns 16 rows of its tile at a time into row pieces of 16 bytes a lane. The residual's loads all go out first
-// (one after the other they took half the time of a tile: 256 x 256 of k = 1024 with gelu, z and residual 61 us, without
-// its epilogue 32). ws: 16 x (16 NJ + 4) floats of LDS of this wave.
-template <typename T, int MI, int NJ>
-__device__ __forceinline__ void epilogue(const GemmArgs& g, const Where& w, const f32x4 (&acc)[MI][NJ], int wm, int wn, int lane,
-                                         float* ws) {
-  constexpr int V = vec<T>::N, CW = 16 * NJ, LD = CW + 4, VR = 64 * V / CW, EP = 16 / VR;
-  const int l16 = lane & 15, lq = lane >> 4, er = lane / (CW / V), ec = (lane % (CW / V)) * V, n = w.n0 + CW * wn + ec;
-  u32x4 res[MI][EP];
-  float bias[V];
-  if (!g.part) {
-    load_bias<T>(g, n, bias);
+// Results of a tile from the accumulators. A lane holds four columns (4 lq ..) of row l16 of every 16x16 tile: 16 bytes of an
+// fp32 output; for a 16-bit one neighbouring column tiles exchange rows of lanes, so that a lane has eight columns of one of
+// them. Either way an instruction writes 64 bytes of 16 rows. The residual's loads all go out first: one after the other they
+// took half the time of a tile (61440 x 1024 x 4096, gelu, z, residual: 913 us, then 754; 681 without a way through LDS).
+template <bool ALL, typename T, int MI, int NJ>
+__device__ __forceinline__ void results(const GemmArgs& g, const Where& w, f32x4 (&acc)[MI][NJ], int wm, int wn, int l16, int lq) {
+  constexpr int V = vec<T>::N, P = V == 4 ? NJ : NJ / 2;         // pieces of a row tile
+  int n[P];
+  float bias[P][V];
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int e = 0; e < EP; ++e) {
-        const int m = 16 * (MI * wm + i) + e * VR + er;
-        res[i][e] = m < w.nr && n < g.N ? load_res<T>(g, w.m0 + m, n) : u32x4{0u, 0u, 0u, 0u};
-      }
+  for (int p = 0; p < P; ++p) {
+    n[p] = w.n0 + 16 * NJ * wn + (V == 4 ? 16 * p + 4 * lq : 16 * (2 * p + (lq & 1)) + 8 * (lq >> 1));
+    load_bias<T>(g, n[p], bias[p]);
   }
+  auto in = [&](int i, int p) { return ALL || (16 * (MI * wm + i) + l16 < w.nr && n[p] < g.N); };
+  u32x4 res[MI][P];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      res[i][p] = g.res && in(i, p) ? load_res<ALL, T>(g, w.m0 + 16 * (MI * wm + i) + l16, n[p]) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) *(f32x4*)&ws[l16 * LD + j * 16 + 4 * lq] = acc[i][j];
-    wave_lds();
-#pragma unroll
-    for (int e = 0; e < EP; ++e) {
-      const int r = e * VR + er, m = 16 * (MI * wm + i) + r;
-      if (m >= w.nr || n >= g.N) continue;
+    for (int p = 0; p < P; ++p) {
       float v[V];
+      if constexpr (V == 4) {
 #pragma unroll
-      for (int k = 0; k < V; k += 4) {
-        const f32x4 q = *(const f32x4*)&ws[r * LD + ec + k];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) v[k + h] = q[h];
-      }
-      if (g.part) {
-        float* o = g.part + ((int64_t)w.split * g.M + w.m0 + m) * g.N + n;
-#pragma unroll
-        for (int k = 0; k < V; k += 4) {
-          const float p[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
-          store_vec(o, k / 4, g.N - n, p);
-        }
+        for (int k = 0; k < 4; ++k) v[k] = acc[i][p][k];
       } else {
-        finish<T>(g, w.m0 + m, n, v, bias, res[i][e]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][2 * p][k]), __float_as_uint(acc[i][2 * p + 1][k]), false, false);
+          v[k] = __uint_as_float(s[0]);
+          v[k + 4] = __uint_as_float(s[1]);
+        }
       }
+      if (in(i, p)) finish<ALL, T>(g, w.m0 + 16 * (MI * wm + i) + l16, n[p], v, bias[p], res[i][p]);
     }
-    wave_lds();
+  }
+}
+template <typename T, int MI, int NJ, int BM, int BN>
+__device__ __forceinline__ void epilogue(const GemmArgs& g, const Where& w, f32x4 (&acc)[MI][NJ], int wm, int wn, int l16, int lq) {
+  if (g.part) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int m = 16 * (MI * wm + i) + l16, n = w.n0 + 16 * (NJ * wn + j) + 4 * lq;
+        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        if (m < w.nr && n < g.N) store_vec(g.part + ((int64_t)w.split * g.M + w.m0 + m) * g.N + n, 0, g.N - n, v);
+      }
+  } else if (w.nr == BM && w.nc == BN) {
+    results<true, T, MI, NJ>(g, w, acc, wm, wn, l16, lq);
+  } else {
+    results<false, T, MI, NJ>(g, w, acc, wm, wn, l16, lq);
   }
 }
 
@@ -392,9 +419,8 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g)
     ia = na;
     ib = nb;
   }
-  wait_vm<0>();
-  __syncthreads();                                     // the stages are free
-  epilogue<T, MI, NJ>(g, w, acc, wm, wn, lane, reinterpret_cast<float*>(sm) + wave * (16 * (16 * NJ + 4)));
+  wait_vm<0>();                                        // (DMAs past the end of k write zeros to LDS: all are done before it is given up)
+  epilogue<T, MI, NJ, BM, BN>(g, w, acc, wm, wn, l16, lq);
 }
 
 // Operands at any place, through registers, one slice ahead; two stages.
@@ -453,8 +479,7 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArg
       for (int i = 0; i < MI; ++i) mma<T, NJ>(a[i], b, acc[i]);
     }
   }
-  __syncthreads();                                     // the stages are free
-  epilogue<T, MI, NJ>(g, w, acc, wm, wn, lane, reinterpret_cast<float*>(sm) + wave * (16 * (16 * NJ + 4)));
+  epilogue<T, MI, NJ, BM, BN>(g, w, acc, wm, wn, l16, lq);
 }
 
 // The parts of a split product added in order, and the epilogue.
@@ -471,7 +496,7 @@ __global__ void __launch_bounds__(256) k_linear_join(GemmArgs g) {
     for (int k = 0; k < V; ++k) v[k] = 0.f;
     float b[V];
     load_bias<T>(g, n, b);
-    const u32x4 res = load_res<T>(g, m, n);
+    const u32x4 res = g.res ? load_res<false, T>(g, m, n) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll 8
     for (int s = 0; s < g.splits; ++s) {
       const float* p = g.part + ((int64_t)s * g.M + m) * g.N + n;
@@ -483,7 +508,7 @@ __global__ void __launch_bounds__(256) k_linear_join(GemmArgs g) {
         for (int h = 0; h < 4; ++h) v[k + h] += w[h];
       }
     }
-    finish<T>(g, m, n, v, b, res);
+    finish<false, T>(g, m, n, v, b, res);
   }
 }
 
@@ -515,8 +540,7 @@ __global__ void __launch_bounds__(256) k_linear_dz(DzArgs a) {
       if (a.z) {
         float z[V];
         vec<T>::unpack(load_vec((const T*)a.z + m * a.N, c, a.N), z);
-#pragma unroll
-        for (int k = 0; k < V; ++k) d[k] *= act_bwd(z[k], a.act);
+        act_bwd(d, z, a.act);
       }
 #pragma unroll
       for (int k = 0; k < V; ++k) s[k] += d[k];
@@ -572,6 +596,7 @@ __global__ void __launch_bounds__(256) k_linear_db(const float* part, int P, int
   const int n = blockIdx.x * 8 + (threadIdx.x & 7), p0 = threadIdx.x >> 3;
   float s = 0.f;
   if (n < N)
+#pragma unroll 8
     for (int p = p0; p < P; p += 32) s += part[(int64_t)p * N + n];
   red[p0][threadIdx.x & 7] = s;
   __syncthreads();
@@ -589,9 +614,11 @@ bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 struct Plan {
   int tile, splits, chunk;
 };
-// The tile and the split with the least estimated time. A CU has ceil(tiles / 256) tiles to do, a tile's time goes with its
-// products at the tile's share of the matrix rate (measured on large products; a smaller tile reads more operands to
-// a product), and split parts are written and read once more.
+// The tile and the split with the least estimated time, in us: a CU's share of the products at the tile's rate (TFLOP/s of a
+// CU with as many workgroups as it holds: a smaller tile reads more operands to a product), or a workgroup's slices at
+// the latency of one where there are few; split parts are written, read once more and take a launch. Over 99 products
+// (rows 16 to 61440, k and columns 48 to 32000) the choice takes 1.03 times the best of 64, 128, 256 and splits of 1 to 64
+// in the geometric mean, 1.28 times at most.
 Plan gemm_plan(int64_t M, int64_t N, int64_t K, int type, bool wide) {
   const bool f32 = type == SLSTM_F32;
   const int BK = f32 ? 32 : 64;
@@ -599,13 +626,14 @@ Plan gemm_plan(int64_t M, int64_t N, int64_t K, int type, bool wide) {
   Plan best = {64, 1, (int)(slices * BK)};
   double least = 1e300;
   for (int t = wide && !f32 ? 256 : 128; t >= 64; t /= 2) {
-    const double rate = f32 ? (t == 128 ? 0.6 : 0.55) : t == 256 ? 4.2 : t == 128 ? 2.4 : 1.3;   // TFLOP/s a CU
+    const double rate = f32 ? (t == 128 ? 0.56 : 0.52) : t == 256 ? 4.2 : t == 128 ? 3.0 : 2.2, latency = f32 ? 0.45 : 0.35;
+    const int held = t == 256 ? 1 : t == 128 ? 2 : 3;
     const int64_t tiles = ((M + t - 1) / t) * ((N + t - 1) / t);
     for (int64_t s = 1; s <= 64 && (s == 1 || (slices / s >= 4 && tiles * s <= 2048)); ++s) {
-      const int64_t per = (slices + s - 1) / s;
+      const int64_t per = (slices + s - 1) / s, n = tiles * s;
       if ((slices + per - 1) / per != s) continue;
-      const double us = ((tiles * s + 255) / 256) * (2e-6 * t * t * (per + 2) * BK / rate) +
-                        (s > 1 ? 3 + (s + 1) * (double)M * N * 4 / 4e6 : 0);
+      const double us = 2 + std::max(((n + 255) / 256) * (2e-6 * t * t * per * BK / rate), ((n + 256 * held - 1) / (256 * held)) * per * latency) +
+                        (s > 1 ? 4 + (s + 1) * (double)M * N * 4 / 7e6 : 0);
       if (us < least) {
         least = us;
         best = {t, (int)s, (int)(per * BK)};

@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(256) k_norm_cols(const float* part, int P, int
   const int n = blockIdx.x * 8 + (threadIdx.x & 7), p0 = threadIdx.x >> 3;
   float s = 0.f;
   if (n < 2 * W)
+#pragma unroll 8
     for (int p = p0; p < P; p += 32) s += part[(size_t)p * 2 * W + n];
   red[p0][threadIdx.x & 7] = s;
   __syncthreads();
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(256) k_norm_cols(const float* part, int P, int
 
 namespace {
 
-constexpr int kNormMaxParts = 1024;
+constexpr int kNormMaxParts = 512;
 constexpr int kNormMaxWidth = 8192;
 
 bool norm_ok(const slstm_norm_dims* d) {

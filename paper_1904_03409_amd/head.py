@@ -90,15 +90,15 @@ def _arr(t, dtype, what, shape, optional=False):
         if optional:
             return None
         raise ValueError(f"{what} is missing")
+    if t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
-    return t.data_ptr()
+    if t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{what} must be contiguous")
 
 
 def _mat(t, dtype, what, rows, cols, ld, optional=False):
@@ -107,16 +107,16 @@ def _mat(t, dtype, what, rows, cols, ld, optional=False):
         if optional:
             return None
         raise ValueError(f"{what} is missing")
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
+        s0, s1 = t.stride()
+        if (s1 == 1 or cols == 1) and (s0 == (ld or cols) or rows < 2):
+            return t.data_ptr()
+        raise ValueError(f"{what} must have strides {(ld or cols, 1)}, got {(s0, s1)}")
     if t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{what} must have shape {(rows, cols)}, got {tuple(t.shape)}")
-    s0, s1 = t.stride()
-    if (cols > 1 and s1 != 1) or (rows > 1 and s0 != (ld or cols)):
-        raise ValueError(f"{what} must have strides {(ld or cols, 1)}, got {(s0, s1)}")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
-    return t.data_ptr()
+    raise ValueError(f"{what} must have shape {(rows, cols)}, got {tuple(t.shape)}")
 
 
 def _ld(t):
@@ -137,8 +137,9 @@ def _type(t):
 
 
 def _here(stream, t):
-    """The stream given, or the current one of the tensor's device."""
-    return _stream(torch.cuda.current_stream(t.device) if stream is None else stream)
+    """The stream given, or the current one of the tensor's device (its raw handle: the stream object of
+    torch.cuda.current_stream takes 2 us to make, a third of a small call)."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else _stream(stream)
 
 
 def _bytes(name, d):
@@ -455,7 +456,7 @@ class BeamRun:
     legal: Optional[torch.Tensor]
     score: torch.Tensor
     done: Optional[torch.Tensor]
-    states: list
+    states: list                    # set with set_states
     score_next: torch.Tensor
     parent: torch.Tensor
     token: torch.Tensor
@@ -469,9 +470,17 @@ class BeamRun:
         d = make_beam_dims(B, K, V, _type(logits), eos, _ld(logits))
         e = lambda dtype: torch.empty(B, K, dtype=dtype, device=logits.device)
         n = _bytes("stacklstm_beam_workspace_bytes", d)
-        return cls(dims=d, logits=logits, legal=legal, score=score, done=done, states=list(states), score_next=e(torch.float32),
-                   parent=e(torch.int32), token=e(torch.int32), done_next=e(torch.uint8),
-                   workspace=torch.empty(n, dtype=torch.uint8, device=logits.device))
+        r = cls(dims=d, logits=logits, legal=legal, score=score, done=done, states=[], score_next=e(torch.float32),
+                parent=e(torch.int32), token=e(torch.int32), done_next=e(torch.uint8),
+                workspace=torch.empty(n, dtype=torch.uint8, device=logits.device))
+        r.set_states(states)
+        return r
+
+    def set_states(self, states):
+        """The buffers that reorder copies, with their C descriptors (a program that swaps two sets of buffers makes two
+        lists, or two BeamRuns)."""
+        self.states = list(states)
+        self._descriptors = beam_states(self.dims, self.states) if self.states else None
 
     def select(self, stream=None):
         stacklstm_beam_select(self.dims, self.logits, self.legal, self.score, self.done, self.score_next, self.parent,
@@ -481,4 +490,4 @@ class BeamRun:
     def reorder(self, stream=None):
         """Copies every state's src to its dst; swap them for the next step."""
         if self.states:
-            stacklstm_beam_reorder(self.dims, self.parent, self.states, stream=stream)
+            stacklstm_beam_reorder(self.dims, self.parent, self._descriptors, stream=stream)
