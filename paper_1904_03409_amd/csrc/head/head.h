@@ -138,6 +138,24 @@ __device__ __forceinline__ float group_reduce(float v, Op op, float* red) {
   return v;
 }
 
+// Sum over P rows of N columns, 8 columns to a workgroup of 1024 threads: column blockIdx.x * 8 + threadIdx.x in the first 8. A
+// column's 128 threads take a row each in turn (768 rows of 400 columns: 3.0 us where 32 threads to a column took 4.4).
+__device__ __forceinline__ float column_sum(const float* part, int P, int N, float (&red)[16][8]) {
+  const int n = blockIdx.x * 8 + (threadIdx.x & 7);
+  float s = 0.f;
+  if (n < N) {
+#pragma unroll 4
+    for (int p = threadIdx.x >> 3; p < P; p += 128) s += part[(int64_t)p * N + n];
+  }
+  s = across<8>(s, op_sum());
+  if ((threadIdx.x & 63) < 8) red[threadIdx.x >> 6][threadIdx.x & 7] = s;
+  __syncthreads();
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v += red[w][threadIdx.x & 7];
+  return v;
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 // exp((x - m) k ln 2) as 2^(x k - mk) in one fused step. mk is m k rounded: every term of a row is off by the one factor
 // 2^off, which its sum and its gradient take out again.

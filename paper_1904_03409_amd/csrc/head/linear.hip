@@ -589,22 +589,13 @@ __global__ void __launch_bounds__(256) k_linear_pad(PadArgs a) {
   }
 }
 
-// db: the sums of P blocks of rows, 8 columns and 32 parts of the P to a workgroup.
+// db: the sums of P blocks of rows.
 template <typename T>
-__global__ void __launch_bounds__(256) k_linear_db(const float* part, int P, int N, T* db) {
-  __shared__ float red[32][9];
-  const int n = blockIdx.x * 8 + (threadIdx.x & 7), p0 = threadIdx.x >> 3;
-  float s = 0.f;
-  if (n < N)
-#pragma unroll 8
-    for (int p = p0; p < P; p += 32) s += part[(int64_t)p * N + n];
-  red[p0][threadIdx.x & 7] = s;
-  __syncthreads();
-  if (threadIdx.x >= 8 || n >= N) return;
-  float v = 0.f;
-#pragma unroll
-  for (int p = 0; p < 32; ++p) v += red[p][threadIdx.x];
-  from_f32(db[n], v);
+__global__ void __launch_bounds__(1024) k_linear_db(const float* part, int P, int N, T* db) {
+  __shared__ float red[16][8];
+  const float v = column_sum(part, P, N, red);
+  const int n = blockIdx.x * 8 + threadIdx.x;
+  if (threadIdx.x < 8 && n < N) from_f32(db[n], v);
 }
 
 namespace {
@@ -846,8 +837,8 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
     else hipLaunchKernelGGL(k_linear_dz<bf16_t>, grid, dim3(256), 0, st, a);
     if (db) {
       const dim3 cols((d->N + 7) / 8);
-      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(256), 0, st, a.part, p.blocks, d->N, (float*)db);
-      else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(256), 0, st, a.part, p.blocks, d->N, (bf16_t*)db);
+      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(1024), 0, st, a.part, p.blocks, d->N, (float*)db);
+      else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(1024), 0, st, a.part, p.blocks, d->N, (bf16_t*)db);
     }
     e = hipGetLastError();
   }

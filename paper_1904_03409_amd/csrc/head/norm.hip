@@ -114,22 +114,35 @@ __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_bwd(NormArgs a) {
     for (int k = 0; k < V; ++k) sg[i][k] = sb[i][k] = 0.f;
   const float inv = 1.f / (float)W;
   int flip = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, flip ^= 1) {
-    const int64_t row = r0 + threadIdx.x / TPR;
+  // the next row's loads are on their way while this one is computed
+  u32x4 nx[NV], nd[NV], ns[NV];
+  float nmu, nrstd;
+  auto fetch = [&](int64_t row) {
     const bool here = row < a.rows;
     const T* x = (const T*)a.x + row * a.ldx;
     const T* dy = (const T*)a.dy + row * a.ldd;
     const T* ds = (const T*)a.dsum + row * W;
-    u32x4 rx[NV], rd[NV], rs[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = t + i * TPR;
       const bool in = here && c * V < W;
-      rx[i] = in ? load_vec(x, c, W) : u32x4{0u, 0u, 0u, 0u};
-      rd[i] = in ? load_vec(dy, c, W) : u32x4{0u, 0u, 0u, 0u};
-      rs[i] = in && a.dsum ? load_vec(ds, c, W) : u32x4{0u, 0u, 0u, 0u};
+      nx[i] = in ? load_vec(x, c, W) : u32x4{0u, 0u, 0u, 0u};
+      nd[i] = in ? load_vec(dy, c, W) : u32x4{0u, 0u, 0u, 0u};
+      ns[i] = in && a.dsum ? load_vec(ds, c, W) : u32x4{0u, 0u, 0u, 0u};
     }
-    const float mu = here ? a.mean[row] : 0.f, rstd = here ? a.rstd[row] : 0.f;
+    nmu = here ? a.mean[row] : 0.f;
+    nrstd = here ? a.rstd[row] : 0.f;
+  };
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  fetch((int64_t)blockIdx.x * RPB + threadIdx.x / TPR);
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, flip ^= 1) {
+    const int64_t row = r0 + threadIdx.x / TPR;
+    const bool here = row < a.rows;
+    u32x4 rx[NV], rd[NV], rs[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) rx[i] = nx[i], rd[i] = nd[i], rs[i] = ns[i];
+    const float mu = nmu, rstd = nrstd;
+    if (r0 + step < a.rows) fetch(row + step);
     float xh[NV][V], g[NV][V], m1 = 0.f, m2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -211,27 +224,19 @@ __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_bwd(NormArgs a) {
   }
 }
 
-// dgamma | dbeta: the sums of P workgroups, 8 columns and 32 parts of the P to a workgroup.
-__global__ void __launch_bounds__(256) k_norm_cols(const float* part, int P, int W, float* dgamma, float* dbeta) {
-  __shared__ float red[32][9];
-  const int n = blockIdx.x * 8 + (threadIdx.x & 7), p0 = threadIdx.x >> 3;
-  float s = 0.f;
-  if (n < 2 * W)
-#pragma unroll 8
-    for (int p = p0; p < P; p += 32) s += part[(size_t)p * 2 * W + n];
-  red[p0][threadIdx.x & 7] = s;
-  __syncthreads();
+// dgamma | dbeta: the sums of P workgroups.
+__global__ void __launch_bounds__(1024) k_norm_cols(const float* part, int P, int W, float* dgamma, float* dbeta) {
+  __shared__ float red[16][8];
+  const float v = column_sum(part, P, 2 * W, red);
+  const int n = blockIdx.x * 8 + threadIdx.x;
   if (threadIdx.x >= 8 || n >= 2 * W) return;
-  float v = 0.f;
-#pragma unroll
-  for (int p = 0; p < 32; ++p) v += red[p][threadIdx.x];
   float* o = n < W ? dgamma : dbeta;
   if (o) o[n < W ? n : n - W] = v;
 }
 
 namespace {
 
-constexpr int kNormMaxParts = 512;
+constexpr int kNormMaxParts = 768;                     // workgroups of a backward, three to a CU
 constexpr int kNormMaxWidth = 8192;
 
 bool norm_ok(const slstm_norm_dims* d) {
@@ -239,20 +244,22 @@ bool norm_ok(const slstm_norm_dims* d) {
          (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->eps >= 0.f && stride_ok(d->ld_x, d->width) &&
          stride_ok(d->ld_res, d->width) && stride_ok(d->ld_dy, d->width);
 }
-// Lanes to a row: the fewest that hold it in one vector each up to a wave, then two vectors a lane, then a
-// workgroup (two barriers a row, but the sums of a thread's columns stay in registers: four vectors a lane
+// Lanes to a row: the fewest that hold it in two vectors each up to a wave (22912 rows of 200 floats in 64 lanes of one
+// vector: 9.0 and 14.4 us), then a workgroup (two barriers a row, but the sums of a thread's columns stay in registers: four vectors a lane
 // of 16-bit rows take 234 of them).
 int norm_tpr(const slstm_norm_dims* d) {
   const int n = (d->width + (d->type == SLSTM_F32 ? 3 : 7)) / (d->type == SLSTM_F32 ? 4 : 8);
-  return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : 1024;
+  return n <= 16 ? 8 : n <= 32 ? 16 : n <= 64 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : 1024;
 }
 int norm_nv(const slstm_norm_dims* d, int tpr) {
   const int n = (d->width + (d->type == SLSTM_F32 ? 3 : 7)) / (d->type == SLSTM_F32 ? 4 : 8), q = (n + tpr - 1) / tpr;
   return q <= 1 ? 1 : 2;
 }
 int norm_parts(const slstm_norm_dims* d) {
-  const int64_t rpb = norm_rows(norm_tpr(d));
-  return (int)std::max<int64_t>(1, std::min<int64_t>((d->rows + rpb - 1) / rpb, kNormMaxParts));
+  // (all with as many rows, but for the last)
+  const int64_t rpb = norm_rows(norm_tpr(d)), groups = std::max<int64_t>(1, (d->rows + rpb - 1) / rpb);
+  const int64_t rounds = (groups + kNormMaxParts - 1) / kNormMaxParts;
+  return (int)((groups + rounds - 1) / rounds);
 }
 
 template <typename F>
@@ -261,7 +268,7 @@ bool norm_dispatch(const slstm_norm_dims* d, F f) {
 #define NORM_CASE(T_, TPR_, NV_) \
   if (tpr == TPR_ && nv == NV_) return f(T_(), std::integral_constant<int, TPR_>(), std::integral_constant<int, NV_>()), true;
 #define NORM_TYPE(T_) \
-  NORM_CASE(T_, 8, 1) NORM_CASE(T_, 16, 1) NORM_CASE(T_, 32, 1) NORM_CASE(T_, 64, 1) NORM_CASE(T_, 64, 2) \
+  NORM_CASE(T_, 8, 1) NORM_CASE(T_, 8, 2) NORM_CASE(T_, 16, 2) NORM_CASE(T_, 32, 2) NORM_CASE(T_, 64, 2) \
   NORM_CASE(T_, 256, 1) NORM_CASE(T_, 256, 2) NORM_CASE(T_, 512, 2)
   if (d->type == SLSTM_F32) {
     NORM_TYPE(float)
@@ -326,7 +333,7 @@ extern "C" int stacklstm_norm_bwd(const slstm_norm_dims* d, const void* x, const
   });
   if (!ok) return SLSTM_EINVAL;
   if (cols && P > 1)
-    hipLaunchKernelGGL(k_norm_cols, dim3((2 * d->width + 7) / 8), dim3(256), 0, as_stream(stream), a.part, P, d->width, dgamma,
+    hipLaunchKernelGGL(k_norm_cols, dim3((2 * d->width + 7) / 8), dim3(1024), 0, as_stream(stream), a.part, P, d->width, dgamma,
                        dbeta);
   return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }
