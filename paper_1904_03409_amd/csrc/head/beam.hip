@@ -162,38 +162,41 @@ __device__ __forceinline__ void beam_out(const BeamArgs& a, int b, int n, u64 ke
   a.done_next[o] = done;
 }
 
-// Vector c of a row of logits, -inf where the row ends and where a token is not allowed.
-template <typename T>
-__device__ __forceinline__ u32x4 load_logits(const BeamArgs& a, int64_t row, int c) {
-  constexpr int V = vec<T>::N;
-  constexpr uint32_t low = kPadLow<T>;
-  u32x4 r = load_vec((const T*)a.x + row * a.ldx, c, a.V, low);
-  if (a.legal) {
-    const uint8_t* l = a.legal + row * a.V + (int64_t)c * V;
-    bool ok[V];
-    if ((c + 1) * V <= a.V) {
-      typedef uint32_t u32_any __attribute__((aligned(1)));
+// load_row of a beam's logits, -inf where a token is not allowed; end: row_end likewise (where `last`: the row's last chunk).
+template <int STEP, typename T, int NV>
+__device__ __forceinline__ void load_logits(const BeamArgs& a, int64_t row, int c0, u32x4 (&raw)[NV], bool last, float& end) {
+  constexpr int V = vec<T>::N, Q = V / 4;
+  constexpr uint32_t low = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  const T* x = (const T*)a.x + row * a.ldx;
+  load_row<STEP>(raw, x, c0, a.V);
+  const int t = threadIdx.x;
+  end = row_end(x, t, last ? a.V : 0);
+  if (!a.legal) return;
+  typedef uint32_t u32_any __attribute__((aligned(1)));
+  const uint8_t* l = a.legal + row * a.V;
+  if (last && has_end<T>(t, a.V) && !l[end_place<T>(t, a.V)]) end = -INFINITY;
+  uint32_t w[NV][Q];                                   // a byte to an element
 #pragma unroll
-      for (int q = 0; q < V / 4; ++q) {
-        const uint32_t w = *(const u32_any*)(l + 4 * q);
+  for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) ok[4 * q + k] = (w >> (8 * k)) & 0xffu;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < V; ++k) ok[k] = c * V + k < a.V && l[k];
+    for (int q = 0; q < Q; ++q) {
+      w[i][q] = 0u;
+      if (c0 + i * STEP < a.V / V) w[i][q] = *(const u32_any*)(l + (c0 + i * STEP) * V + 4 * q);
     }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int k = 0; k < V; ++k) {
+      const bool ok = (w[i][k / 4] >> (8 * (k & 3))) & 0xffu;
       if constexpr (V == 4) {
-        r[k] = ok[k] ? r[k] : low;
+        raw[i][k] = ok ? raw[i][k] : low;
       } else {
         const uint32_t keep = k & 1 ? 0x0000ffffu : 0xffff0000u;
-        r[k / 2] = ok[k] ? r[k / 2] : (r[k / 2] & keep) | (low & ~keep);
+        raw[i][k / 2] = ok ? raw[i][k / 2] : (raw[i][k / 2] & keep) | (low & ~keep);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  return r;
 }
 
 // Whether a beam goes on with tokens; if not, its chunk's keys are written (a finished beam's one).
@@ -219,8 +222,12 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
   if (!beam_runs(a, row, ch, score)) return;
   u32x4 raw[NV];
   float most[NV], mine = -INFINITY;                    // largest of a vector, of all
-#pragma unroll
-  for (int i = 0; i < NV; ++i) raw[i] = load_logits<T>(a, row, c0 + i * NT);
+  // sum of 2^(x k - ref) of this thread, ref the largest x k so far: the exponentials run while later vectors arrive
+  // (1024 rows of 64001: 43.4 us with a pass for the maximum before)
+  float ref = -1e30f, sum = 0.f;
+  const bool tail = !JOIN || ch + 1 == a.chunks;
+  float end;
+  load_logits<NT, T>(a, row, c0, raw, tail, end);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float v[V];
@@ -229,10 +236,24 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
 #pragma unroll
     for (int k = 1; k < V; ++k) most[i] = fmaxf(most[i], v[k]);
     mine = fmaxf(mine, most[i]);
+    if constexpr (!JOIN) {
+      const float up = fmaxf(ref, most[i] * kLog2e);
+      sum *= __builtin_amdgcn_exp2f(ref - up);
+      ref = up;
+      opaque_vec(raw[i]);
+      vec<T>::unpack(raw[i], v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], kLog2e, -ref));
+    }
     __builtin_amdgcn_sched_barrier(0);                 // (one vector unpacked at a time, here and below)
   }
-  float m, sum = 0.f;
-  Expo ex;
+  mine = fmaxf(mine, end);
+  if constexpr (!JOIN) {
+    const float up = fmaxf(ref, end * kLog2e);
+    sum = sum * __builtin_amdgcn_exp2f(ref - up) + __builtin_amdgcn_exp2f(__builtin_fmaf(end, kLog2e, -up));
+    ref = up;
+  }
+  float m;
   if constexpr (JOIN) {
     const float* q = a.part + (size_t)row * a.chunks * 2;
     m = -INFINITY;
@@ -245,16 +266,23 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
     }
   } else {
     m = group_reduce<NT>(mine, op_max(), red[0]);
-    ex = Expo(m, kLog2e);
+  }
+  const Expo ex(m, kLog2e);
+  if constexpr (!JOIN) {
+    if (fabsf(m) < 1e29f) {
+      sum *= __builtin_amdgcn_exp2f(ref - ex.mk);
+    } else {                                           // out of ref's range (lowest values, infinities): once more, from memory
+      sum = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < NV; ++i) {
+        float v[V], e;
+        u32x4 w[1];
+        load_logits<NT, T>(a, row, c0 + i * NT, w, false, e);
+        vec<T>::unpack(w[0], v);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float v[V];
-      vec<T>::unpack(raw[i], v);
-#pragma unroll
-      for (int k = 0; k < V; ++k) sum += ex(v[k]);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int k = 0; k < V; ++k) sum += ex(v[k]);
+      }
+      sum += ex(end);
     }
   }
   sum = group_reduce<NT>(sum, op_sum(), red[1]);
@@ -278,13 +306,19 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
       }
     }
   }
+  if (end >= lo) {
+    const float total = (end - lse) + score;
+    if (total >= tb && total > -INFINITY) topk_put(make_key(total, end_place<T>(t, a.V)), s);
+  }
   topk_rank<NT>(a.K, s, [&](auto f) {
+    f(make_key((end - lse) + score, end_place<T>(t, a.V)));
 #pragma unroll 1
     for (int i = 0; i < NV; ++i) {
       // (read again: a loop over registers would take them all at once)
-      const u32x4 w = load_logits<T>(a, row, c0 + i * NT);
-      float v[V];
-      vec<T>::unpack(w, v);
+      u32x4 w[1];
+      float v[V], e;
+      load_logits<NT, T>(a, row, c0 + i * NT, w, false, e);
+      vec<T>::unpack(w[0], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) f(make_key((v[k] - lse) + score, (c0 + i * NT) * V + k));
     }
@@ -303,8 +337,9 @@ __global__ void __launch_bounds__(256) k_beam_part(BeamArgs a) {
   if ((a.done && a.done[row]) || !(a.score[row] > -INFINITY)) return;
   u32x4 raw[kPartVecs];
   float m = -INFINITY, sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < kPartVecs; ++i) raw[i] = load_logits<T>(a, row, c0 + i * 256);
+  float end;
+  load_logits<256, T>(a, row, c0, raw, ch + 1 == a.chunks, end);
+  m = end;
 #pragma unroll
   for (int i = 0; i < kPartVecs; ++i) {
     float v[V];
@@ -321,6 +356,7 @@ __global__ void __launch_bounds__(256) k_beam_part(BeamArgs a) {
 #pragma unroll
     for (int k = 0; k < V; ++k) sum += ex(v[k]);
   }
+  sum += ex(end);
   sum = group_reduce<256>(sum, op_sum(), red[1]) * __builtin_amdgcn_exp2f(-ex.off);
   if (t == 0) {
     a.part[(size_t)blockIdx.x * 2] = m;

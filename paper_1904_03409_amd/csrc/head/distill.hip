@@ -163,13 +163,10 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
   int* idx = lds + sub * 3 * n;
   float *p = (float*)(idx + n), *u = p + n;
   const T* x = (const T*)a.x + row * a.ldx;
-  constexpr uint32_t low = kPadLow<T>;                 // past the row's end: no share in maximum and sums
   u32x4 raw[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = t + i * TPR;
-    raw[i] = here ? load_vec(x, c, a.V, low) : u32x4{low, low, low, low};
-  }
+  const int W = here ? a.V : 0;
+  load_row<TPR>(raw, x, t, W);
+  const float end = row_end(x, t, W);
   const RowTargets r = row_targets<TPR>(a, row, here, t, idx, p, red[0]);
   for (int j = t; j <= a.K; j += TPR) {
     const int i = j < a.K ? idx[j] : r.label;
@@ -181,7 +178,7 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
     logst = here ? a.stats_in[row * 3 + 1] : 0.f;
     logs1 = here ? a.stats_in[row * 3 + 2] : 0.f;
   } else {
-    m = -INFINITY;
+    m = end;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       float v[V];
@@ -210,6 +207,10 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
         }
         __builtin_amdgcn_sched_barrier(0);             // (one vector unpacked at a time)
       }
+      const float e = et(end);
+      st += e;
+      if (MODE == SQUARE) s1 = __builtin_fmaf(e, e, s1);
+      if (MODE == BOTH) s1 += e1(end);
     };
     const int mode = expo_mode(a.tau, second);
     if (mode == ONE) sums(std::integral_constant<int, ONE>());
@@ -242,21 +243,15 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
   if (here) g = row_grad(a, r, row, m, logst, logs1);
 #pragma unroll
   for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
-  auto put = [&](auto f) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = t + i * TPR;
-      if (c * V < a.V) {
-        float v[V];
+  if (here)
+    each_grad(g, [&](auto f) {
+      store_row<TPR, T, NV>(dx, t, a.V, [&](int i, float (&v)[V]) {
         vec<T>::unpack(raw[i], v);
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = f(v[k]);
-        store_vec(dx, c, a.V, v);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  if (here) each_grad(g, put);
+      });
+      if (has_end<T>(t, a.V)) from_f32(dx[end_place<T>(t, a.V)], f(end));
+    });
   // the elements that the teacher's entries and the label change, behind the stores above
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if constexpr (TPR > 64) __syncthreads();
@@ -276,18 +271,14 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a) {
   const int64_t row = blockIdx.x / a.chunks;
   const int ch = blockIdx.x % a.chunks, t = threadIdx.x, lo = ch * kChunkVecs * 256 * V;
   const T* x = (const T*)a.x + row * a.ldx;
-  constexpr uint32_t low = kPadLow<T>;
   u32x4 raw[kChunkVecs];
-#pragma unroll
-  for (int i = 0; i < kChunkVecs; ++i) {
-    const int c = (ch * kChunkVecs + i) * 256 + t;
-    raw[i] = load_vec(x, c, a.V, low);
-  }
+  load_row<256>(raw, x, ch * kChunkVecs * 256 + t, a.V);
+  const float end = row_end(x, t, ch + 1 == a.chunks ? a.V : 0);
   for (int j = t; j <= a.K; j += 256) {
     const int i = j < a.K ? a.index[row * a.K + j] : a.label ? a.label[row] : -1;
     if (i >= lo && i < a.V && i < lo + kChunkVecs * 256 * V) a.ent[row * (a.K + 1) + j] = to_f32(x[i]);
   }
-  float m = -INFINITY;
+  float m = end;
 #pragma unroll
   for (int i = 0; i < kChunkVecs; ++i) {
     float v[V];
@@ -310,6 +301,8 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a) {
       if (a.tau != 1.f) s1 += e1(v[k]);
     }
   }
+  st += et(end);
+  if (a.tau != 1.f) s1 += e1(end);
   st = group_reduce<256>(st, op_sum(), red[1]) * __builtin_amdgcn_exp2f(-et.off);
   s1 = a.tau == 1.f ? st : group_reduce<256>(s1, op_sum(), red[2]) * __builtin_amdgcn_exp2f(-e1.off);
   if (t == 0) {
@@ -334,14 +327,11 @@ __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
   const int64_t row = blockIdx.x / per;
   const int ch = blockIdx.x % per, t = threadIdx.x, lo = ch * kChunkVecs * 256 * V, hi = lo + kChunkVecs * 256 * V;
   const T* x = (const T*)a.x + row * a.ldx;
-  constexpr uint32_t low = kPadLow<T>;
   u32x4 raw[kChunkVecs];
+  float end = 0.f;
   if (a.dx) {
-#pragma unroll
-    for (int i = 0; i < kChunkVecs; ++i) {
-      const int c = (ch * kChunkVecs + i) * 256 + t;
-      raw[i] = load_vec(x, c, a.V, low);
-    }
+    load_row<256>(raw, x, ch * kChunkVecs * 256 + t, a.V);
+    end = row_end(x, t, ch + 1 == a.chunks ? a.V : 0);
   }
   const RowTargets r = row_targets<256>(a, row, true, t, idx, p, red[0]);
   float m, logst, logs1;
@@ -389,16 +379,12 @@ __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
   const RowGrad g = row_grad(a, r, row, m, logst, logs1);
   __syncthreads();                                     // (every element of the chunk that is fetched by place has been)
   each_grad(g, [&](auto f) {
-#pragma unroll
-    for (int i = 0; i < kChunkVecs; ++i) {
-      const int c = (ch * kChunkVecs + i) * 256 + t;
-      if (c * V >= a.V) continue;
-      float v[V];
+    store_row<256, T, kChunkVecs>(dx, ch * kChunkVecs * 256 + t, a.V, [&](int i, float (&v)[V]) {
       vec<T>::unpack(raw[i], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = f(v[k]);
-      store_vec(dx, c, a.V, v);
-    }
+    });
+    if (ch + 1 == a.chunks && has_end<T>(t, a.V)) from_f32(dx[end_place<T>(t, a.V)], f(end));
   });
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();

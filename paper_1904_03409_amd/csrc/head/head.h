@@ -46,14 +46,12 @@ __device__ __forceinline__ float to_f32(bf16_t v) { return bf16_bits_to_f32(v); 
 __device__ __forceinline__ void from_f32(float& d, float v) { d = v; }
 __device__ __forceinline__ void from_f32(bf16_t& d, float v) { d = f32_to_bf16_bits(v); }
 
-// Vector i of a row of W elements, `pad` (the bits of 32 bits' worth of elements) past the row's end.
-constexpr uint32_t kPadZero = 0u;
-template <typename T> constexpr uint32_t kPadLow = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // -inf
+// Vector i of a row of W elements, zeros past the row's end.
 template <typename T>
-__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W, uint32_t pad = kPadZero) {
+__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W) {
   constexpr int V = vec<T>::N;
   if ((i + 1) * V <= W) return *(const u32x4_any*)(row + i * V);
-  u32x4 r = {pad, pad, pad, pad};
+  u32x4 r = {0u, 0u, 0u, 0u};
   if constexpr (V == 4) {
 #pragma unroll
     for (int k = 0; k < 3; ++k)
@@ -61,10 +59,7 @@ __device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W, uint32_t p
   } else {
 #pragma unroll
     for (int k = 0; k < 7; ++k)
-      if (i * V + k < W) {
-        const uint32_t e = row[i * V + k];
-        r[k / 2] = k & 1 ? (r[k / 2] & 0xffffu) | e << 16 : (r[k / 2] & 0xffff0000u) | e;
-      }
+      if (i * V + k < W) r[k / 2] |= (uint32_t)row[i * V + k] << (16 * (k & 1));
   }
   return r;
 }
@@ -78,6 +73,41 @@ __device__ __forceinline__ void store_vec(T* row, int i, int W, const float (&v)
 #pragma unroll
   for (int k = 0; k < V - 1; ++k)
     if (i * V + k < W) from_f32(row[i * V + k], v[k]);
+}
+
+// The whole vectors c0, c0 + STEP, .. of a row, -inf behind them (no share in maximum and sums), and with row_end the element
+// behind the last whole one that lane t takes of the fewer than a vector that are left: -inf for most. (Partial vectors
+// put together element by element cost a branch to each vector and the registers of its other outcome.)
+template <int STEP, typename T, int NV>
+__device__ __forceinline__ void load_row(u32x4 (&raw)[NV], const T* row, int c0, int W) {
+  constexpr uint32_t low = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    raw[i] = u32x4{low, low, low, low};
+    if (c0 + i * STEP < W / vec<T>::N) raw[i] = *(const u32x4_any*)(row + (c0 + i * STEP) * vec<T>::N);
+  }
+}
+template <typename T>
+__device__ __forceinline__ bool has_end(int t, int W) { return t < W % vec<T>::N; }
+template <typename T>
+__device__ __forceinline__ int end_place(int t, int W) { return W / vec<T>::N * vec<T>::N + t; }
+template <typename T>
+__device__ __forceinline__ float row_end(const T* row, int t, int W) {
+  return has_end<T>(t, W) ? to_f32(row[end_place<T>(t, W)]) : -INFINITY;
+}
+// f(i, v): the values of whole vector c0 + i STEP, written to the row.
+template <int STEP, typename T, int NV, typename F>
+__device__ __forceinline__ void store_row(T* row, int c0, int W, F f) {
+  constexpr int V = vec<T>::N;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (c0 + i * STEP < W / V) {
+      float v[V];
+      f(i, v);
+      *(u32x4_any*)(row + (c0 + i * STEP) * V) = vec<T>::pack(v);
+    }
+    __builtin_amdgcn_sched_barrier(0);                 // (one vector unpacked at a time)
+  }
 }
 
 // Packed values that are unpacked again behind this point, instead of being kept unpacked in registers.
