@@ -70,42 +70,36 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 }
 
 struct TopkLds {
-  u64 list[kList], out[kMaxBeams], red[16];
-  uint32_t grp[64], thr;
+  u64 list[kList], red[16];
+  uint32_t grp[64];
   int count;
 };
 
-// The K-th largest of the 64 groups' largest values (in order bits; 0: the group has none), in every thread.
-// mine: this thread's. All NT threads call.
+// The largest values of 64 groups of NT threads' (mine: this thread's, in order bits; 0: none), to LDS. A barrier follows.
 template <int NT>
-__device__ __forceinline__ uint32_t topk_bound(uint32_t mine, int K, TopkLds& s) {
+__device__ __forceinline__ void topk_groups(uint32_t mine, TopkLds& s) {
   constexpr int G = NT / 64;                           // threads of a group
   mine = lanes_max<G>(mine);
   const int t = threadIdx.x;
   if (t % G == 0) s.grp[t / G] = mine;
   if (t == 0) s.count = 0;
-  if (t < kMaxBeams) s.out[t] = 0;
-  __syncthreads();
-  if (t < 64) {
-    // the largest value that K groups reach
-    const uint32_t v = s.grp[t];
-    int reach = 0;
+}
+// The largest value that K of the groups reach (0: they have fewer), by every wave for itself.
+__device__ __forceinline__ uint32_t topk_bound(int K, const TopkLds& s) {
+  const uint32_t v = s.grp[threadIdx.x & 63];
+  int reach = 0;
 #pragma unroll
-    for (int j = 0; j < 64; ++j) reach += (uint32_t)__builtin_amdgcn_readlane((int)v, j) >= v;
-    const uint32_t b = lanes_max<64>(reach >= K ? v : 0u);
-    if (t == 0) s.thr = b;
-  }
-  __syncthreads();
-  return s.thr;
+  for (int j = 0; j < 64; ++j) reach += (uint32_t)__builtin_amdgcn_readlane((int)v, j) >= v;
+  return lanes_max<64>(reach >= K ? v : 0u);
 }
 __device__ __forceinline__ void topk_put(u64 key, TopkLds& s) {
   const int i = atomicAdd(&s.count, 1);
   if (i < kList) s.list[i] = key;
 }
-// The K best of the listed keys (all different) to s.out, falling, zeros behind the last. each(f): calls f with every
-// key of this thread, listed or not, for lists that did not fit.
-template <int NT, typename Each>
-__device__ __forceinline__ void topk_rank(int K, TopkLds& s, Each each) {
+// emit(n, key) for the K best of the listed keys (all different), n their rank, and key 0 for the places past them, each by some
+// thread. each(f): calls f with every key of this thread, listed or not, for lists that did not fit.
+template <int NT, typename Each, typename Emit>
+__device__ __forceinline__ void topk_rank(int K, TopkLds& s, Each each, Emit emit) {
   __syncthreads();
   const int n = s.count, t = threadIdx.x;
   if (n <= kList) {
@@ -114,9 +108,9 @@ __device__ __forceinline__ void topk_rank(int K, TopkLds& s, Each each) {
       int above = 0;
 #pragma unroll 8
       for (int j = 0; j < n; ++j) above += s.list[j] > k;
-      if (above < K) s.out[above] = k;
+      if (above < K) emit(above, k);
     }
-    __syncthreads();
+    for (int i = n + t; i < K; i += NT) emit(i, (u64)0);
     return;
   }
   u64 last = ~(u64)0;
@@ -133,10 +127,9 @@ __device__ __forceinline__ void topk_rank(int K, TopkLds& s, Each each) {
     if ((t & 63) == 0) s.red[t >> 6] = best;
     __syncthreads();
     for (int w = 0; w < NT / 64; ++w) best = s.red[w] > best ? s.red[w] : best;
-    if (t == 0) s.out[r] = best;
     __syncthreads();
-    last = best;
-    if (!best) break;                                  // (every thread has the same)
+    if (t == 0) emit(r, best);
+    last = best;                                       // (every thread has the same; 0: none is left)
   }
 }
 
@@ -215,7 +208,7 @@ template <typename T, int NT, int NV, bool JOIN>
 __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
   constexpr int V = vec<T>::N;
   __shared__ TopkLds s;
-  __shared__ float red[2][16];
+  __shared__ float red[3][16];
   const int64_t row = JOIN ? blockIdx.x / a.chunks : blockIdx.x;
   const int ch = JOIN ? blockIdx.x % a.chunks : 0, t = threadIdx.x, c0 = ch * NT * NV + t;
   const float score = a.score[row];
@@ -253,41 +246,51 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
     sum = sum * __builtin_amdgcn_exp2f(ref - up) + __builtin_amdgcn_exp2f(__builtin_fmaf(end, kLog2e, -up));
     ref = up;
   }
-  float m;
+  topk_groups<NT>(mine > -INFINITY ? order_bits(mine) : 0u, s);
+  float m, lse;
   if constexpr (JOIN) {
+    // (every wave for itself: 64 chunks at a time)
     const float* q = a.part + (size_t)row * a.chunks * 2;
     m = -INFINITY;
-    for (int i = t; i < a.chunks; i += NT) m = fmaxf(m, q[2 * i]);
-    m = group_reduce<NT>(m, op_max(), red[0]);
-    for (int i = t; i < a.chunks; i += NT) {
+    for (int i = t & 63; i < a.chunks; i += 64) m = fmaxf(m, q[2 * i]);
+    m = lanes<64>(m, op_max());
+    for (int i = t & 63; i < a.chunks; i += 64) {
       // (a chunk of -inf alone has the sum 0 and no share)
       const float mi = q[2 * i], si = q[2 * i + 1];
       sum += mi == -INFINITY ? si : si * __builtin_amdgcn_exp2f((mi - m) * kLog2e);
     }
+    lse = m + logf(lanes<64>(sum, op_sum()));
+    __syncthreads();
   } else {
-    m = group_reduce<NT>(mine, op_max(), red[0]);
-  }
-  const Expo ex(m, kLog2e);
-  if constexpr (!JOIN) {
-    if (fabsf(m) < 1e29f) {
-      sum *= __builtin_amdgcn_exp2f(ref - ex.mk);
-    } else {                                           // out of ref's range (lowest values, infinities): once more, from memory
+    // maxima, reference and sums of the waves with one barrier
+    constexpr int W = NT / 64;
+    const int w = t >> 6, l = t & (W - 1);
+    const float wref = lanes<64>(ref, op_max());
+    const float wmax = lanes<64>(mine, op_max()), wsum = lanes<64>(sum * __builtin_amdgcn_exp2f(ref - wref), op_sum());
+    if ((t & 63) == 0) red[0][w] = wmax, red[1][w] = wref, red[2][w] = wsum;
+    __syncthreads();
+    m = lanes<W>(red[0][l], op_max());
+    const float top = lanes<W>(red[1][l], op_max());
+    sum = lanes<W>(red[2][l] * __builtin_amdgcn_exp2f(red[1][l] - top), op_sum());
+    const Expo ex(m, kLog2e);                          // (its mk is top)
+    if (!(fabsf(m) < 1e29f)) {                         // out of ref's range (lowest values, infinities): once more, from memory
       sum = 0.f;
 #pragma unroll 1
       for (int i = 0; i < NV; ++i) {
         float v[V], e;
-        u32x4 w[1];
-        load_logits<NT, T>(a, row, c0 + i * NT, w, false, e);
-        vec<T>::unpack(w[0], v);
+        u32x4 u[1];
+        load_logits<NT, T>(a, row, c0 + i * NT, u, false, e);
+        vec<T>::unpack(u[0], v);
 #pragma unroll
         for (int k = 0; k < V; ++k) sum += ex(v[k]);
       }
       sum += ex(end);
+      __syncthreads();
+      sum = group_reduce<NT>(sum, op_sum(), red[0]);
     }
+    lse = m + ex.log_sum(sum);
   }
-  sum = group_reduce<NT>(sum, op_sum(), red[1]);
-  const float lse = m + (JOIN ? logf(sum) : ex.log_sum(sum));
-  const uint32_t bound = topk_bound<NT>(mine > -INFINITY ? order_bits(mine) : 0u, a.K, s);
+  const uint32_t bound = topk_bound(a.K, s);
   // Totals rise with x, but two different x may have one total, where the lower place wins: elements a few
   // roundings below the bound are looked at as well.
   const float xb = bound ? from_order(bound) : -INFINITY;
@@ -322,9 +325,7 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
 #pragma unroll
       for (int k = 0; k < V; ++k) f(make_key((v[k] - lse) + score, (c0 + i * NT) * V + k));
     }
-  });
-  u64* out = a.cand + ((size_t)row * a.chunks + ch) * a.K;
-  for (int j = t; j < a.K; j += NT) out[j] = s.out[j];
+  }, [&](int n, u64 key) { a.cand[((size_t)row * a.chunks + ch) * a.K + n] = key; });
 }
 
 // A chunk's maximum and sum.
@@ -377,15 +378,16 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamArgs a) {
   };
   uint32_t mine = 0;
   for (int64_t i = t; i < n; i += 256) mine = max(mine, (uint32_t)(cand[i] >> 32));
-  const uint32_t bound = topk_bound<256>(mine, a.K, s);
+  topk_groups<256>(mine, s);
+  __syncthreads();
+  const uint32_t bound = topk_bound(a.K, s);
   for (int64_t i = t; i < n; i += 256) {
     const u64 k = get(i);
     if (k && (uint32_t)(k >> 32) >= bound) topk_put(k, s);
   }
   topk_rank<256>(a.K, s, [&](auto f) {
     for (int64_t i = t; i < n; i += 256) f(get(i));
-  });
-  if (t < a.K) beam_out(a, b, t, s.out[t]);
+  }, [&](int place, u64 key) { beam_out(a, b, place, key); });
 }
 
 // A whole search of at most kSmall continuations: a wave to a row for the softmax sums, totals in LDS.
@@ -425,7 +427,9 @@ __global__ void __launch_bounds__(512) k_beam_small(BeamArgs a) {
     const float v = tot[i];
     if (v > -INFINITY) mine = max(mine, order_bits(v));
   }
-  const uint32_t bound = topk_bound<512>(mine, a.K, s);
+  topk_groups<512>(mine, s);
+  __syncthreads();
+  const uint32_t bound = topk_bound(a.K, s);
 #pragma unroll 4
   for (int i = t; i < n; i += 512) {
     const u64 k = make_key(tot[i], i);
@@ -433,8 +437,7 @@ __global__ void __launch_bounds__(512) k_beam_small(BeamArgs a) {
   }
   topk_rank<512>(a.K, s, [&](auto f) {
     for (int i = t; i < n; i += 512) f(make_key(tot[i], i));
-  });
-  if (t < a.K) beam_out(a, b, t, s.out[t]);
+  }, [&](int place, u64 key) { beam_out(a, b, place, key); });
 }
 
 namespace {
