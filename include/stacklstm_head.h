@@ -6,10 +6,11 @@
  *
  * Conventions for every entry point:
  *  - All array arguments are DEVICE pointers, owned by the caller; the library keeps none of them
- *    after the call returns and holds no state between calls. Matrices are row-major. A matrix with
- *    an ld_ field in the dims may have that many elements from row to row (0: dense); the others are
+ *    after the call returns and holds no state between calls, but for kernels' launch attributes,
+ *    set once per device. Matrices are row-major. A matrix with an ld_ field in the dims may have
+ *    that many elements from row to row (0: dense); the others are
  *    dense. Arrays need only their element's alignment; 16-byte aligned ones with strides of whole
- *    16 bytes get the fastest paths.
+ *    16 bytes get the fastest paths. A work space is 16-byte aligned.
  *  - Calls are asynchronous on `stream` (a hipStream_t; NULL = default stream) and never synchronise
  *    the host. They allocate nothing and may be captured into a graph.
  *  - Outputs are overwritten, not accumulated, and must not overlap inputs (exceptions are named).

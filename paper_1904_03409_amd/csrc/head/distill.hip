@@ -84,7 +84,7 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const RowTargets
   for (int j = t; j < a.K; j += N)
     if (p[j] > 0.f || p[j] != p[j]) kl += p[j] * (logf(p[j]) - ((u[j] - m) * it - logst));
   kl = group_reduce<N>(kl, op_sum(), red);
-  float loss = r.some ? a.alpha * a.tau * a.tau * kl : 0.f;
+  float loss = r.some && a.alpha > 0.f ? a.alpha * a.tau * a.tau * kl : 0.f;
   if (r.label >= 0 && a.alpha < 1.f) loss += (1.f - a.alpha) * (logs1 - (u[a.K] - m));
   return loss;
 }
@@ -243,6 +243,8 @@ __global__ void __launch_bounds__(distill_threads(TPR)) k_distill_rows(DistillAr
   if (here) g = row_grad(a, r, row, m, logst, logs1);
 #pragma unroll
   for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
+  // (dx may be x: every logit that is fetched by its place has been)
+  if constexpr (TPR > 64) __syncthreads();
   if (here)
     each_grad(g, [&](auto f) {
       store_row<TPR, T, NV>(dx, t, a.V, [&](int i, float (&v)[V]) {
@@ -446,7 +448,7 @@ int distill_run(const slstm_distill_dims* d, DistillArgs a, void* workspace, siz
   } else {
     const dim3 all((unsigned)(d->rows * a.chunks));
     if (!a.stats_in) {
-      if (!workspace) return SLSTM_EINVAL;
+      if (!workspace || ((uintptr_t)workspace & 3u)) return SLSTM_EINVAL;
       if (ws_bytes < stacklstm_distill_workspace_bytes(d)) return SLSTM_EWORKSPACE;
       a.part = (float*)workspace;
       a.ent = (float*)((char*)workspace + distill_part_bytes(d));

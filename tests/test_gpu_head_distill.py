@@ -66,7 +66,12 @@ def test_loss_and_gradient(R, V, K, dtype):
     r2 = hd.DistillRun.of(r.logits, r.index, r.value, r.label, r.grad, float(tau), float(alpha))
     r2.dlogits = r2.logits = r.logits.clone()
     r2.step()
-    assert torch.equal(r2.dlogits, step) and torch.equal(r2.loss, r2.loss)
+    assert torch.equal(r2.dlogits, step)
+    r3 = hd.DistillRun.of(r.logits, r.index, r.value, r.label, r.grad, float(tau), float(alpha))
+    r3.stats = r.stats
+    r3.dlogits = r3.logits = r.logits.clone()
+    r3.backward()
+    assert torch.equal(r3.dlogits, r.dlogits)
 
 
 @pytest.mark.parametrize("V", [90, 3000, 40000])
@@ -101,6 +106,9 @@ def test_masked_logits_and_rows(V):
     close(got[:6], loss[:6], "f32", "loss")
     close(gd[:6], d[:6], "f32", "dlogits")
     assert np.isnan(gd[6]).all() and np.isnan(gd[7]).all()
+    # without a weight the teacher's term is nothing, also where it would be infinite
+    r0 = hd.DistillRun.of(r.logits, r.index, r.value, r.label, r.grad, 2.0, 0.0)
+    assert np.isfinite(get(r0.step())[2])
     # the gradient of a row whose grad is 0 is 0, whatever it holds
     r.grad.zero_()
     r.step()
