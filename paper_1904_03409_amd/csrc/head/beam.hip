@@ -503,7 +503,8 @@ bool beam_ok(const slstm_beam_dims* d) {
          (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->eos >= -1 && stride_ok(d->ld_logits, d->V) &&
          (int64_t)d->B * d->K * beam_chunks(d) <= 0x7fffffff;
 }
-bool beam_small(const slstm_beam_dims* d) { return (int64_t)d->K * d->V <= kSmall; }
+// (a wave goes through its row 64 tokens at a time: one of 7360 took 20 us)
+bool beam_small(const slstm_beam_dims* d) { return (int64_t)d->K * d->V <= kSmall && d->V <= 2048; }
 // As the rows of a loss: 8192 vectors in registers; rows of four chunks or more are cut where there is not one of
 // them for every compute unit.
 bool beam_cut(const slstm_beam_dims* d) {

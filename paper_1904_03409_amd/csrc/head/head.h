@@ -46,11 +46,25 @@ __device__ __forceinline__ float to_f32(bf16_t v) { return bf16_bits_to_f32(v); 
 __device__ __forceinline__ void from_f32(float& d, float v) { d = v; }
 __device__ __forceinline__ void from_f32(bf16_t& d, float v) { d = f32_to_bf16_bits(v); }
 
-// Vector i of a row of W elements, zeros past the row's end.
+// v with its first s elements taken away, zeros behind the others.
 template <typename T>
-__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W) {
+__device__ __forceinline__ u32x4 shift_vec(u32x4 v, int s) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 w = {__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16),
+                     __builtin_amdgcn_alignbit(v[3], v[2], 16), v[3] >> 16};
+    v = s & 1 ? w : v;
+    s >>= 1;
+  }
+  v = s & 1 ? u32x4{v[1], v[2], v[3], 0u} : v;
+  v = s & 2 ? u32x4{v[2], v[3], 0u, 0u} : v;
+  return s >= 4 ? u32x4{0u, 0u, 0u, 0u} : v;
+}
+// Vector i of a row of W elements, zeros past the row's end, in two parts: the load, of the row's last 16 bytes where the row
+// ends in the vector or before it (no branch waits for a value), and the shift to the vector's place.
+template <typename T>
+__device__ __forceinline__ u32x4 fetch_vec(const T* row, int i, int W) {
   constexpr int V = vec<T>::N;
-  if ((i + 1) * V <= W) return *(const u32x4_any*)(row + i * V);
+  if (W >= V) return *(const u32x4_any*)(row + min(i * V, W - V));
   u32x4 r = {0u, 0u, 0u, 0u};
   if constexpr (V == 4) {
 #pragma unroll
@@ -63,6 +77,16 @@ __device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W) {
   }
   return r;
 }
+template <typename T>
+__device__ __forceinline__ u32x4 place_vec(u32x4 v, int i, int W) {
+  constexpr int V = vec<T>::N;
+  if (W < V) return v;
+  const int s = i * V - min(i * V, W - V);
+  if (W % V != 0) return shift_vec<T>(v, s);
+  return s ? u32x4{0u, 0u, 0u, 0u} : v;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 load_vec(const T* row, int i, int W) { return place_vec<T>(fetch_vec(row, i, W), i, W); }
 template <typename T>
 __device__ __forceinline__ void store_vec(T* row, int i, int W, const float (&v)[vec<T>::N]) {
   constexpr int V = vec<T>::N;
@@ -169,7 +193,7 @@ __device__ __forceinline__ float group_reduce(float v, Op op, float* red) {
 }
 
 // Sum over P rows of N columns, 8 columns to a workgroup of 1024 threads: column blockIdx.x * 8 + threadIdx.x in the first 8. A
-// column's 128 threads take a row each in turn (768 rows of 400 columns: 3.0 us where 32 threads to a column took 4.4).
+// column's 128 threads take a row each in turn (768 rows of 400 columns: 3.8 us where 32 threads to a column took 4.4).
 __device__ __forceinline__ float column_sum(const float* part, int P, int N, float (&red)[16][8]) {
   const int n = blockIdx.x * 8 + (threadIdx.x & 7);
   float s = 0.f;

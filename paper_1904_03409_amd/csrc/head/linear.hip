@@ -11,6 +11,7 @@
 // Where the tiles do not fill the chip the sum over k is split, and k_linear_join adds the parts and applies the
 // epilogue.
 #include <algorithm>
+#include <atomic>
 
 #include "../../../include/stacklstm_head.h"
 #include "head.h"
@@ -26,6 +27,9 @@ struct GemmArgs {
   int64_t ldy, ldr;
   int act;
   float* part;                                         // [splits][M][N], NULL: none
+  const void* dz;                                      // k_linear_any: z, where the operand that is dz is given as dy
+  int64_t lddz;
+  int dzact;
 };
 
 // sigma(2 sqrt(2/pi) (z + 0.044715 z^3)): 1 / (1 + 2^(z (k + k3 z^2)))
@@ -187,10 +191,9 @@ struct Where {
   int split, m0, n0, kbeg, kend, nr, nc;
 };
 template <int BM, int BN>
-__device__ __forceinline__ Where where(const GemmArgs& g) {
+__device__ __forceinline__ Where where(const GemmArgs& g, int lid) {
   Where w;
   const int NTL = (g.N + BN - 1) / BN, MTL = (g.M + BM - 1) / BM, tiles = NTL * MTL, all = tiles * g.splits;
-  int lid = (int)blockIdx.x;
   // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of tiles, in groups of 8 row tiles to a
   // column tile, so that what its L2 holds is used again
   const int full = all & ~7;
@@ -326,7 +329,7 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g)
   constexpr int BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ, MEET = MI >= 4 ? 1 : 0;
   static_assert(SA - SB <= 1 && SB - SA <= 1 && SA >= 2 && SB >= 2, "stages");
   extern __shared__ __align__(16) unsigned char sm[];
-  const Where w = where<BM, BN>(g);
+  const Where w = where<BM, BN>(g, (int)blockIdx.x);
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
   Mover<T, AT, BM, NT, S::IA> ma;
@@ -423,49 +426,92 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g)
   epilogue<T, MI, NJ, BM, BN>(g, w, acc, wm, wn, l16, lq);
 }
 
-// Operands at any place, through registers, one slice ahead; two stages.
-template <typename T, bool AT, bool BT, int BM, int BN>
-__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArgs g) {
+// Operands at any place, through registers, one slice ahead; two stages. A slice's loads all go out before the first is
+// waited for; rows are cut to their ends, and zeros put behind them, on the way to LDS. With DZ an operand is dy act'(z),
+// made on that way too (rounded to T, as a stored one is): A of dx, B of dW.
+template <typename T, bool AT, bool BT, int BM, int BN, bool DZ>
+__device__ __forceinline__ void any_tile(const GemmArgs& g, int lid) {
   typedef Tile<T, BM, BN> S;
   typedef typename frag_of<T>::type frag;
   constexpr int BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ;
+  constexpr bool DA = DZ && !BT, DB = DZ && AT;
   extern __shared__ __align__(16) unsigned char sm[];
-  const Where w = where<BM, BN>(g);
+  const Where w = where<BM, BN>(g, lid);
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
   const T* A = (const T*)g.A + (AT ? w.m0 : (int64_t)w.m0 * g.lda);
   const T* B = (const T*)g.B + (BT ? w.n0 : (int64_t)w.n0 * g.ldb);
-  u32x4 ra[S::IA], rb[S::IB];
+  [[maybe_unused]] const T* Z = (const T*)g.dz + (!BT ? (int64_t)w.m0 * g.lddz : w.n0);
+  u32x4 ra[S::IA], rb[S::IB], rz[DA ? S::IA : DB ? S::IB : 1];
+  // f(i, row, granule): granule i of the thread; rows past the last are the last one (their results are not stored, or they
+  // are taken out of the slice)
+  auto each = [&](auto tall, auto rows, auto n, auto f) {
+    constexpr bool TALL = decltype(tall)::value;
+#pragma unroll
+    for (int i = 0; i < decltype(n)::value; ++i) {
+      int r, c;
+      place<T, TALL, decltype(rows)::value>(i * NT + tid, r, c);
+      f(i, r, c);
+    }
+  };
+  typedef std::bool_constant<AT> at;
+  typedef std::bool_constant<BT> bt;
+  typedef std::integral_constant<int, BM> bm;
+  typedef std::integral_constant<int, BN> bn;
+  typedef std::integral_constant<int, S::IA> na;
+  typedef std::integral_constant<int, S::IB> nb;
+  // A granule's row, and the row's elements from the slice (flat) or the tile (tall) on.
+  auto spot = [&](auto tall, const T* p, int64_t ld, int k0, int rows, int r) {
+    const int left = w.kend - k0, rr = min(r, (decltype(tall)::value ? left : rows) - 1);
+    return p + (decltype(tall)::value ? (int64_t)(k0 + rr) * ld : (int64_t)rr * ld + k0);
+  };
   auto fetch = [&](int k0) {
     const int left = w.kend - k0;
-#pragma unroll
-    for (int i = 0; i < S::IA; ++i) {
-      int r, c;
-      place<T, AT, BM>(i * NT + tid, r, c);
-      const bool in = left > 0 && r < (AT ? left : w.nr);
-      ra[i] = in ? load_vec(A + (AT ? (int64_t)(k0 + r) * g.lda : (int64_t)r * g.lda + k0), c, AT ? w.nr : left) : u32x4{0u, 0u, 0u, 0u};
-    }
-#pragma unroll
-    for (int i = 0; i < S::IB; ++i) {
-      int r, c;
-      place<T, BT, BN>(i * NT + tid, r, c);
-      const bool in = left > 0 && r < (BT ? left : w.nc);
-      rb[i] = in ? load_vec(B + (BT ? (int64_t)(k0 + r) * g.ldb : (int64_t)r * g.ldb + k0), c, BT ? w.nc : left) : u32x4{0u, 0u, 0u, 0u};
-    }
+    each(at(), bm(), na(), [&](int i, int r, int c) {
+      ra[i] = fetch_vec(spot(at(), A, g.lda, k0, w.nr, r), c, AT ? w.nr : left);
+      if constexpr (DA)
+        if (g.dz) rz[i] = fetch_vec(spot(at(), Z, g.lddz, k0, w.nr, r), c, left);
+    });
+    each(bt(), bn(), nb(), [&](int i, int r, int c) {
+      rb[i] = fetch_vec(spot(bt(), B, g.ldb, k0, w.nc, r), c, BT ? w.nc : left);
+      if constexpr (DB)
+        if (g.dz) rz[i] = fetch_vec(spot(bt(), Z, g.lddz, k0, w.nc, r), c, w.nc);
+    });
+  };
+  auto through = [&](u32x4& dy, u32x4 z) {
+    float d[vec<T>::N], v[vec<T>::N];
+    vec<T>::unpack(dy, d);
+    vec<T>::unpack(z, v);
+    act_bwd(d, v, g.dzact);
+    dy = vec<T>::pack(d);
   };
   f32x4 acc[MI][NJ];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  fetch(w.kbeg);
+  if (w.kbeg < w.kend) fetch(w.kbeg);
   int buf = 0;
   for (int k0 = w.kbeg; k0 < w.kend; k0 += BK, buf ^= 1) {
     unsigned char* st = sm + buf * (S::ABYTES + S::BBYTES);
-#pragma unroll
-    for (int i = 0; i < S::IA; ++i) *(u32x4*)(st + (i * NT + tid) * 16) = ra[i];
-#pragma unroll
-    for (int i = 0; i < S::IB; ++i) *(u32x4*)(st + S::ABYTES + (i * NT + tid) * 16) = rb[i];
+    const int left = w.kend - k0;
+    const bool cut_a = left < BK || w.nr < BM, cut_b = left < BK || w.nc < BN;
+    each(at(), bm(), na(), [&](int i, int r, int c) {
+      u32x4 v = ra[i];
+      if (cut_a) v = place_vec<T>(v, c, AT ? w.nr : left);
+      if constexpr (DA)
+        if (g.dz) through(v, cut_a ? place_vec<T>(rz[i], c, left) : rz[i]);
+      if (AT && r >= left) v = u32x4{0u, 0u, 0u, 0u};
+      *(u32x4*)(st + (i * NT + tid) * 16) = v;
+    });
+    each(bt(), bn(), nb(), [&](int i, int r, int c) {
+      u32x4 v = rb[i];
+      if (cut_b) v = place_vec<T>(v, c, BT ? w.nc : left);
+      if constexpr (DB)
+        if (g.dz) through(v, cut_b ? place_vec<T>(rz[i], c, w.nc) : rz[i]);
+      if (BT && r >= left) v = u32x4{0u, 0u, 0u, 0u};
+      *(u32x4*)(st + S::ABYTES + (i * NT + tid) * 16) = v;
+    });
     __syncthreads();
     if (k0 + BK < w.kend) fetch(k0 + BK);
 #pragma unroll
@@ -480,6 +526,10 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArg
     }
   }
   epilogue<T, MI, NJ, BM, BN>(g, w, acc, wm, wn, l16, lq);
+}
+template <typename T, bool AT, bool BT, int BM, int BN>
+__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArgs g) {
+  any_tile<T, AT, BT, BM, BN, false>(g, (int)blockIdx.x);
 }
 
 // The parts of a split product added in order, and the epilogue.
@@ -518,50 +568,61 @@ struct DzArgs {
   const void *dy, *z;
   int64_t ldd, ldz;
   void* dz;                                            // NULL: dy serves
-  float* part;                                         // [row blocks][N], NULL: no db
+  float* part;                                         // [row blocks][N], NULL: no sums, or
+  void* db;                                            // one block of rows: the sums themselves
 };
-}  // namespace
-
-// dz = dy act'(z), and the sums of its columns over a block of rows: 32 column vectors, 8 rows at a time.
-template <typename T>
-__global__ void __launch_bounds__(256) k_linear_dz(DzArgs a) {
-  constexpr int V = vec<T>::N;
-  __shared__ float red[8][32 * V + 4];
-  const int c = (int)blockIdx.x * 32 + (threadIdx.x & 31), r8 = threadIdx.x >> 5;
-  const int64_t lo = (int64_t)blockIdx.y * a.rows, hi = min((int64_t)a.M, lo + a.rows);
+// CV column vectors (strip bx) of a block of rows (by), 256 / CV rows at a time and the loads of four such steps together: a row
+// after the other, each with a wait, 128 rows of 520 took 23 us.
+template <typename T, int CV>
+__device__ __forceinline__ void dz_strip(const DzArgs& a, int bx, int by) {
+  constexpr int V = vec<T>::N, R = 256 / CV, U = 4;
+  __shared__ float red[R][CV * V + 4];
+  const int t = threadIdx.x % CV, c = bx * CV + t, r = threadIdx.x / CV;
+  const int64_t lo = (int64_t)by * a.rows, hi = min((int64_t)a.M, lo + a.rows);
   float s[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) s[k] = 0.f;
   if (c * V < a.N) {
-#pragma unroll 4
-    for (int64_t m = lo + r8; m < hi; m += 8) {
-      float d[V];
-      vec<T>::unpack(load_vec((const T*)a.dy + m * a.ldd, c, a.N), d);
-      if (a.z) {
-        float z[V];
-        vec<T>::unpack(load_vec((const T*)a.z + m * a.N, c, a.N), z);
-        act_bwd(d, z, a.act);
+    for (int64_t m = lo + r; m < hi; m += U * R) {
+      u32x4 rd[U], rz[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t n = min(m + u * R, hi - 1);
+        rd[u] = fetch_vec((const T*)a.dy + n * a.ldd, c, a.N);
+        if (a.z) rz[u] = fetch_vec((const T*)a.z + n * a.N, c, a.N);
       }
 #pragma unroll
-      for (int k = 0; k < V; ++k) s[k] += d[k];
-      if (a.dz) store_vec((T*)a.dz + m * a.ldz, c, (int)a.ldz, d);       // (zeros to the end of the padded row)
+      for (int u = 0; u < U; ++u) {
+        const int64_t n = m + u * R;
+        if (n >= hi) break;
+        float d[V];
+        vec<T>::unpack(place_vec<T>(rd[u], c, a.N), d);
+        if (a.z) {
+          float z[V];
+          vec<T>::unpack(place_vec<T>(rz[u], c, a.N), z);
+          act_bwd(d, z, a.act);
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[k] += d[k];
+        if (a.dz) store_vec((T*)a.dz + n * a.ldz, c, (int)a.ldz, d);     // (zeros to the end of the padded row)
+      }
     }
   }
-  if (!a.part) return;
+  if (!a.part && !a.db) return;
 #pragma unroll
-  for (int k = 0; k < V; ++k) red[r8][(threadIdx.x & 31) * V + k] = s[k];
+  for (int k = 0; k < V; ++k) red[r][t * V + k] = s[k];
   __syncthreads();
-  for (int i = threadIdx.x; i < 32 * V; i += 256) {
-    const int n = (int)blockIdx.x * 32 * V + i;
+  for (int i = threadIdx.x; i < CV * V; i += 256) {
+    const int n = bx * CV * V + i;
     if (n >= a.N) continue;
     float v = 0.f;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) v += red[r][i];
-    a.part[(int64_t)blockIdx.y * a.N + n] = v;
+    for (int k = 0; k < R; ++k) v += red[k][i];
+    if (a.db) from_f32(((T*)a.db)[n], v);
+    else a.part[(int64_t)by * a.N + n] = v;
   }
 }
 
-namespace {
 struct PadArgs {
   struct {
     const void* src;
@@ -571,22 +632,50 @@ struct PadArgs {
   } op[2];
   uint32_t first;                                      // first workgroup of the second
 };
-}  // namespace
-
 // Rows copied to rows of whole granules, zeros behind their ends; 16 rows to a workgroup.
 template <typename T>
-__global__ void __launch_bounds__(256) k_linear_pad(PadArgs a) {
-  constexpr int V = vec<T>::N;
-  const bool second = blockIdx.x >= a.first;
+__device__ __forceinline__ void pad_rows(const PadArgs& a, uint32_t b) {
+  constexpr int V = vec<T>::N, U = 4;
+  const bool second = b >= a.first;
   const auto& o = a.op[second];
-  const int nv = (o.cols + V - 1) / V;
-  const int64_t r0 = (int64_t)(blockIdx.x - (second ? a.first : 0)) * 16, n = min((int64_t)16, o.rows - r0) * nv;
-#pragma unroll 4
-  for (int64_t i = threadIdx.x; i < n; i += 256) {
-    const int64_t r = r0 + (uint32_t)i / (uint32_t)nv;
-    const int c = (int)((uint32_t)i % (uint32_t)nv);
-    *(u32x4*)((T*)o.dst + (r * nv + c) * V) = load_vec((const T*)o.src + r * o.ld, c, o.cols);
+  const uint32_t nv = (o.cols + V - 1) / V;
+  const int64_t r0 = (int64_t)(b - (second ? a.first : 0)) * 16;
+  const uint32_t n = (uint32_t)min((int64_t)16, o.rows - r0) * nv;
+  for (uint32_t i = threadIdx.x; i < n; i += 256 * U) {
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t j = min(i + 256 * u, n - 1);
+      v[u] = fetch_vec((const T*)o.src + (r0 + j / nv) * o.ld, (int)(j % nv), o.cols);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t j = i + 256 * u;
+      if (j < n) *(u32x4*)((T*)o.dst + (r0 * nv + j) * V) = place_vec<T>(v[u], (int)(j % nv), o.cols);
+    }
   }
+}
+}  // namespace
+
+// dz = dy act'(z), and the sums of its columns over a block of rows, by the first nd workgroups; copies by the others.
+template <typename T, int CV>
+__global__ void __launch_bounds__(256) k_linear_dz(DzArgs a, int strips, int nd, PadArgs p) {
+  const int b = (int)blockIdx.x;
+  if (b < nd) dz_strip<T, CV>(a, b % strips, b / strips);
+  else pad_rows<T>(p, (uint32_t)(b - nd));
+}
+template <typename T>
+__global__ void __launch_bounds__(256) k_linear_pad(PadArgs a) {
+  pad_rows<T>(a, blockIdx.x);
+}
+
+// A whole backward of few rows in one launch: nx tiles of dx, nw of dW, then strips of db; dz is made where it is read.
+template <typename T>
+__global__ void __launch_bounds__(256, 2) k_linear_few(GemmArgs x, GemmArgs w, DzArgs a, int nx, int nw) {
+  const int b = (int)blockIdx.x;
+  if (b < nx) any_tile<T, false, false, 64, 64, true>(x, b);
+  else if (b < nx + nw) any_tile<T, true, true, 64, 64, true>(w, b - nx);
+  else dz_strip<T, 8>(a, b - nx - nw, 0);
 }
 
 // db: the sums of P blocks of rows.
@@ -624,7 +713,7 @@ Plan gemm_plan(int64_t M, int64_t N, int64_t K, int type, bool wide) {
       const int64_t per = (slices + s - 1) / s, n = tiles * s;
       if ((slices + per - 1) / per != s) continue;
       const double us = 2 + std::max(((n + 255) / 256) * (2e-6 * t * t * per * BK / rate), ((n + 256 * held - 1) / (256 * held)) * per * latency) +
-                        (s > 1 ? 4 + (s + 1) * (double)M * N * 4 / 7e6 : 0);
+                        (s > 1 ? 5 + (s + 1) * (double)M * N * 4 / 7e6 : 0);
       if (us < least) {
         least = us;
         best = {t, (int)s, (int)(per * BK)};
@@ -642,9 +731,22 @@ size_t gemm_bytes(int64_t M, int64_t N, int64_t K, int type) {
   return type == SLSTM_F32 ? a : std::max(a, part_bytes(gemm_plan(M, N, K, type, true), M, N));
 }
 
-hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int threads, int lds, hipStream_t st) {
-  const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+// A kernel's LDS limit is raised once to a device, not at every call.
+hipError_t allow_lds(const void* kern, int lds, std::atomic<uint64_t>& devices) {
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (bit && (devices.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  const hipError_t s = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (s == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+  return s;
+}
+hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int threads, int lds, std::atomic<uint64_t>& devices, hipStream_t st) {
+  if (lds > 65536) {
+    const hipError_t e = allow_lds(kern, lds, devices);
+    if (e != hipSuccess) return e;
+  }
   const int64_t tiles = (((int64_t)g.M + tile - 1) / tile) * (((int64_t)g.N + tile - 1) / tile) * g.splits;
   GemmArgs a = g;
   void* args[] = {&a};
@@ -653,12 +755,14 @@ hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int thread
 template <typename T, bool AT, bool BT, int TILE, int SA, int SB>
 hipError_t launch_dma(const GemmArgs& g, hipStream_t st) {
   typedef Tile<T, TILE, TILE> S;
-  return tile_launch((const void*)k_linear<T, AT, BT, TILE, TILE, SA, SB>, g, TILE, S::NT, S::ABYTES * SA + S::BBYTES * SB, st);
+  static std::atomic<uint64_t> devices;
+  return tile_launch((const void*)k_linear<T, AT, BT, TILE, TILE, SA, SB>, g, TILE, S::NT, S::ABYTES * SA + S::BBYTES * SB, devices, st);
 }
 template <typename T, bool AT, bool BT, int TILE>
 hipError_t launch_any(const GemmArgs& g, hipStream_t st) {
   typedef Tile<T, TILE, TILE> S;
-  return tile_launch((const void*)k_linear_any<T, AT, BT, TILE, TILE>, g, TILE, S::NT, (S::ABYTES + S::BBYTES) * 2, st);
+  static std::atomic<uint64_t> devices;
+  return tile_launch((const void*)k_linear_any<T, AT, BT, TILE, TILE>, g, TILE, S::NT, (S::ABYTES + S::BBYTES) * 2, devices, st);
 }
 
 // A matrix of rows as a product reads it. whole: its rows are whole granules at aligned places, in reach of a
@@ -674,10 +778,18 @@ int64_t padded(int64_t cols, int type) { return (cols + granule(type) - 1) / gra
 constexpr int64_t kReach = 1 << 21;
 bool dims_whole(int64_t cols, int64_t ld, int type) { return cols % granule(type) == 0 && ld % granule(type) == 0 && ld <= kReach; }
 Operand as_is(const void* p, int64_t cols, int64_t ld, int type) { return {p, ld, al16(p) && dims_whole(cols, ld, type)}; }
-// Whether matrices at odd places are copied for this many rows of x, and a copy's bytes (by the dims alone).
+// Whether matrices at odd places are copied for this many rows of x, and a copy's bytes (by the dims alone). Copied, and through
+// registers as they are, a training pass of 300 x 333 x 83 f32 37.4 and 46.8 us, 700 x 777 x 1001 bf16 37.8 and 53.4, 129 x 85
+// x 46 f32 25.2 and 26.6; 4000 x 333 x 777 f32 121 and 179.
 bool copies(int64_t M) { return M > 128; }
 bool needs_copy(int64_t M, int64_t cols, int64_t ld, int type) {
   return copies(M) && !dims_whole(cols, ld, type) && padded(cols, type) <= kReach;
+}
+// A backward in one launch (k_linear_few): up to 128 rows, and a sum of dx over N of at most 8 slices, which take the latency
+// of a load and of act' each. (A training pass of 3 x 16 x 16: 22.6 us with a launch for each of dz, dx and dW, 13.7 in one. 128
+// x 512 in, gelu: 256 out in one 17.6 us, 260 out in three 5.0 + 9.4 + 5.9; 380 out in one 24.7.)
+bool few_rows(const slstm_linear_dims* d) {
+  return d->M > 0 && d->M <= 128 && d->N <= (d->type == SLSTM_F32 ? 256 : 512);
 }
 size_t copy_bytes(int64_t rows, int64_t cols, int type) { return ((size_t)rows * padded(cols, type) * esize(type) + 255) & ~(size_t)255; }
 
@@ -742,15 +854,18 @@ bool linear_ok(const slstm_linear_dims* d) {
   const int64_t most = 0x7fffffff;
   return tiles(d->M, d->N) <= most && tiles(d->M, d->K) <= most && tiles(d->K, d->N) <= most;
 }
-// Blocks of rows of k_linear_dz: about 2048 workgroups, none for fewer than 64 rows.
+// Strips of columns and blocks of rows of k_linear_dz: about 2048 workgroups, none for fewer than 64 rows, one block for up to
+// 128 (it writes db itself). Up to 2048 rows strips of 8 vectors (128 bytes of a row), more workgroups; 32 above.
 struct DzPlan {
+  bool narrow;
   int strips, blocks, rows;
 };
 DzPlan dz_plan(const slstm_linear_dims* d) {
   DzPlan p;
-  const int V = granule(d->type);
-  p.strips = (d->N + 32 * V - 1) / (32 * V);
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(d->M + 63) / 64, 2048 / p.strips, 256}));
+  p.narrow = d->M <= 2048;
+  const int cols = (p.narrow ? 8 : 32) * granule(d->type);
+  p.strips = (d->N + cols - 1) / cols;
+  const int64_t want = d->M <= 128 ? 1 : std::max<int64_t>(1, std::min<int64_t>({(d->M + 63) / 64, 2048 / p.strips, 256}));
   p.rows = (int)(((d->M + want - 1) / want + 7) / 8 * 8);
   p.blocks = (int)std::max<int64_t>(1, (d->M + std::max(1, p.rows) - 1) / std::max(1, p.rows));
   return p;
@@ -824,29 +939,48 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
   char* ws = (char*)workspace;
   const int64_t ldx = row_stride(d->ld_x, d->K), ldw = row_stride(d->ld_w, d->N), ldd = row_stride(d->ld_dy, d->N);
   const bool product = dx || dW, own = s.x > s.dz && product && d->M > 0;
+  if (few_rows(d)) {
+    auto tiles = [](int64_t m, int64_t n) { return (int)(((m + 63) / 64) * ((n + 63) / 64)); };
+    GemmArgs gx = {}, gw = {};
+    gx.M = (int)d->M, gx.N = d->K, gx.K = d->N, gx.A = dy, gx.lda = ldd, gx.B = W, gx.ldb = ldw, gx.y = dx, gx.ldy = d->K;
+    gw.M = d->K, gw.N = d->N, gw.K = (int)d->M, gw.A = x, gw.lda = ldx, gw.B = dy, gw.ldb = ldd, gw.y = dW, gw.ldy = d->N;
+    gx.splits = gw.splits = 1, gx.chunk = gx.K, gw.chunk = gw.K;
+    if (act) gx.dz = gw.dz = z, gx.lddz = gw.lddz = d->N, gx.dzact = gw.dzact = d->act;
+    DzArgs a = {};
+    a.M = (int)d->M, a.N = d->N, a.act = d->act, a.rows = (int)d->M, a.dy = dy, a.z = act ? z : nullptr, a.ldd = ldd, a.db = db;
+    const int nx = dx ? tiles(d->M, d->K) : 0, nw = dW ? tiles(d->K, d->N) : 0, nb = db ? dz_plan(d).strips : 0;
+    if (nx + nw + nb == 0) return SLSTM_OK;
+    const dim3 grid(nx + nw + nb);
+    constexpr int lds = 2 * (Tile<float, 64, 64>::ABYTES + Tile<float, 64, 64>::BBYTES);
+    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_few<float>, grid, dim3(256), lds, st, gx, gw, a, nx, nw);
+    else hipLaunchKernelGGL(k_linear_few<bf16_t>, grid, dim3(256), lds, st, gx, gw, a, nx, nw);
+    return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+  }
   Operand oz = as_is(dy, d->N, ldd, d->type);
   if (own) oz = {ws + s.dz, padded(d->N, d->type), padded(d->N, d->type) <= kReach};
+  Copies cp;
+  Operand ox = {}, ow = {};
+  if (dW) ox = s.W > s.x ? cp.add(x, d->M, d->K, ldx, ws + s.x, d->type) : as_is(x, d->K, ldx, d->type);
+  if (dx) ow = s.db > s.W ? cp.add(W, d->K, d->N, ldw, ws + s.W, d->type) : as_is(W, d->N, ldw, d->type);
+  const DzPlan p = dz_plan(d);
+  const int nd = db || own ? p.strips * p.blocks : 0;
   hipError_t e = hipSuccess;
-  if (db || own) {
-    const DzPlan p = dz_plan(d);
+  if (nd + cp.blocks > 0) {
     DzArgs a = {};
     a.M = (int)d->M, a.N = d->N, a.act = d->act, a.rows = p.rows, a.dy = dy, a.z = act ? z : nullptr;
-    a.ldd = ldd, a.ldz = padded(d->N, d->type), a.dz = own ? ws + s.dz : nullptr, a.part = db ? (float*)(ws + s.db) : nullptr;
-    const dim3 grid(p.strips, p.blocks);
-    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_dz<float>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_linear_dz<bf16_t>, grid, dim3(256), 0, st, a);
-    if (db) {
+    a.ldd = ldd, a.ldz = padded(d->N, d->type), a.dz = own ? ws + s.dz : nullptr, a.part = db && p.blocks > 1 ? (float*)(ws + s.db) : nullptr;
+    a.db = db && p.blocks == 1 ? db : nullptr;
+    const dim3 grid((unsigned)(nd + cp.blocks));
+    auto run = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, p.strips, nd, cp.a); };
+    if (d->type == SLSTM_F32) run(p.narrow ? k_linear_dz<float, 8> : k_linear_dz<float, 32>);
+    else run(p.narrow ? k_linear_dz<bf16_t, 8> : k_linear_dz<bf16_t, 32>);
+    if (a.part) {
       const dim3 cols((d->N + 7) / 8);
       if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(1024), 0, st, a.part, p.blocks, d->N, (float*)db);
       else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(1024), 0, st, a.part, p.blocks, d->N, (bf16_t*)db);
     }
     e = hipGetLastError();
   }
-  Copies cp;
-  Operand ox = {}, ow = {};
-  if (dW) ox = s.W > s.x ? cp.add(x, d->M, d->K, ldx, ws + s.x, d->type) : as_is(x, d->K, ldx, d->type);
-  if (dx) ow = s.db > s.W ? cp.add(W, d->K, d->N, ldw, ws + s.W, d->type) : as_is(W, d->N, ldw, d->type);
-  if (e == hipSuccess) e = cp.run(d->type, st);
   float* part = (float*)(ws + s.part);
   if (e == hipSuccess && dx) {
     GemmArgs g = {};

@@ -14,7 +14,7 @@
 namespace {
 
 struct NormArgs {
-  int rows, W;
+  int rows, W, parts, strips;                          // of a backward: workgroups that take rows, and columns
   float eps;
   const void *x, *res, *dy, *dsum;
   int64_t ldx, ldr, ldd;
@@ -99,11 +99,60 @@ __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_fwd(NormArgs a) {
   }
 }
 
+// dgamma | dbeta of a strip of 16 vectors of columns over all rows, for few rows: NT / 16 rows at a time.
+template <typename T, int NT>
+__device__ __forceinline__ void norm_strip(const NormArgs& a, int strip) {
+  constexpr int V = vec<T>::N, NW = NT / 64;
+  __shared__ float red[NW][2][16 * V];
+  const int c = strip * 16 + (threadIdx.x & 15), W = a.W;
+  float sg[V], sb[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) sg[k] = sb[k] = 0.f;
+  if (c * V < W) {
+#pragma unroll 4
+    for (int row = threadIdx.x >> 4; row < a.rows; row += NT / 16) {
+      float x[V], d[V];
+      vec<T>::unpack(load_vec((const T*)a.x + row * a.ldx, c, W), x);
+      vec<T>::unpack(load_vec((const T*)a.dy + row * a.ldd, c, W), d);
+      const float mu = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        sg[k] += d[k] * ((x[k] - mu) * rstd);
+        sb[k] += d[k];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    sg[k] = across<16>(sg[k], op_sum());
+    sb[k] = across<16>(sb[k], op_sum());
+  }
+  if ((threadIdx.x & 63) < 16) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      red[threadIdx.x >> 6][0][threadIdx.x % 16 * V + k] = sg[k];
+      red[threadIdx.x >> 6][1][threadIdx.x % 16 * V + k] = sb[k];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * V; i += NT) {
+    const int which = i / (16 * V), n = strip * 16 * V + i % (16 * V);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += red[w][which][i % (16 * V)];
+    float* o = which ? a.dbeta : a.dgamma;
+    if (o && n < W) o[n] = v;
+  }
+}
+
 // Rows in turn; a thread keeps the sums of its columns over the rows that its workgroup takes, and the
 // workgroups' sums are added by k_norm_cols in a fixed order (no atomics: equal runs are equal bit for bit).
+// Few rows have workgroups of their own for the columns' sums instead, which read the rows again (from L2: a launch costs
+// more).
 template <typename T, int TPR, int NV>
 __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_bwd(NormArgs a) {
   constexpr int V = vec<T>::N, RPB = norm_rows(TPR);
+  if ((int)blockIdx.x >= a.parts) return norm_strip<T, norm_threads(TPR)>(a, (int)blockIdx.x - a.parts);
   __shared__ float red[2][2][16];
   extern __shared__ float cols[];                      // TPR <= 64: [2][W]
   const int t = threadIdx.x & (TPR - 1), W = a.W;
@@ -133,7 +182,7 @@ __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_bwd(NormArgs a) {
     nmu = here ? a.mean[row] : 0.f;
     nrstd = here ? a.rstd[row] : 0.f;
   };
-  const int64_t step = (int64_t)gridDim.x * RPB;
+  const int64_t step = (int64_t)a.parts * RPB;
   fetch((int64_t)blockIdx.x * RPB + threadIdx.x / TPR);
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, flip ^= 1) {
     const int64_t row = r0 + threadIdx.x / TPR;
@@ -181,9 +230,9 @@ __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_bwd(NormArgs a) {
       store_vec(dx, c, W, o);
     }
   }
-  if (!a.dgamma && !a.dbeta) return;
-  float* pg = gridDim.x == 1 ? a.dgamma : a.part + (size_t)blockIdx.x * 2 * W;
-  float* pb = gridDim.x == 1 ? a.dbeta : a.part + (size_t)blockIdx.x * 2 * W + W;
+  if (a.strips || (!a.dgamma && !a.dbeta)) return;
+  float* pg = a.parts == 1 ? a.dgamma : a.part + (size_t)blockIdx.x * 2 * W;
+  float* pb = a.parts == 1 ? a.dbeta : a.part + (size_t)blockIdx.x * 2 * W + W;
   if constexpr (TPR <= 64) {
     // rows of a wave, then the waves one after the other
 #pragma unroll
@@ -247,12 +296,13 @@ bool norm_ok(const slstm_norm_dims* d) {
 // Lanes to a row: the fewest that hold it in two vectors each up to a wave (22912 rows of 200 floats in 64 lanes of one
 // vector: 9.0 and 14.4 us), then a workgroup (two barriers a row, but the sums of a thread's columns stay in registers: four vectors a lane
 // of 16-bit rows take 234 of them).
+int norm_vec(const slstm_norm_dims* d) { return d->type == SLSTM_F32 ? 4 : 8; }
 int norm_tpr(const slstm_norm_dims* d) {
-  const int n = (d->width + (d->type == SLSTM_F32 ? 3 : 7)) / (d->type == SLSTM_F32 ? 4 : 8);
+  const int n = (d->width + norm_vec(d) - 1) / norm_vec(d);
   return n <= 16 ? 8 : n <= 32 ? 16 : n <= 64 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : 1024;
 }
 int norm_nv(const slstm_norm_dims* d, int tpr) {
-  const int n = (d->width + (d->type == SLSTM_F32 ? 3 : 7)) / (d->type == SLSTM_F32 ? 4 : 8), q = (n + tpr - 1) / tpr;
+  const int n = (d->width + norm_vec(d) - 1) / norm_vec(d), q = (n + tpr - 1) / tpr;
   return q <= 1 ? 1 : 2;
 }
 int norm_parts(const slstm_norm_dims* d) {
@@ -316,7 +366,7 @@ extern "C" int stacklstm_norm_bwd(const slstm_norm_dims* d, const void* x, const
   const int P = norm_parts(d);
   const bool cols = dgamma || dbeta;
   if (cols && P > 1) {
-    if (!workspace) return SLSTM_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 3u)) return SLSTM_EINVAL;
     if (ws_bytes < stacklstm_norm_workspace_bytes(d)) return SLSTM_EWORKSPACE;
   }
   NormArgs a = {};
@@ -325,14 +375,17 @@ extern "C" int stacklstm_norm_bwd(const slstm_norm_dims* d, const void* x, const
   a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.dgamma = dgamma, a.dbeta = dbeta;
   a.part = (float*)workspace;
   a.ldx = row_stride(d->ld_x, d->width), a.ldd = row_stride(d->ld_dy, d->width);
+  // up to 256 rows: strips of columns (17 rows of 1072: 17.9 us a training pass with a launch for the columns)
+  a.parts = P;
+  a.strips = cols && P > 1 && d->rows <= 256 ? (d->width + 16 * norm_vec(d) - 1) / (16 * norm_vec(d)) : 0;
   const bool ok = norm_dispatch(d, [&](auto t, auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value;
-    const size_t lds = TPR <= 64 && cols ? (size_t)2 * d->width * 4 : 0;
-    hipLaunchKernelGGL((k_norm_bwd<decltype(t), TPR, decltype(nv)::value>), dim3(P), dim3(norm_threads(TPR)), lds,
+    const size_t lds = TPR <= 64 && cols && !a.strips ? (size_t)2 * d->width * 4 : 0;
+    hipLaunchKernelGGL((k_norm_bwd<decltype(t), TPR, decltype(nv)::value>), dim3(P + a.strips), dim3(norm_threads(TPR)), lds,
                        as_stream(stream), a);
   });
   if (!ok) return SLSTM_EINVAL;
-  if (cols && P > 1)
+  if (cols && P > 1 && !a.strips)
     hipLaunchKernelGGL(k_norm_cols, dim3((2 * d->width + 7) / 8), dim3(1024), 0, as_stream(stream), a.part, P, d->width, dgamma,
                        dbeta);
   return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
