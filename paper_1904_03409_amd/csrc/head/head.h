@@ -162,6 +162,7 @@ __device__ __forceinline__ float half_swap(float v, Op op) {       // lane ^ 32
 }
 template <int N, typename Op>
 __device__ __forceinline__ float lanes(float v, Op op) {
+  asm("" : "+v"(v));                                   // (a product stays rounded: fused into the first sum it gives every lane another result)
   if constexpr (N >= 2) v = op(v, dpp_move<0xb1>(v));              // quad_perm 1, 0, 3, 2
   if constexpr (N >= 4) v = op(v, dpp_move<0x4e>(v));              // quad_perm 2, 3, 0, 1
   if constexpr (N >= 8) v = op(v, dpp_move<0x141>(v));             // row_half_mirror
@@ -173,6 +174,7 @@ __device__ __forceinline__ float lanes(float v, Op op) {
 // The other way round: over the lanes that have the same place in their group of N, the groups of a wave joined.
 template <int N, typename Op>
 __device__ __forceinline__ float across(float v, Op op) {
+  asm("" : "+v"(v));
   if constexpr (N <= 8) v = op(v, __shfl_xor(v, 8));
   if constexpr (N <= 16) v = row_swap(v, op);
   if constexpr (N <= 32) v = half_swap(v, op);

@@ -99,6 +99,27 @@ def test_ties_go_to_the_lower_place(V, K):
         assert (np.diff(place)[same] > 0).all(), kind
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V", [(64, 83), (64, 1500), (64, 9000), (64, 33000), (64, 64001), (2, 64001), (3, 131072)])
+def test_one_beam_ranks_its_logits(B, V, dtype):
+    """Where one beam is alive, the continuations are its logits in order, equal ones by their place and with equal totals:
+    a row has one log sum, whichever threads look at its tokens."""
+    hd = _hd()
+    rng = rng_for("beam one", B, V, dtype)
+    K = 16
+    x = rounded(2.5 * rng.standard_normal((B * K, V)), "bf16")
+    score = np.full((B, K), -np.inf, np.float32)
+    alive = rng.integers(0, K, B)
+    score[np.arange(B), alive] = -20 * rng.random(B) - 1
+    got = _select(hd, x, score, dtype=dtype)
+    row = x[np.arange(B) * K + alive]
+    order = np.argsort(-row, axis=1, kind="stable")[:, :K]
+    assert np.array_equal(got[1], np.repeat(alive[:, None], K, 1))
+    assert np.array_equal(got[2], order)
+    top = np.take_along_axis(row, order, 1)
+    assert np.array_equal(np.diff(got[0], axis=1) == 0, np.diff(top, axis=1) == 0)
+
+
 @pytest.mark.parametrize("V", [90, 5000, 50000])
 def test_nonfinite_and_masked(V):
     hd = _hd()
