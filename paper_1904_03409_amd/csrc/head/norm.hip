@@ -293,13 +293,14 @@ bool norm_ok(const slstm_norm_dims* d) {
          (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->eps >= 0.f && stride_ok(d->ld_x, d->width) &&
          stride_ok(d->ld_res, d->width) && stride_ok(d->ld_dy, d->width);
 }
-// Lanes to a row: the fewest that hold it in two vectors each up to a wave (22912 rows of 200 floats in 64 lanes of one
-// vector: 9.0 and 14.4 us), then a workgroup (two barriers a row, but the sums of a thread's columns stay in registers: four vectors a lane
-// of 16-bit rows take 234 of them).
+// Lanes to a row: the fewest that hold it in one vector each, up to a wave (with half the lanes and two vectors, 30000 x 512 bf16
+// took 28.4 and 29.7 us, forward and backward, instead of 25.8 and 27.7; 22912 x 100 f32 9.3 and 13.0 instead of 8.5 and 9.7),
+// of two in a whole wave, then a workgroup (two barriers a row, but the sums of a thread's columns stay in registers: four
+// vectors a lane of 16-bit rows take 234 of them).
 int norm_vec(const slstm_norm_dims* d) { return d->type == SLSTM_F32 ? 4 : 8; }
 int norm_tpr(const slstm_norm_dims* d) {
   const int n = (d->width + norm_vec(d) - 1) / norm_vec(d);
-  return n <= 16 ? 8 : n <= 32 ? 16 : n <= 64 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : 1024;
+  return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : 1024;
 }
 int norm_nv(const slstm_norm_dims* d, int tpr) {
   const int n = (d->width + norm_vec(d) - 1) / norm_vec(d), q = (n + tpr - 1) / tpr;
@@ -318,7 +319,7 @@ bool norm_dispatch(const slstm_norm_dims* d, F f) {
 #define NORM_CASE(T_, TPR_, NV_) \
   if (tpr == TPR_ && nv == NV_) return f(T_(), std::integral_constant<int, TPR_>(), std::integral_constant<int, NV_>()), true;
 #define NORM_TYPE(T_) \
-  NORM_CASE(T_, 8, 1) NORM_CASE(T_, 8, 2) NORM_CASE(T_, 16, 2) NORM_CASE(T_, 32, 2) NORM_CASE(T_, 64, 2) \
+  NORM_CASE(T_, 8, 1) NORM_CASE(T_, 16, 1) NORM_CASE(T_, 32, 1) NORM_CASE(T_, 64, 1) NORM_CASE(T_, 64, 2) \
   NORM_CASE(T_, 256, 1) NORM_CASE(T_, 256, 2) NORM_CASE(T_, 512, 2)
   if (d->type == SLSTM_F32) {
     NORM_TYPE(float)
