@@ -46,8 +46,9 @@ __device__ __forceinline__ RowTargets row_targets(const DistillArgs& a, int64_t 
   const float it = 1.f / a.tau;
   for (int j = t; j < a.K; j += N) {
     int i = here ? a.index[row * a.K + j] : -1;
+    const float w = here ? a.value[row * a.K + j] : 0.f;           // (with the index, not behind it)
     if (i < 0 || i >= a.V) i = -1;
-    const float v = i >= 0 ? a.value[row * a.K + j] * it : -INFINITY;
+    const float v = i >= 0 ? w * it : -INFINITY;
     idx[j] = i;
     p[j] = v;
     top = (v > top || v != v) ? v : top;               // (a NaN stays: the row's loss is NaN)
@@ -142,8 +143,8 @@ __device__ __forceinline__ void each_grad(const RowGrad& g, Put put) {
 __device__ __forceinline__ float entry_grad(const DistillArgs& a, const RowGrad& g, const RowTargets& r, int place, float x,
                                             const int* idx, const float* p) {
   float s = 0.f;
-  for (int j = 0; j < a.K; ++j)
-    if (idx[j] == place) s += p[j];
+#pragma unroll 8
+  for (int j = 0; j < a.K; ++j) s += idx[j] == place ? p[j] : 0.f;
   float v = g(x) - g.a * s;
   if (place == r.label) v -= g.b;
   return v;
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
   constexpr int V = vec<T>::N;
-  __shared__ float red[6][16];
+  __shared__ float red[3][16];
   __shared__ int idx[kEntries + 1];
   __shared__ float p[kEntries + 1], u[kEntries + 1];
   // without a gradient there is one workgroup to a row
@@ -335,20 +336,25 @@ __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
     load_row<256>(raw, x, ch * kChunkVecs * 256 + t, a.V);
     end = row_end(x, t, ch + 1 == a.chunks ? a.V : 0);
   }
-  const RowTargets r = row_targets<256>(a, row, true, t, idx, p, red[0]);
-  float m, logst, logs1;
+  // the chunks' sums joined by every wave for itself, 64 at a time; the first loads go out ahead of the barriers below
+  const float* q = a.part + (size_t)row * a.chunks * 3;
+  const int l = t & 63;
+  float m, logst, logs1, q0[3] = {-INFINITY, 0.f, 0.f};
   if (a.stats_in) {
     m = a.stats_in[row * 3];
     logst = a.stats_in[row * 3 + 1];
     logs1 = a.stats_in[row * 3 + 2];
-  } else {
-    const float* q = a.part + (size_t)row * a.chunks * 3;
-    m = -INFINITY;
-    for (int i = t; i < a.chunks; i += 256) m = fmaxf(m, q[3 * i]);
-    m = group_reduce<256>(m, op_max(), red[2]);
+  } else if (l < a.chunks) {
+    q0[0] = q[3 * l], q0[1] = q[3 * l + 1], q0[2] = q[3 * l + 2];
+  }
+  const RowTargets r = row_targets<256>(a, row, true, t, idx, p, red[0]);
+  if (!a.stats_in) {
+    m = fmaxf(-INFINITY, q0[0]);                       // (of a chunk of NaN alone: -inf)
+    for (int i = l + 64; i < a.chunks; i += 64) m = fmaxf(m, q[3 * i]);
+    m = lanes<64>(m, op_max());
     float st = 0.f, s1 = 0.f;
-    for (int i = t; i < a.chunks; i += 256) {
-      const float mi = q[3 * i], vt = q[3 * i + 1], v1 = q[3 * i + 2];
+    for (int i = l; i < a.chunks; i += 64) {
+      const float mi = i == l ? q0[0] : q[3 * i], vt = i == l ? q0[1] : q[3 * i + 1], v1 = i == l ? q0[2] : q[3 * i + 2];
       // (nothing to take from a chunk of -inf, unless it holds NaN or all chunks are like it)
       if (mi == -INFINITY && m > -INFINITY) {
         st += vt;
@@ -358,25 +364,26 @@ __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
       st += vt * __builtin_amdgcn_exp2f((mi - m) * (kLog2e / a.tau));
       s1 += v1 * __builtin_amdgcn_exp2f((mi - m) * kLog2e);
     }
-    logst = logf(group_reduce<256>(st, op_sum(), red[3]));
-    logs1 = logf(group_reduce<256>(s1, op_sum(), red[4]));
+    logst = logf(lanes<64>(st, op_sum()));
+    logs1 = logf(lanes<64>(s1, op_sum()));
   }
   for (int j = t; j <= a.K; j += 256) {
     const int i = j < a.K ? idx[j] : r.label;
     u[j] = i < 0 ? 0.f : a.ent ? a.ent[row * (a.K + 1) + j] : i >= lo && i < hi ? to_f32(x[i]) : 0.f;
   }
-  if (ch == 0) {
+  auto row_out = [&] {
+    if (ch != 0) return;
     if (a.stats && t == 0) {
       a.stats[row * 3] = m;
       a.stats[row * 3 + 1] = logst;
       a.stats[row * 3 + 2] = logs1;
     }
     if (a.loss) {
-      const float loss = row_loss<256>(a, r, t, idx, p, u, m, logst, logs1, red[5]);
+      const float loss = row_loss<256>(a, r, t, idx, p, u, m, logst, logs1, red[2]);
       if (t == a.K % 256) a.loss[row] = loss;
     }
-  }
-  if (!a.dx) return;
+  };
+  if (!a.dx) return row_out();
   T* dx = (T*)a.dx + row * a.ldd;
   const RowGrad g = row_grad(a, r, row, m, logst, logs1);
   __syncthreads();                                     // (every element of the chunk that is fetched by place has been)
@@ -388,6 +395,7 @@ __global__ void __launch_bounds__(256) k_distill_chunk(DistillArgs a) {
     });
     if (ch + 1 == a.chunks && has_end<T>(t, a.V)) from_f32(dx[end_place<T>(t, a.V)], f(end));
   });
+  row_out();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (g.zero) return;
