@@ -30,6 +30,9 @@ struct GemmArgs {
   const void* dz;                                      // k_linear_any: z, where the operand that is dz is given as dy
   int64_t lddz;
   int dzact;
+  const float* dbpart;                                 // dW: blocks of rows summed by workgroups behind the tiles, [dbrows][N]
+  int tiles, dbrows;
+  void* db;
 };
 
 // sigma(2 sqrt(2/pi) (z + 0.044715 z^3)): 1 / (1 + 2^(z (k + k3 z^2)))
@@ -211,6 +214,24 @@ __device__ __forceinline__ Where where(const GemmArgs& g, int lid) {
   return w;
 }
 
+// db: columns 32 b .. of the sums of P blocks of rows, by NT threads with NT floats of LDS.
+template <typename T, int NT>
+__device__ __forceinline__ void db_cols(const float* part, int P, int N, T* db, int b, float* red) {
+  const int n = b * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+  float s = 0.f;
+  if (n < N) {
+#pragma unroll 8
+    for (int p = r; p < P; p += NT / 32) s += part[(int64_t)p * N + n];
+  }
+  red[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= 32 || n >= N) return;
+  float v = 0.f;
+#pragma unroll
+  for (int k = 0; k < NT / 32; ++k) v += red[32 * k + threadIdx.x];
+  from_f32(db[n], v);
+}
+
 // Results of a tile from the accumulators. A lane holds four columns (4 lq ..) of row l16 of every 16x16 tile: 16 bytes of an
 // fp32 output; for a 16-bit one neighbouring column tiles exchange rows of lanes, so that a lane has eight columns of one of
 // them. Either way an instruction writes 64 bytes of 16 rows. The residual's loads all go out first: one after the other they
@@ -329,6 +350,8 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g)
   constexpr int BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ, MEET = MI >= 4 ? 1 : 0;
   static_assert(SA - SB <= 1 && SB - SA <= 1 && SA >= 2 && SB >= 2, "stages");
   extern __shared__ __align__(16) unsigned char sm[];
+  if constexpr (AT)
+    if ((int)blockIdx.x >= g.tiles) return db_cols<T, NT>(g.dbpart, g.dbrows, g.N, (T*)g.db, (int)blockIdx.x - g.tiles, (float*)sm);
   const Where w = where<BM, BN>(g, (int)blockIdx.x);
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
@@ -529,6 +552,10 @@ __device__ __forceinline__ void any_tile(const GemmArgs& g, int lid) {
 }
 template <typename T, bool AT, bool BT, int BM, int BN>
 __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArgs g) {
+  extern __shared__ __align__(16) unsigned char sm[];
+  if constexpr (AT)
+    if ((int)blockIdx.x >= g.tiles)
+      return db_cols<T, Tile<T, BM, BN>::NT>(g.dbpart, g.dbrows, g.N, (T*)g.db, (int)blockIdx.x - g.tiles, (float*)sm);
   any_tile<T, AT, BT, BM, BN, false>(g, (int)blockIdx.x);
 }
 
@@ -678,13 +705,11 @@ __global__ void __launch_bounds__(256, 2) k_linear_few(GemmArgs x, GemmArgs w, D
   else dz_strip<T, 8>(a, b - nx - nw, 0);
 }
 
-// db: the sums of P blocks of rows.
+// db where no dW is asked for.
 template <typename T>
-__global__ void __launch_bounds__(1024) k_linear_db(const float* part, int P, int N, T* db) {
-  __shared__ float red[16][8];
-  const float v = column_sum(part, P, N, red);
-  const int n = blockIdx.x * 8 + threadIdx.x;
-  if (threadIdx.x < 8 && n < N) from_f32(db[n], v);
+__global__ void __launch_bounds__(256) k_linear_db(const float* part, int P, int N, T* db) {
+  __shared__ float red[256];
+  db_cols<T, 256>(part, P, N, db, (int)blockIdx.x, red);
 }
 
 namespace {
@@ -749,8 +774,9 @@ hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int thread
   }
   const int64_t tiles = (((int64_t)g.M + tile - 1) / tile) * (((int64_t)g.N + tile - 1) / tile) * g.splits;
   GemmArgs a = g;
+  a.tiles = (int)tiles;
   void* args[] = {&a};
-  return hipLaunchKernel(kern, dim3((unsigned)tiles), dim3(threads), args, lds, st);
+  return hipLaunchKernel(kern, dim3((unsigned)(tiles + (g.dbpart ? (g.N + 31) / 32 : 0))), dim3(threads), args, lds, st);
 }
 template <typename T, bool AT, bool BT, int TILE, int SA, int SB>
 hipError_t launch_dma(const GemmArgs& g, hipStream_t st) {
@@ -849,9 +875,9 @@ bool linear_ok(const slstm_linear_dims* d) {
   if (!stride_ok(d->ld_x, d->K) || !stride_ok(d->ld_w, d->N) || !stride_ok(d->ld_res, d->N) || !stride_ok(d->ld_y, d->N) ||
       !stride_ok(d->ld_dy, d->N))
     return false;
-  // tiles of 64 of each output, in 31 bits
+  // tiles of 64 of each output, and 2^19 workgroups for db, in 31 bits
   auto tiles = [](int64_t m, int64_t n) { return ((m + 63) / 64) * ((n + 63) / 64); };
-  const int64_t most = 0x7fffffff;
+  const int64_t most = 0x7fffffff - (1 << 19);
   return tiles(d->M, d->N) <= most && tiles(d->M, d->K) <= most && tiles(d->K, d->N) <= most;
 }
 // Strips of columns and blocks of rows of k_linear_dz: about 2048 workgroups, none for fewer than 64 rows, one block for up to
@@ -974,10 +1000,10 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
     auto run = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, p.strips, nd, cp.a); };
     if (d->type == SLSTM_F32) run(p.narrow ? k_linear_dz<float, 8> : k_linear_dz<float, 32>);
     else run(p.narrow ? k_linear_dz<bf16_t, 8> : k_linear_dz<bf16_t, 32>);
-    if (a.part) {
-      const dim3 cols((d->N + 7) / 8);
-      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(1024), 0, st, a.part, p.blocks, d->N, (float*)db);
-      else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(1024), 0, st, a.part, p.blocks, d->N, (bf16_t*)db);
+    if (a.part && !dW) {
+      const dim3 cols((d->N + 31) / 32);
+      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_linear_db<float>, cols, dim3(256), 0, st, a.part, p.blocks, d->N, (float*)db);
+      else hipLaunchKernelGGL(k_linear_db<bf16_t>, cols, dim3(256), 0, st, a.part, p.blocks, d->N, (bf16_t*)db);
     }
     e = hipGetLastError();
   }
@@ -990,6 +1016,7 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
   if (e == hipSuccess && dW) {
     GemmArgs g = {};
     g.M = d->K, g.N = d->N, g.K = (int)d->M, g.y = dW, g.ldy = d->N;
+    if (db && p.blocks > 1) g.dbpart = (const float*)(ws + s.db), g.dbrows = p.blocks, g.db = db;
     e = gemm<true, true>(g, ox, oz, d->type, part, st);
   }
   return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
