@@ -344,15 +344,15 @@ struct Mover {
 // 2 x 65536 x 1024 x 4096 flop of 16 bits, random values, dx: with fragments read at the start of each slice, two stages, 1090
 // TFLOP/s.
 template <typename T, bool AT, bool BT, int BM, int BN, int SA, int SB>
-__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g) {
+__device__ __forceinline__ void dma_tile(const GemmArgs& g, int lid) {
   typedef Tile<T, BM, BN> S;
   typedef typename frag_of<T>::type frag;
   constexpr int BK = S::BK, NT = S::NT, MI = S::MI, NJ = S::NJ, MEET = MI >= 4 ? 1 : 0;
   static_assert(SA - SB <= 1 && SB - SA <= 1 && SA >= 2 && SB >= 2, "stages");
   extern __shared__ __align__(16) unsigned char sm[];
   if constexpr (AT)
-    if ((int)blockIdx.x >= g.tiles) return db_cols<T, NT>(g.dbpart, g.dbrows, g.N, (T*)g.db, (int)blockIdx.x - g.tiles, (float*)sm);
-  const Where w = where<BM, BN>(g, (int)blockIdx.x);
+    if (lid >= g.tiles) return db_cols<T, NT>(g.dbpart, g.dbrows, g.N, (T*)g.db, lid - g.tiles, (float*)sm);
+  const Where w = where<BM, BN>(g, lid);
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, l16 = lane & 15, lq = lane >> 4;
   Mover<T, AT, BM, NT, S::IA> ma;
@@ -447,6 +447,18 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g)
   }
   wait_vm<0>();                                        // (DMAs past the end of k write zeros to LDS: all are done before it is given up)
   epilogue<T, MI, NJ, BM, BN>(g, w, acc, wm, wn, l16, lq);
+}
+
+template <typename T, bool AT, bool BT, int BM, int BN, int SA, int SB>
+__global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear(GemmArgs g) {
+  dma_tile<T, AT, BT, BM, BN, SA, SB>(g, (int)blockIdx.x);
+}
+// dx and dW (and db) in one launch: the first x.tiles workgroups take dx.
+template <typename T, int TILE, int SA, int SB>
+__global__ void __launch_bounds__((Tile<T, TILE, TILE>::NT), 2) k_linear_both(GemmArgs x, GemmArgs w) {
+  const int b = (int)blockIdx.x;
+  if (b < x.tiles) dma_tile<T, false, false, TILE, TILE, SA, SB>(x, b);
+  else dma_tile<T, true, true, TILE, TILE, SA, SB>(w, b - x.tiles);
 }
 
 // Operands at any place, through registers, one slice ahead; two stages. A slice's loads all go out before the first is
@@ -718,7 +730,17 @@ bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 // How a product runs: block tile, parts of k.
 struct Plan {
   int tile, splits, chunk;
+  double us;                                           // estimated
 };
+// A CU's TFLOP/s with as many workgroups of a tile as it holds, and the us of a slice where there are few.
+struct TileCost {
+  double rate, latency;
+  int held;
+};
+TileCost tile_cost(bool f32, int t) {
+  return {f32 ? (t == 128 ? 0.56 : 0.52) : t == 256 ? 4.2 : t == 128 ? 3.0 : 2.2, f32 ? 0.45 : 0.35, t == 256 ? 1 : t == 128 ? 2 : 3};
+}
+double join_us(int64_t M, int64_t N, int64_t s) { return s > 1 ? 5 + (s + 1) * (double)M * N * 4 / 7e6 : 0; }
 // The tile and the split with the least estimated time, in us: a CU's share of the products at the tile's rate (TFLOP/s of a
 // CU with as many workgroups as it holds: a smaller tile reads more operands to a product), or a workgroup's slices at
 // the latency of one where there are few; split parts are written, read once more and take a launch. Over 99 products
@@ -728,21 +750,39 @@ Plan gemm_plan(int64_t M, int64_t N, int64_t K, int type, bool wide) {
   const bool f32 = type == SLSTM_F32;
   const int BK = f32 ? 32 : 64;
   const int64_t slices = std::max<int64_t>(1, (K + BK - 1) / BK);
-  Plan best = {64, 1, (int)(slices * BK)};
-  double least = 1e300;
+  Plan best = {64, 1, (int)(slices * BK), 1e300};
   for (int t = wide && !f32 ? 256 : 128; t >= 64; t /= 2) {
-    const double rate = f32 ? (t == 128 ? 0.56 : 0.52) : t == 256 ? 4.2 : t == 128 ? 3.0 : 2.2, latency = f32 ? 0.45 : 0.35;
-    const int held = t == 256 ? 1 : t == 128 ? 2 : 3;
+    const TileCost c = tile_cost(f32, t);
     const int64_t tiles = ((M + t - 1) / t) * ((N + t - 1) / t);
     for (int64_t s = 1; s <= 64 && (s == 1 || (slices / s >= 4 && tiles * s <= 2048)); ++s) {
       const int64_t per = (slices + s - 1) / s, n = tiles * s;
       if ((slices + per - 1) / per != s) continue;
-      const double us = 2 + std::max(((n + 255) / 256) * (2e-6 * t * t * per * BK / rate), ((n + 256 * held - 1) / (256 * held)) * per * latency) +
-                        (s > 1 ? 5 + (s + 1) * (double)M * N * 4 / 7e6 : 0);
-      if (us < least) {
-        least = us;
-        best = {t, (int)s, (int)(per * BK)};
-      }
+      const double us = 2 + std::max(((n + 255) / 256) * (2e-6 * t * t * per * BK / c.rate), ((n + 256 * c.held - 1) / (256 * c.held)) * per * c.latency) +
+                        join_us(M, N, s);
+      if (us < best.us) best = {t, (int)s, (int)(per * BK), us};
+    }
+  }
+  return best;
+}
+// dx [M, K] and dW [K, N] in one launch: tile and dW's split (us 1e300: not to be). Their workgroups share the CUs, so the whole
+// rounds and the last one's waits of two launches become one sum of work.
+Plan both_plan(int64_t M, int64_t K, int64_t N, int type) {
+  const bool f32 = type == SLSTM_F32;
+  const int BK = f32 ? 32 : 64;
+  const int64_t sx = (N + BK - 1) / BK, sw = std::max<int64_t>(1, (M + BK - 1) / BK);
+  Plan best = {64, 1, (int)(sw * BK), 1e300};
+  for (int t = 128; t >= 64; t /= 2) {
+    const TileCost c = tile_cost(f32, t);
+    const int64_t tx = ((M + t - 1) / t) * ((K + t - 1) / t), tw = ((K + t - 1) / t) * ((N + t - 1) / t);
+    if (tx + tw > 1 << 20) continue;
+    for (int64_t s = 1; s <= 64 && (s == 1 || (sw / s >= 4 && tw * s <= 2048)); ++s) {
+      const int64_t per = (sw + s - 1) / s;
+      if ((sw + per - 1) / per != s) continue;
+      const double slice = 2e-6 * t * t * BK / c.rate;
+      const double share = std::min<double>(c.held, (tx + tw * s + 255) / 256);      // workgroups that a CU holds together
+      const double us = 2 + std::max((tx * sx + tw * s * per) * slice / 256 + 0.5 * per * slice, std::max(sx, per) * std::max(c.latency, share * slice)) +
+                        join_us(K, N, s);
+      if (us < best.us) best = {t, (int)s, (int)(per * BK), us};
     }
   }
   return best;
@@ -840,6 +880,30 @@ struct Copies {
   }
 };
 
+hipError_t join_launch(const GemmArgs& g, int type, hipStream_t st) {
+  const int V = granule(type);
+  const int64_t n = (int64_t)g.M * ((g.N + V - 1) / V);
+  const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 4096));
+  if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_join<float>, grid, dim3(256), 0, st, g);
+  else hipLaunchKernelGGL(k_linear_join<bf16_t>, grid, dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+template <typename T, int TILE, int SA, int SB>
+hipError_t launch_both(GemmArgs x, GemmArgs w, hipStream_t st) {
+  typedef Tile<T, TILE, TILE> S;
+  constexpr int lds = S::ABYTES * SA + S::BBYTES * SB;
+  static std::atomic<uint64_t> devices;
+  const void* kern = (const void*)k_linear_both<T, TILE, SA, SB>;
+  if (lds > 65536) {
+    const hipError_t e = allow_lds(kern, lds, devices);
+    if (e != hipSuccess) return e;
+  }
+  auto tiles = [](const GemmArgs& g) { return ((g.M + TILE - 1) / TILE) * ((g.N + TILE - 1) / TILE) * g.splits; };
+  x.tiles = tiles(x), w.tiles = tiles(w);
+  void* args[] = {&x, &w};
+  return hipLaunchKernel(kern, dim3(x.tiles + w.tiles + (w.dbpart ? (w.N + 31) / 32 : 0)), dim3(S::NT), args, lds, st);
+}
+
 // One product with its epilogue; g has the sizes and the outputs.
 template <bool AT, bool BT>
 hipError_t gemm(GemmArgs g, const Operand& A, const Operand& B, int type, float* part, hipStream_t st) {
@@ -859,13 +923,26 @@ hipError_t gemm(GemmArgs g, const Operand& A, const Operand& B, int type, float*
     else if (p.tile == 256) e = launch_dma<bf16_t, AT, BT, 256, 3, 2>(g, st);
     else e = big ? launch_dma<bf16_t, AT, BT, 128, 3, 2>(g, st) : launch_dma<bf16_t, AT, BT, 64, 3, 3>(g, st);
   }
-  if (e != hipSuccess || p.splits == 1) return e;
-  const int V = granule(type);
-  const int64_t n = (int64_t)g.M * ((g.N + V - 1) / V);
-  const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 4096));
-  if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_join<float>, grid, dim3(256), 0, st, g);
-  else hipLaunchKernelGGL(k_linear_join<bf16_t>, grid, dim3(256), 0, st, g);
-  return hipGetLastError();
+  return e != hipSuccess || p.splits == 1 ? e : join_launch(g, type, st);
+}
+// Both products of a backward, dW's split in p.
+hipError_t gemm_both(GemmArgs x, GemmArgs w, const Operand& dz, const Operand& W, const Operand& X, const Plan& p, int type, float* part,
+                     hipStream_t st) {
+  x.A = dz.p, x.lda = dz.ld, x.B = W.p, x.ldb = W.ld, x.splits = 1, x.chunk = x.K;
+  w.A = X.p, w.lda = X.ld, w.B = dz.p, w.ldb = dz.ld, w.splits = p.splits, w.chunk = p.chunk;
+  w.part = p.splits > 1 ? part : nullptr;
+  hipError_t e;
+  if (type == SLSTM_F32) e = p.tile == 128 ? launch_both<float, 128, 3, 2>(x, w, st) : launch_both<float, 64, 3, 3>(x, w, st);
+  else e = p.tile == 128 ? launch_both<bf16_t, 128, 3, 2>(x, w, st) : launch_both<bf16_t, 64, 3, 3>(x, w, st);
+  return e != hipSuccess || p.splits == 1 ? e : join_launch(w, type, st);
+}
+// Whether one launch is estimated to take less than two and the gap between them (fp32's two are a fifth slower than estimated:
+// a last round's workgroups have a CU to themselves). One and two launches, us of dx and dW: 6000 x 176 x 416 bf16 16.5 and 24.3,
+// f32 27.9 and 38.7; 7680 x 512 x 512 f32 77.8 and 82.6; two where chains of slices are long: 512 x 1024 x 8000 f32 177 and 147,
+// 128 x 1024 x 32000 583 and 165.
+bool both_pays(const slstm_linear_dims* d, const Plan& b) {
+  const double two = gemm_plan(d->M, d->K, d->N, d->type, true).us + gemm_plan(d->K, d->N, d->M, d->type, true).us + 1;
+  return d->M > 0 && b.us * (d->type == SLSTM_F32 ? 0.8 : 1.) < two;
 }
 
 bool linear_ok(const slstm_linear_dims* d) {
@@ -916,7 +993,8 @@ Spaces bwd_spaces(const slstm_linear_dims* d) {
   s.W = s.x + (needs_copy(d->M, d->K, row_stride(d->ld_x, d->K), d->type) ? copy_bytes(d->M, d->K, d->type) : 0);
   s.db = s.W + (needs_copy(d->M, d->N, row_stride(d->ld_w, d->N), d->type) ? copy_bytes(d->K, d->N, d->type) : 0);
   s.part = s.db + (((size_t)dz_plan(d).blocks * d->N * 4 + 255) & ~(size_t)255);
-  s.total = s.part + std::max(gemm_bytes(d->M, d->K, d->N, d->type), gemm_bytes(d->K, d->N, d->M, d->type));
+  s.total = s.part + std::max({gemm_bytes(d->M, d->K, d->N, d->type), gemm_bytes(d->K, d->N, d->M, d->type),
+                               part_bytes(both_plan(d->M, d->K, d->N, d->type), d->K, d->N)});
   return s;
 }
 
@@ -1008,16 +1086,18 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
     e = hipGetLastError();
   }
   float* part = (float*)(ws + s.part);
-  if (e == hipSuccess && dx) {
-    GemmArgs g = {};
-    g.M = (int)d->M, g.N = d->K, g.K = d->N, g.y = dx, g.ldy = d->K;
-    e = gemm<false, false>(g, oz, ow, d->type, part, st);
+  GemmArgs gx = {}, gw = {};
+  gx.M = (int)d->M, gx.N = d->K, gx.K = d->N, gx.y = dx, gx.ldy = d->K;
+  gw.M = d->K, gw.N = d->N, gw.K = (int)d->M, gw.y = dW, gw.ldy = d->N;
+  if (db && p.blocks > 1) gw.dbpart = (const float*)(ws + s.db), gw.dbrows = p.blocks, gw.db = db;
+  if (dx && dW && ox.whole && ow.whole && oz.whole) {
+    const Plan b = both_plan(d->M, d->K, d->N, d->type);
+    if (both_pays(d, b)) {
+      if (e == hipSuccess) e = gemm_both(gx, gw, oz, ow, ox, b, d->type, part, st);
+      return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+    }
   }
-  if (e == hipSuccess && dW) {
-    GemmArgs g = {};
-    g.M = d->K, g.N = d->N, g.K = (int)d->M, g.y = dW, g.ldy = d->N;
-    if (db && p.blocks > 1) g.dbpart = (const float*)(ws + s.db), g.dbrows = p.blocks, g.db = db;
-    e = gemm<true, true>(g, ox, oz, d->type, part, st);
-  }
+  if (e == hipSuccess && dx) e = gemm<false, false>(gx, oz, ow, d->type, part, st);
+  if (e == hipSuccess && dW) e = gemm<true, true>(gw, ox, oz, d->type, part, st);
   return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }
