@@ -52,6 +52,19 @@ def test_forward_and_backward(M, K, N, dtype):
     close(r.db, dz.sum(0), dtype, "db")
 
 
+# a backward of few rows in one launch, up to its ends and past them; dx and dW in one launch, sums of dW split and not; db in
+# strips narrow and wide, of several blocks of rows; rows that end in every place of a vector, or have less than one
+LAUNCHES = [(128, 512, 256), (128, 512, 260), (128, 300, 257), (100, 300, 300), (128, 70, 3), (5, 1, 513), (77, 65, 7), (33, 301, 302),
+            (129, 85, 46), (200, 512, 512), (660, 413, 23), (700, 333, 5), (1000, 500, 333), (2048, 200, 31), (2049, 96, 516),
+            (2100, 300, 1100), (6000, 176, 416), (9000, 9, 11)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", LAUNCHES)
+def test_launches(M, K, N, dtype):
+    test_forward_and_backward(M, K, N, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [3, 8])
 def test_strides(dtype, pad):
