@@ -573,34 +573,43 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArg
   any_tile<T, AT, BT, BM, BN, false>(g, (int)blockIdx.x);
 }
 
-// The parts of a split product added in order, and the epilogue.
+// The parts of a split product, and the epilogue: 64 vectors to a workgroup, each wave adds every fourth part, the first one the
+// waves' sums, always in the same order (dW of 26751 x 176 x 416 bf16: 6.9 us; with all parts added by one wave 18).
 template <typename T>
 __global__ void __launch_bounds__(256) k_linear_join(GemmArgs g) {
   constexpr int V = vec<T>::N;
-  const int nv = (g.N + V - 1) / V;
-  const int64_t all = (int64_t)g.M * nv;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    const int64_t m = i / nv;
-    const int n = (int)(i - m * nv) * V;
-    float v[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = 0.f;
-    float b[V];
+  __shared__ float red[3][V][64];
+  const int nv = (g.N + V - 1) / V, q = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const int64_t all = (int64_t)g.M * nv, at = (int64_t)blockIdx.x * 64 + l, i = min(at, all - 1), m = i / nv;
+  const int n = (int)(i - m * nv) * V;
+  float b[V], v[V];
+  u32x4 res = {0u, 0u, 0u, 0u};
+  if (q == 0) {
     load_bias<T>(g, n, b);
-    const u32x4 res = g.res ? load_res<false, T>(g, m, n) : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll 8
-    for (int s = 0; s < g.splits; ++s) {
-      const float* p = g.part + ((int64_t)s * g.M + m) * g.N + n;
-#pragma unroll
-      for (int k = 0; k < V; k += 4) {
-        float w[4];
-        vec<float>::unpack(load_vec(p, k / 4, g.N - n), w);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) v[k + h] += w[h];
-      }
-    }
-    finish<false, T>(g, m, n, v, b, res);
+    if (g.res) res = load_res<false, T>(g, m, n);
   }
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = 0.f;
+#pragma unroll 8
+  for (int s = q; s < g.splits; s += 4) {
+    const float* p = g.part + ((int64_t)s * g.M + m) * g.N + n;
+#pragma unroll
+    for (int k = 0; k < V; k += 4) {
+      float w[4];
+      vec<float>::unpack(load_vec(p, k / 4, g.N - n), w);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) v[k + h] += w[h];
+    }
+  }
+  if (q) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) red[q - 1][k][l] = v[k];
+  }
+  __syncthreads();
+  if (q || at >= all) return;
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] += red[0][k][l] + red[1][k][l] + red[2][k][l];
+  finish<false, T>(g, m, n, v, b, res);
 }
 
 namespace {
@@ -885,7 +894,7 @@ struct Copies {
 hipError_t join_launch(const GemmArgs& g, int type, hipStream_t st) {
   const int V = granule(type);
   const int64_t n = (int64_t)g.M * ((g.N + V - 1) / V);
-  const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 4096));
+  const dim3 grid((unsigned)((n + 63) / 64));          // (a product that is split has at most 2048 tiles)
   if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_join<float>, grid, dim3(256), 0, st, g);
   else hipLaunchKernelGGL(k_linear_join<bf16_t>, grid, dim3(256), 0, st, g);
   return hipGetLastError();
