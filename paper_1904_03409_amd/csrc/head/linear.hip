@@ -79,7 +79,7 @@ __device__ __forceinline__ void act_bwd(float (&d)[V], const float (&z)[V], int 
     case SLSTM_ACT_GELU:
       each([](float v) {
         const float s = gelu_gate(v);
-        return s + v * s * (1.f - s) * (1.5957691216057308f + 0.21406859f * v * v);
+        return s + v * s * (1.f - s) * (1.5957691216057308f + 0.21406445f * v * v);
       });
       break;
   }
