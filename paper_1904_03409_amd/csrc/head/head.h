@@ -213,16 +213,18 @@ __device__ __forceinline__ float column_sum(const float* part, int P, int N, flo
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
-// exp((x - m) k ln 2) as 2^(x k - mk) in one fused step. mk is m k rounded: every term of a row is off by the one factor
-// 2^off, which its sum and its gradient take out again.
+// exp((x - m) k ln 2) as 2^(x k - mk) in one fused step, m the largest x of a row. mk is m k rounded: every term of a row is
+// off by the one factor 2^off, which its sum and its gradient take out again. off is up to half a rounding step of mk, 32 where
+// |mk| is below 2^30; past that the factor (or its square) would leave fp32's range, but no value there is within 64 of m k but m
+// itself: an element is the maximum or nothing (2^-64), and is told from it by any k that is no smaller. A power of two makes
+// m k exact and off 0.
 struct Expo {
   float k, mk, off;
   __device__ __forceinline__ Expo() {}
   __device__ __forceinline__ Expo(float m, float k_) : k(k_), mk(m * k_) {
-    // past fp32's range (logits of the type's lowest value): an element is the maximum or nothing, and is told from it by
-    // any power of two that keeps both in range
-    if (!(fabsf(mk) < 1e38f) && fabsf(m) < INFINITY) {
-      k = 0x1p-60f;
+    if (!(fabsf(mk) < 0x1p30f) && fabsf(m) < INFINITY) {
+      // (past fp32's range a smaller power does: neighbours of such an m are 2^81 apart and more, and k is at most 2^21)
+      k = fabsf(mk) < 1e38f ? __uint_as_float((__float_as_uint(k) + 0x7fffffu) & 0x7f800000u) : 0x1p-60f;
       mk = m * k;
     }
     off = __builtin_fmaf(m, k, -mk);
