@@ -20,6 +20,7 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr int kMaxBeams = 64, kList = 1024;
+constexpr float kFar = -0x1p29f;                       // base-2 exponents below it are none of a row's sum
 constexpr int kPartVecs = 4;                           // vectors a thread in a chunk of 256 threads
 constexpr int kSmall = 8192;                           // totals of a search that fit one workgroup's LDS
 
@@ -217,9 +218,9 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
   if (!beam_runs(a, row, ch, score)) return;
   u32x4 raw[NV];
   float most[NV], mine = -INFINITY;                    // largest of a vector, of all
-  // sum of 2^(x k - ref) of this thread, ref the largest x k so far: the exponentials run while later vectors arrive
-  // (1024 rows of 64001 in 41 us; 43.4 with a pass for the maximum before)
-  float ref = -1e30f, sum = 0.f;
+  // sum of 2^(x k - ref) of this thread, ref the largest x k so far, from kFar on (whose rounding keeps the sum in range): the
+  // exponentials run while later vectors arrive (1024 rows of 64001 in 41 us; 43.4 with a pass for the maximum before)
+  float ref = kFar, sum = 0.f;
   const bool tail = !JOIN || ch + 1 == a.chunks;
   float end;
   load_logits<NT, T>(a, row, c0, raw, tail, end);
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(NT) k_beam_rows(BeamArgs a) {
     const float top = lanes<W>(red[1][l], op_max());
     sum = lanes<W>(red[2][l] * __builtin_amdgcn_exp2f(red[1][l] - top), op_sum());
     const Expo ex(m, kLog2e);                          // (its mk is top)
-    if (!(fabsf(m) < 1e29f)) {                         // out of ref's range (lowest values, infinities): once more, from memory
+    if (!(fabsf(m) < -0.5f * kFar)) {                  // out of ref's range (masked rows, infinities): once more, from memory
       sum = 0.f;
 #pragma unroll 1
       for (int i = 0; i < NV; ++i) {

@@ -113,3 +113,9 @@ def test_beam_of_far_logits_in_a_workgroup(V):
 @pytest.mark.parametrize("V", [33000, 131072])
 def test_beam_of_far_logits_in_chunks(V, dtype):
     _beam_of_far_logits(V, 4, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,V", [(4, 5003), (4, 9000), (160, 33000)])
+def test_beam_of_far_logits_in_rows(B, V, dtype):
+    _beam_of_far_logits(V, B, dtype)
