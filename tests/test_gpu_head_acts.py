@@ -5,7 +5,7 @@ import pytest
 
 from tests import head_ref as ref
 from tests.gpu_helpers import need_gpu
-from tests.head_gpu import get, rounded, up
+from tests.head_gpu import ULP16, get, rounded, up
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,19 @@ def test_gelu_derivative_has_no_bias(n):
         z = rounded(np.linspace(lo, hi, n), "f32")
         g = _through(z, "gelu", "f32")[1]
         assert abs((g - ref.act_grad(z, "gelu")).mean()) <= 1e-7
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [120, 3000])
+def test_tanh_keeps_small_values(n, dtype):
+    """Every value against itself, not against the largest: eight roundings of 2^-24 (exp2, 1 - e, 1 + e, its reciprocal, the
+    product, each up to one or two of them, over 1 - e of at least 0.39 e)."""
+    z = np.geomspace(1e-36, 20.0, n // 2)
+    z = rounded(np.concatenate([-z, z]), dtype)
+    y, g = _through(z, "tanh", dtype)
+    one = ULP16 if dtype == "bf16" else 0.0
+    assert (np.abs(y - np.tanh(z)) <= (5e-7 + one) * np.abs(np.tanh(z))).all()
+    # the derivative 1 / cosh^2: the exponent's rounding grows with z
+    want = 1 / np.cosh(z) ** 2
+    assert (np.abs(g - want) <= (1e-6 + 4e-7 * np.abs(z) + one) * want).all()
+    assert _through(np.zeros(n), "tanh", dtype)[0].tolist() == [0.0] * n
