@@ -88,7 +88,8 @@ __device__ __forceinline__ void act_bwd(float (&d)[V], const float (&z)[V], int 
     case SLSTM_ACT_GELU:
       each([](float v) {
         const float s = gelu_gate(v);
-        return s + v * s * (1.f - s) * (1.5957691216057308f + 0.21406445f * v * v);
+        // (s (1 - s) is 0 long before |z| = 64: the square of a large z stays finite beside it)
+        return s + v * s * (1.f - s) * (1.5957691216057308f + 0.21406445f * fminf(v * v, 4096.f));
       });
       break;
   }

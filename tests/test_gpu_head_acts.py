@@ -5,7 +5,7 @@ import pytest
 
 from tests import head_ref as ref
 from tests.gpu_helpers import need_gpu
-from tests.head_gpu import ULP16, get, rounded, up
+from tests.head_gpu import TOL32, ULP16, get, rounded, up
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +44,22 @@ def test_tanh_keeps_small_values(n, dtype):
     want = 1 / np.cosh(z) ** 2
     assert (np.abs(g - want) <= (1e-6 + 4e-7 * np.abs(z) + one) * want).all()
     assert _through(np.zeros(n), "tanh", dtype)[0].tolist() == [0.0] * n
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu", "tanh", "silu", "gelu"])
+@pytest.mark.parametrize("n", [90, 400])
+def test_ends_of_the_range(n, act, dtype):
+    """Values and derivatives from -40 to 40 and on to the type's largest value, each within the bar of its own size (of 1 for
+    smaller ones) and of one rounding to the type."""
+    big = np.array([1e3, 1e5, 1e10, 1e18, 2e19, 1e25, 1e30, 3e38])
+    z = rounded(np.concatenate([np.linspace(-40, 40, n - 16), -big, big]), dtype)
+    y, g = _through(z, act, dtype)
+    c = np.clip(z, -1e3, 1e3)                           # (past it the derivative is at its end, and 64 bits overflow in it)
+    wy, wg = ref.act(c, act), ref.act_grad(c, act)
+    far = np.abs(z) > 1e3
+    if act != "tanh":
+        wy[far] = np.where((z[far] < 0) & (act != "none"), 0.0, z[far])
+    one = ULP16 if dtype == "bf16" else 0.0
+    for got, want in ((y, wy), (g, wg)):
+        assert (np.abs(got - want) <= TOL32 * np.maximum(1, np.abs(want)) + one * np.abs(want)).all(), act
