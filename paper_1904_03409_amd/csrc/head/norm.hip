@@ -205,9 +205,8 @@ __global__ void __launch_bounds__(norm_threads(TPR)) k_norm_bwd(NormArgs a) {
         if (a.gamma && c * V + h < W) vec<float>::unpack(load_vec(a.gamma, (c * V + h) / 4, W), w);
 #pragma unroll
         for (int k = h; k < h + 4; ++k) {
-          // (past the row's end dy is 0, and 0 times whatever x's zeros became is added: 0 as mu is finite,
-          // else this row's sums are NaN all the same)
-          xh[i][k] = (xh[i][k] - mu) * rstd;
+          // (past the row's end dy is 0, but (0 - mu) rstd may be past fp32's range, and 0 times that is NaN)
+          xh[i][k] = c * V + k < W ? (xh[i][k] - mu) * rstd : 0.f;
           sg[i][k] += g[i][k] * xh[i][k];
           sb[i][k] += g[i][k];
           g[i][k] *= w[k - h];

@@ -119,3 +119,22 @@ def test_beam_of_far_logits_in_chunks(V, dtype):
 @pytest.mark.parametrize("B,V", [(4, 5003), (4, 9000), (160, 33000)])
 def test_beam_of_far_logits_in_rows(B, V, dtype):
     _beam_of_far_logits(V, B, dtype)
+
+
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 7, 33, 100, 200, 257, 515, 1030])
+def test_norm_backward_of_rows_far_from_zero(width):
+    """Rows of one large value: no deviation, so xh is 0 and dx = rstd (g - mean g), whatever mean times rstd would be."""
+    hd = _hd()
+    rng = rng_for("far rows", width)
+    rows, eps = 300, 1e-12
+    x = np.tile(2.0 ** 113 * rng.choice([-1.0, 1.0], (rows, 1)), (1, width))
+    dy = rounded(rng.standard_normal((rows, width)), "f32")
+    r = hd.NormRun.of(up(x, "f32"), up(np.ones(width), "f32"), up(np.zeros(width), "f32"), dy=up(dy, "f32"), eps=eps)
+    assert not get(r.forward()).any()
+    r.backward()
+    rstd = get(r.rstd)
+    assert np.array_equal(get(r.mean), x[:, 0])
+    want, _, db = ref.norm_bwd(x, x[:, 0], rstd, None, dy, None)
+    close(r.dx, want, "f32", "dx", extra=1e-6 * (rstd * np.abs(dy).max())[:, None])
+    assert not get(r.dgamma).any()
+    close(r.dbeta, db, "f32", "dbeta")
