@@ -44,12 +44,11 @@ template <int N>
 __device__ __forceinline__ RowTargets row_targets(const DistillArgs& a, int64_t row, bool here, int t, int* idx, float* p,
                                                   float* red) {
   float top = -INFINITY;
-  const float it = 1.f / a.tau;
   for (int j = t; j < a.K; j += N) {
     int i = here ? a.index[row * a.K + j] : -1;
     const float w = here ? a.value[row * a.K + j] : 0.f;           // (with the index, not behind it)
     if (i < 0 || i >= a.V) i = -1;
-    const float v = i >= 0 ? w * it : -INFINITY;
+    const float v = i >= 0 ? w : -INFINITY;
     idx[j] = i;
     p[j] = v;
     top = (v > top || v != v) ? v : top;               // (a NaN stays: the row's loss is NaN)
@@ -60,7 +59,8 @@ __device__ __forceinline__ RowTargets row_targets(const DistillArgs& a, int64_t 
   for (int j = t; j < a.K; j += N) {
     const float v = p[j];
     if (idx[j] >= 0 && (top > -INFINITY || v != v)) {
-      const float e = __expf(v - top);
+      // (the difference first: values of the type's lowest are alike, over whatever tau)
+      const float e = expf((v - top) / a.tau);
       p[j] = e;
       s += e;
     } else {

@@ -138,3 +138,26 @@ def test_norm_backward_of_rows_far_from_zero(width):
     close(r.dx, want, "f32", "dx", extra=1e-6 * (rstd * np.abs(dy).max())[:, None])
     assert not get(r.dgamma).any()
     close(r.dbeta, db, "f32", "dbeta")
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.5, 1e-3])
+@pytest.mark.parametrize("V", [90, 40000])
+def test_teacher_values_at_the_ends_of_the_range(V, tau):
+    """p depends on the values' differences: all entries at the lowest value are alike, one of the largest is alone."""
+    hd = _hd()
+    rng = rng_for("teacher", V, tau)
+    top = -LOWEST
+    value = np.array([[LOWEST] * 4, [top] * 4, [top, LOWEST, 0, 1e37], [LOWEST, LOWEST, -np.inf, LOWEST], [3e36, 3e36, 1, 2],
+                      [0, -1e30, -1e35, LOWEST]], np.float32)
+    R, K = value.shape
+    x = rounded(rng.standard_normal((R, V)), "f32")
+    index = np.tile(np.array([0, 5, V - 2, 7], np.int32), (R, 1))
+    grad = np.ones(R, np.float32)
+    tau = float(np.float32(tau))
+    r = hd.DistillRun.of(up(x, "f32"), up(index), up(value), None, up(grad), tau, 1.0)
+    r.step()
+    v = value.astype(np.float64)
+    loss, d = ref.distill(x, index, v, None, grad.astype(np.float64), tau, 1.0)
+    assert (loss != 0).all()
+    close(r.loss, loss, "f32", "loss")
+    close(r.dlogits, d, "f32", "dlogits")
