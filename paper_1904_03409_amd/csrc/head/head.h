@@ -236,4 +236,14 @@ struct Expo {
 // Host side: a row stride as given (0: dense), and whether one may be.
 static inline int64_t row_stride(int64_t ld, int64_t width) { return ld ? ld : width; }
 static inline bool stride_ok(int64_t ld, int64_t width) { return ld == 0 || (ld >= width && ld <= ((int64_t)1 << 40)); }
+// Workgroups of a launch at most: HIP refuses a grid of 2^32 threads and more, and a workgroup here has up to 1024. Calls with more
+// are cut into several launches, of whole rows (or searches) that need nothing of each other.
+constexpr int64_t kMostGroups = 1 << 21;
+// f(first, n) for pieces of `all` that are `most` long.
+template <typename F>
+static inline void in_pieces(int64_t all, int64_t most, F f) {
+  for (int64_t i = 0; i < all; i += most) f(i, all - i < most ? all - i : most);
+}
+template <typename T>
+static inline T* offset(T* p, int64_t n) { return p ? p + n : nullptr; }
 static inline hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }

@@ -350,10 +350,17 @@ extern "C" int stacklstm_norm_fwd(const slstm_norm_dims* d, const void* x, const
   a.x = x, a.res = res, a.gamma = gamma, a.beta = beta, a.sum = sum, a.y = y, a.mean = mean, a.rstd = rstd;
   a.ldx = row_stride(d->ld_x, d->width), a.ldr = row_stride(d->ld_res, d->width);
   const bool ok = norm_dispatch(d, [&](auto t, auto tpr, auto nv) {
-    constexpr int TPR = decltype(tpr)::value;
-    const int64_t blocks = (d->rows + norm_rows(TPR) - 1) / norm_rows(TPR);
-    hipLaunchKernelGGL((k_norm_fwd<decltype(t), TPR, decltype(nv)::value>), dim3((unsigned)blocks), dim3(norm_threads(TPR)), 0,
-                       as_stream(stream), a);
+    typedef decltype(t) T;
+    constexpr int TPR = decltype(tpr)::value, RPB = norm_rows(TPR);
+    in_pieces(d->rows, kMostGroups * RPB, [&](int64_t r0, int64_t n) {
+      NormArgs p = a;
+      p.rows = (int)n;
+      p.x = offset((const T*)x, r0 * a.ldx), p.res = offset((const T*)res, r0 * a.ldr);
+      p.sum = offset((T*)sum, r0 * a.W), p.y = offset((T*)y, r0 * a.W);
+      p.mean = offset(mean, r0), p.rstd = offset(rstd, r0);
+      hipLaunchKernelGGL((k_norm_fwd<T, TPR, decltype(nv)::value>), dim3((unsigned)((n + RPB - 1) / RPB)), dim3(norm_threads(TPR)),
+                         0, as_stream(stream), p);
+    });
   });
   if (!ok) return SLSTM_EINVAL;
   return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
