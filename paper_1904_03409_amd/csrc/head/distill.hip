@@ -413,8 +413,7 @@ int distill_chunks(const slstm_distill_dims* d) { return (distill_vecs(d) + kChu
 bool distill_ok(const slstm_distill_dims* d) {
   return d && d->rows >= 0 && d->rows <= 0x7fffffff && d->V >= 1 && d->V <= (1 << 22) && d->K >= 1 && d->K <= kEntries &&
          (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->tau >= 1e-6f && d->tau <= 1e6f && d->alpha >= 0.f &&
-         d->alpha <= 1.f && stride_ok(d->ld_logits, d->V) && stride_ok(d->ld_dlogits, d->V) &&
-         d->rows * distill_chunks(d) <= 0x7fffffff;
+         d->alpha <= 1.f && stride_ok(d->ld_logits, d->V) && stride_ok(d->ld_dlogits, d->V);
 }
 // Whole rows in registers hold up to 8192 vectors; rows of four chunks or more are cut where there are not two
 // of them for every compute unit.
@@ -448,25 +447,45 @@ int distill_run(const slstm_distill_dims* d, DistillArgs a, void* workspace, siz
   a.ldx = row_stride(d->ld_logits, d->V), a.ldd = row_stride(d->ld_dlogits, d->V);
   a.chunks = distill_chunks(d);
   if (a.dx == a.x && a.ldx != a.ldd) return SLSTM_EINVAL;
-  if (!distill_cut(d)) {
+  const bool cut = distill_cut(d);
+  if (cut && !a.stats_in) {
+    if (!workspace || ((uintptr_t)workspace & 3u)) return SLSTM_EINVAL;
+    if (ws_bytes < stacklstm_distill_workspace_bytes(d)) return SLSTM_EWORKSPACE;
+    a.part = (float*)workspace;
+    a.ent = (float*)((char*)workspace + distill_part_bytes(d));
+  }
+  // rows r0 .. r0 + n
+  auto rows = [&](auto t, int64_t r0, int64_t n) {
+    typedef decltype(t) T;
+    DistillArgs p = a;
+    p.rows = (int)n;
+    p.x = offset((const T*)a.x, r0 * a.ldx), p.dx = offset((T*)a.dx, r0 * a.ldd);
+    p.index = a.index + r0 * a.K, p.value = a.value + r0 * a.K, p.label = offset(a.label, r0);
+    p.grad = offset(a.grad, r0), p.stats_in = offset(a.stats_in, r0 * 3);
+    p.loss = offset(a.loss, r0), p.stats = offset(a.stats, r0 * 3);
+    p.part = offset(a.part, r0 * a.chunks * 3), p.ent = offset(a.ent, r0 * (a.K + 1));
+    return p;
+  };
+  if (!cut) {
     distill_dispatch(d, [&](auto t, auto tpr, auto nv) {
       constexpr int TPR = decltype(tpr)::value, RPB = distill_rows(TPR);
-      hipLaunchKernelGGL((k_distill_rows<decltype(t), TPR, decltype(nv)::value>), dim3((unsigned)((d->rows + RPB - 1) / RPB)),
-                         dim3(distill_threads(TPR)), (size_t)RPB * 3 * (d->K + 1) * 4, st, a);
+      in_pieces(d->rows, kMostGroups * RPB, [&](int64_t r0, int64_t n) {
+        hipLaunchKernelGGL((k_distill_rows<decltype(t), TPR, decltype(nv)::value>), dim3((unsigned)((n + RPB - 1) / RPB)),
+                           dim3(distill_threads(TPR)), (size_t)RPB * 3 * (d->K + 1) * 4, st, rows(t, r0, n));
+      });
     });
   } else {
-    const dim3 all((unsigned)(d->rows * a.chunks));
-    if (!a.stats_in) {
-      if (!workspace || ((uintptr_t)workspace & 3u)) return SLSTM_EINVAL;
-      if (ws_bytes < stacklstm_distill_workspace_bytes(d)) return SLSTM_EWORKSPACE;
-      a.part = (float*)workspace;
-      a.ent = (float*)((char*)workspace + distill_part_bytes(d));
-      if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_distill_part<float>, all, dim3(256), 0, st, a);
-      else hipLaunchKernelGGL(k_distill_part<bf16_t>, all, dim3(256), 0, st, a);
-    }
-    const dim3 grid = a.dx ? all : dim3((unsigned)d->rows);
-    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_distill_chunk<float>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_distill_chunk<bf16_t>, grid, dim3(256), 0, st, a);
+    auto run = [&](auto t) {
+      typedef decltype(t) T;
+      in_pieces(d->rows, kMostGroups / a.chunks, [&](int64_t r0, int64_t n) {
+        const dim3 all((unsigned)(n * a.chunks));
+        const DistillArgs p = rows(t, r0, n);
+        if (!a.stats_in) hipLaunchKernelGGL(k_distill_part<T>, all, dim3(256), 0, st, p);
+        hipLaunchKernelGGL(k_distill_chunk<T>, a.dx ? all : dim3((unsigned)n), dim3(256), 0, st, p);
+      });
+    };
+    if (d->type == SLSTM_F32) run(float());
+    else run(bf16_t());
   }
   return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }

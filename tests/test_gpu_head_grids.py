@@ -27,3 +27,44 @@ def test_norm_of_many_narrow_rows():
     hd.stacklstm_norm_fwd(hd.make_norm_dims(R, 1), x, None, None, None, None, y, mean, rstd)
     assert torch.equal(mean, x[:, 0]) and not y.any()
     assert rstd.min() == rstd.max()
+
+
+def test_distill_of_many_narrow_rows():
+    hd = _hd()
+    R, V = (1 << 29) + 70, 2
+    x = torch.arange(R * V, device="cuda", dtype=torch.int32).remainder_(61).to(torch.bfloat16).view(R, V)
+    index = torch.full((R, 1), -1, dtype=torch.int32, device="cuda")
+    value, label = torch.zeros(R, 1, device="cuda"), torch.zeros(R, dtype=torch.int32, device="cuda")
+    loss = torch.full((R,), 7e9, device="cuda")
+    d = torch.full((R, V), 7.0, dtype=torch.bfloat16, device="cuda")
+    dims = hd.make_distill_dims(R, V, 1, hd.SLSTM_BF16, 1.0, 0.0)
+    ws = torch.empty(hd.stacklstm_distill_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+    hd.stacklstm_distill_step(dims, x, index, value, label, None, loss, d, ws)
+    worst, off = 0.0, 0.0
+    for lo in range(0, R, 1 << 26):                      # log(1 + exp(x1 - x0)) and its derivative, a piece at a time
+        p = x[lo:lo + (1 << 26)].float()
+        gap = p[:, 1] - p[:, 0]
+        worst = max(worst, float((loss[lo:lo + (1 << 26)] - torch.logaddexp(gap, torch.zeros_like(gap))).abs().max()))
+        off = max(off, float((d[lo:lo + (1 << 26), 1].float() - torch.sigmoid(gap)).abs().max()))
+    assert worst < 60 * 1e-5 and off < 2.0 ** -8
+
+
+def test_distill_of_many_long_rows():
+    """Rows in chunks, in place: every row is one base row, shifted."""
+    hd = _hd()
+    R, V = 233100, 32772
+    base = torch.randn(V, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    x = base + torch.arange(R, device="cuda").remainder_(4).float()[:, None]
+    label = torch.arange(R, device="cuda", dtype=torch.int32).remainder_(V)
+    index, value = torch.full((R, 1), -1, dtype=torch.int32, device="cuda"), torch.zeros(R, 1, device="cuda")
+    loss = torch.full((R,), 7e9, device="cuda")
+    dims = hd.make_distill_dims(R, V, 1, hd.SLSTM_F32, 1.0, 0.0)
+    ws = torch.empty(hd.stacklstm_distill_workspace_bytes(dims), dtype=torch.uint8, device="cuda")
+    hd.stacklstm_distill_step(dims, x, index, value, label, None, loss, x, ws)
+    want = torch.logsumexp(base.double(), 0) - base.double()
+    assert float((loss - want[label.long()]).abs().max()) < 1e-5 * float(want.max())
+    q = torch.softmax(base.double(), 0)
+    for lo in (0, 116500, 232950, R - 90):
+        d = q.repeat(90, 1)
+        d[torch.arange(90, device="cuda"), label[lo:lo + 90].long()] -= 1
+        assert float((x[lo:lo + 90] - d).abs().max()) < 1e-5
