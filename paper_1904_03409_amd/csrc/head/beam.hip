@@ -505,7 +505,7 @@ int beam_chunks(const slstm_beam_dims* d) { return (beam_vecs(d) + 256 * kPartVe
 bool beam_ok(const slstm_beam_dims* d) {
   return d && d->B >= 0 && d->K >= 1 && d->K <= kMaxBeams && d->V >= 1 && d->V <= (1 << 22) &&
          (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && d->eos >= -1 && stride_ok(d->ld_logits, d->V) &&
-         (int64_t)d->B * d->K * beam_chunks(d) <= 0x7fffffff;
+         (int64_t)d->B * d->K <= 0x7fffffff;
 }
 // (a wave goes through its row 64 tokens at a time: one of 7360 took 20 us)
 bool beam_small(const slstm_beam_dims* d) { return (int64_t)d->K * d->V <= kSmall && d->V <= 2048; }
@@ -517,10 +517,9 @@ bool beam_cut(const slstm_beam_dims* d) {
 size_t beam_part_bytes(const slstm_beam_dims* d) { return ((size_t)d->B * d->K * beam_chunks(d) * 8 + 255) & ~(size_t)255; }
 
 template <typename T>
-void beam_rows(const slstm_beam_dims* d, const BeamArgs& a, hipStream_t st) {
-  const unsigned rows = (unsigned)((int64_t)d->B * d->K);
+void beam_rows(const slstm_beam_dims* d, const BeamArgs& a, unsigned rows, bool cut, hipStream_t st) {
   const int n = beam_vecs(d);
-  if (beam_cut(d)) {
+  if (cut) {
     hipLaunchKernelGGL(k_beam_part<T>, dim3(rows * a.chunks), dim3(256), 0, st, a);
     hipLaunchKernelGGL((k_beam_rows<T, 256, kPartVecs, true>), dim3(rows * a.chunks), dim3(256), 0, st, a);
   } else if (n <= 1024) {
@@ -554,20 +553,34 @@ extern "C" int stacklstm_beam_select(const slstm_beam_dims* d, const void* logit
   a.x = logits, a.ldx = row_stride(d->ld_logits, d->V), a.legal = legal, a.done = done, a.score = score;
   a.score_next = score_next, a.parent = parent, a.token = token, a.done_next = done_next;
   const hipStream_t st = as_stream(stream);
-  if (beam_small(d)) {
-    if (d->type == SLSTM_F32) hipLaunchKernelGGL(k_beam_small<float>, dim3(d->B), dim3(512), 0, st, a);
-    else hipLaunchKernelGGL(k_beam_small<bf16_t>, dim3(d->B), dim3(512), 0, st, a);
-  } else {
+  const bool small = beam_small(d), cut = !small && beam_cut(d);
+  if (!small) {
     if (!workspace || ((uintptr_t)workspace & 7u)) return SLSTM_EINVAL;
     if (ws_bytes < stacklstm_beam_workspace_bytes(d)) return SLSTM_EWORKSPACE;
-    const bool cut = beam_cut(d);
     a.chunks = cut ? beam_chunks(d) : 1;
     a.part = (float*)workspace;
     a.cand = (u64*)((char*)workspace + (cut ? beam_part_bytes(d) : 0));
-    if (d->type == SLSTM_F32) beam_rows<float>(d, a, st);
-    else beam_rows<bf16_t>(d, a, st);
-    hipLaunchKernelGGL(k_beam_merge, dim3(d->B), dim3(256), 0, st, a);
   }
+  auto run = [&](auto t) {
+    typedef decltype(t) T;
+    // (at most 64 beams of 1024 chunks)
+    in_pieces(d->B, small ? kMostGroups : kMostGroups / (a.K * a.chunks), [&](int64_t b0, int64_t n) {
+      const int64_t r0 = b0 * a.K, r = n * a.K;
+      BeamArgs p = a;
+      p.B = (int)n;
+      p.x = offset((const T*)logits, r0 * a.ldx), p.legal = offset(legal, r0 * a.V), p.score = score + r0, p.done = offset(done, r0);
+      p.part = offset(a.part, r0 * a.chunks * 2), p.cand = offset(a.cand, r0 * a.chunks * a.K);
+      p.score_next = score_next + r0, p.parent = parent + r0, p.token = token + r0, p.done_next = done_next + r0;
+      if (small) {
+        hipLaunchKernelGGL(k_beam_small<T>, dim3((unsigned)n), dim3(512), 0, st, p);
+      } else {
+        beam_rows<T>(d, p, (unsigned)r, cut, st);
+        hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)n), dim3(256), 0, st, p);
+      }
+    });
+  };
+  if (d->type == SLSTM_F32) run(float());
+  else run(bf16_t());
   return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }
 

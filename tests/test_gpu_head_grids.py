@@ -68,3 +68,39 @@ def test_distill_of_many_long_rows():
         d = q.repeat(90, 1)
         d[torch.arange(90, device="cuda"), label[lo:lo + 90].long()] -= 1
         assert float((x[lo:lo + 90] - d).abs().max()) < 1e-5
+
+
+def test_beam_of_many_searches():
+    hd = _hd()
+    B, V = (1 << 23) + 9, 3
+    x = torch.arange(B * V, device="cuda", dtype=torch.int32).remainder_(1009).float().view(B, V)
+    r = hd.BeamRun.of(x, torch.zeros(B, 1, device="cuda"))
+    r.parent.fill_(7), r.token.fill_(7), r.score_next.fill_(7)
+    r.select()
+    assert torch.equal(r.token[:, 0], x.argmax(1).int()) and not r.parent.any()
+    for lo in (0, 1 << 21, (1 << 22) - 500, B - 1000):  # searches need nothing of each other: fewer of them give the same bits
+        few = hd.BeamRun.of(x[lo:lo + 1000], torch.zeros(1000, 1, device="cuda"))
+        few.select()
+        assert torch.equal(r.score_next[lo:lo + 1000], few.score_next)
+
+
+def test_beam_of_many_rows():
+    hd = _hd()
+    K, V = 64, 129
+    B = (1 << 18) + 3
+    # beams further down score less, and a row's best token is its own number: search b goes on with beam 0's best tokens
+    row = torch.arange(B * K, device="cuda", dtype=torch.int32)
+    x = torch.zeros(B * K, V, dtype=torch.bfloat16, device="cuda")
+    at = (row % V).long()
+    for lo in range(0, B * K, 1 << 22):
+        x[torch.arange(lo, min(B * K, lo + (1 << 22)), device="cuda"), at[lo:lo + (1 << 22)]] = 50.0
+    score = (-100.0 * torch.arange(K, device="cuda", dtype=torch.float32)).repeat(B, 1)
+    r = hd.BeamRun.of(x, score)
+    r.parent.fill_(7), r.token.fill_(7), r.score_next.fill_(7)
+    r.select()
+    best = at.view(B, K)[:, 0].int()
+    assert not r.parent.any() and torch.equal(r.token[:, 0], best)
+    # then the lowest tokens but that one
+    lowest = torch.arange(K - 1, device="cuda", dtype=torch.int32).repeat(B, 1)
+    assert torch.equal(r.token[:, 1:], lowest + (lowest >= best[:, None]).int())
+    assert float(r.score_next[:, 0].abs().max()) < 1e-5
