@@ -533,6 +533,10 @@ void beam_rows(const slstm_beam_dims* d, const BeamArgs& a, unsigned rows, bool 
   }
 }
 
+// Workgroups of a state's copy, and of a launch at most (of 256 threads).
+int64_t reorder_groups(const CopyState& c, int64_t rows) { return c.pieces ? c.pieces * rows : (rows + 15) / 16; }
+constexpr int64_t kMostReorder = 4 * kMostGroups;
+
 }  // namespace
 
 extern "C" size_t stacklstm_beam_workspace_bytes(const slstm_beam_dims* d) {
@@ -590,8 +594,9 @@ extern "C" int stacklstm_beam_reorder(const slstm_beam_dims* d, const int32_t* p
   if (count < 0 || count > SLSTM_BEAM_MAX_STATES) return SLSTM_EINVAL;
   if (count == 0 || d->B == 0) return SLSTM_OK;
   if (!parent || !states) return SLSTM_EINVAL;
+  const int64_t rows = (int64_t)d->B * d->K;
   ReorderArgs a = {};
-  a.K = d->K, a.count = count, a.rows = (int64_t)d->B * d->K, a.parent = parent;
+  a.K = d->K, a.count = count, a.rows = rows, a.parent = parent;
   int64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
     const slstm_beam_state& s = states[i];
@@ -602,23 +607,37 @@ extern "C" int stacklstm_beam_reorder(const slstm_beam_dims* d, const int32_t* p
     // nothing is read from where a state is written
     auto meets = [&](const void* p, int64_t bytes) {
       const char* s0 = (const char*)p;
-      return p && d0 < s0 + bytes && s0 < d0 + pitch * a.rows;
+      return p && d0 < s0 + bytes && s0 < d0 + pitch * rows;
     };
-    if (meets(parent, a.rows * 4)) return SLSTM_EINVAL;
+    if (meets(parent, rows * 4)) return SLSTM_EINVAL;
     for (int j = 0; j < count; ++j) {
       const slstm_beam_state& o = states[j];
       if (o.slots < 1 || o.slot_bytes < 1 || o.slot_bytes > kMostBytes / o.slots) return SLSTM_EINVAL;
-      if (meets(o.src, o.slot_bytes * o.slots * a.rows) || meets(o.live, a.rows * 4)) return SLSTM_EINVAL;
+      if (meets(o.src, o.slot_bytes * o.slots * rows) || meets(o.live, rows * 4)) return SLSTM_EINVAL;
     }
     CopyState& c = a.st[i];
     c.src = (const char*)s.src, c.dst = (char*)s.dst, c.live = s.live, c.slot_bytes = s.slot_bytes, c.slots = s.slots;
-    const int64_t pieces = pitch <= kShort ? 0 : (pitch + kPiece - 1) / kPiece;
-    const int64_t n = pieces ? pieces * a.rows : (a.rows + 15) / 16;
-    if (pieces > 0x7fffffff || blocks + n > 0x7fffffff) return SLSTM_EINVAL;
-    c.pieces = (int32_t)pieces;
-    c.first = (uint32_t)blocks;
-    blocks += n;
+    c.pieces = pitch <= kShort ? 0 : (int32_t)((pitch + kPiece - 1) / kPiece);
+    c.first = (uint32_t)blocks;                        // (of a call of one launch)
+    blocks += reorder_groups(c, rows);
   }
-  hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), a);
+  const hipStream_t st = as_stream(stream);
+  if (blocks <= kMostReorder) {
+    hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  } else {
+    // state by state, as many searches as one launch takes (one search of one state has up to 64 rows of 2^17 pieces)
+    for (int i = 0; i < count; ++i) {
+      const CopyState& c = a.st[i];
+      const int64_t pitch = c.slot_bytes * c.slots;
+      in_pieces(d->B, std::max<int64_t>(1, kMostReorder / (std::max(c.pieces, 1) * (int64_t)d->K)), [&](int64_t b0, int64_t n) {
+        const int64_t r0 = b0 * d->K;
+        ReorderArgs p = a;
+        p.count = 1, p.rows = n * d->K, p.parent = parent + r0;
+        p.st[0] = c;
+        p.st[0].src = c.src + r0 * pitch, p.st[0].dst = c.dst + r0 * pitch, p.st[0].live = offset(c.live, r0), p.st[0].first = 0;
+        hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)reorder_groups(c, p.rows)), dim3(256), 0, st, p);
+      });
+    }
+  }
   return hipGetLastError() == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
 }

@@ -104,3 +104,21 @@ def test_beam_of_many_rows():
     lowest = torch.arange(K - 1, device="cuda", dtype=torch.int32).repeat(B, 1)
     assert torch.equal(r.token[:, 1:], lowest + (lowest >= best[:, None]).int())
     assert float(r.score_next[:, 0].abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("width", [1, 300])
+def test_reorder_of_many_rows(width):
+    hd = _hd()
+    K = 64
+    B = ((1 << 28) + (1 << 8)) // K if width == 1 else ((1 << 24) + (1 << 8)) // K
+    n = B * K
+    src = torch.arange(n, device="cuda", dtype=torch.int32).remainder_(251).to(torch.uint8)[:, None]
+    src = src + torch.arange(width, device="cuda").to(torch.uint8)
+    dst = torch.full_like(src, 255)
+    parent = torch.arange(n, device="cuda", dtype=torch.int32).mul_(7).add_(5).remainder_(K).view(B, K)
+    other, copy = torch.arange(n, device="cuda", dtype=torch.int32), torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    hd.stacklstm_beam_reorder(hd.make_beam_dims(B, K, 1), parent, [(src, dst, None), (other, copy, None)])
+    frm = parent.view(-1) + torch.arange(B, device="cuda", dtype=torch.int32).mul_(K).repeat_interleave(K)
+    assert torch.equal(copy, frm)
+    for lo in range(0, n, 1 << 24):
+        assert torch.equal(dst[lo:lo + (1 << 24)], src[frm[lo:lo + (1 << 24)].long()])
