@@ -828,28 +828,40 @@ hipError_t allow_lds(const void* kern, int lds, std::atomic<uint64_t>& devices) 
   if (s == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
   return s;
 }
+// T the operands' type, AT: whether A has k as the row. Products with more tiles than a launch may have workgroups are not split
+// over k; they go out in several launches of whole rows of tiles.
+template <typename T, bool AT>
 hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int threads, int lds, std::atomic<uint64_t>& devices, hipStream_t st) {
   if (lds > 65536) {
     const hipError_t e = allow_lds(kern, lds, devices);
     if (e != hipSuccess) return e;
   }
-  const int64_t tiles = (((int64_t)g.M + tile - 1) / tile) * (((int64_t)g.N + tile - 1) / tile) * g.splits;
-  GemmArgs a = g;
-  a.tiles = (int)tiles;
-  void* args[] = {&a};
-  return hipLaunchKernel(kern, dim3((unsigned)(tiles + (g.dbpart ? (g.N + 31) / 32 : 0))), dim3(threads), args, lds, st);
+  const int64_t across = ((int64_t)g.N + tile - 1) / tile * g.splits;
+  hipError_t e = hipSuccess;
+  in_pieces(g.M, tile * std::max<int64_t>(1, kMostGroups / across), [&](int64_t m0, int64_t m) {
+    GemmArgs a = g;
+    a.M = (int)m;
+    a.tiles = (int)((m + tile - 1) / tile * across);
+    a.A = (const T*)g.A + (AT ? m0 : m0 * g.lda);
+    a.y = offset((T*)g.y, m0 * g.ldy), a.z = offset((T*)g.z, m0 * g.N), a.res = offset((const T*)g.res, m0 * g.ldr);
+    if (m0) a.dbpart = nullptr;
+    void* args[] = {&a};
+    if (e == hipSuccess)
+      e = hipLaunchKernel(kern, dim3((unsigned)(a.tiles + (a.dbpart ? (g.N + 31) / 32 : 0))), dim3(threads), args, lds, st);
+  });
+  return e;
 }
 template <typename T, bool AT, bool BT, int TILE, int SA, int SB>
 hipError_t launch_dma(const GemmArgs& g, hipStream_t st) {
   typedef Tile<T, TILE, TILE> S;
   static std::atomic<uint64_t> devices;
-  return tile_launch((const void*)k_linear<T, AT, BT, TILE, TILE, SA, SB>, g, TILE, S::NT, S::ABYTES * SA + S::BBYTES * SB, devices, st);
+  return tile_launch<T, AT>((const void*)k_linear<T, AT, BT, TILE, TILE, SA, SB>, g, TILE, S::NT, S::ABYTES * SA + S::BBYTES * SB, devices, st);
 }
 template <typename T, bool AT, bool BT, int TILE>
 hipError_t launch_any(const GemmArgs& g, hipStream_t st) {
   typedef Tile<T, TILE, TILE> S;
   static std::atomic<uint64_t> devices;
-  return tile_launch((const void*)k_linear_any<T, AT, BT, TILE, TILE>, g, TILE, S::NT, (S::ABYTES + S::BBYTES) * 2, devices, st);
+  return tile_launch<T, AT>((const void*)k_linear_any<T, AT, BT, TILE, TILE>, g, TILE, S::NT, (S::ABYTES + S::BBYTES) * 2, devices, st);
 }
 
 // A matrix of rows as a product reads it. whole: its rows are whole granules at aligned places, in reach of a

@@ -122,3 +122,41 @@ def test_reorder_of_many_rows(width):
     assert torch.equal(copy, frm)
     for lo in range(0, n, 1 << 24):
         assert torch.equal(dst[lo:lo + (1 << 24)], src[frm[lo:lo + (1 << 24)].long()])
+
+
+@pytest.mark.parametrize("N", [1, 2])
+def test_linear_of_many_rows(N):
+    """2^24 tiles of one column, odd rows (copied) and whole ones."""
+    hd = _hd()
+    M, K = 1 << 30, 1 if N == 1 else 8
+    x = torch.arange(M, device="cuda", dtype=torch.int32).remainder_(253).to(torch.bfloat16)[:, None]
+    if K > 1:
+        x = x.repeat(1, K)
+    W = torch.zeros(K, N, dtype=torch.bfloat16, device="cuda")
+    W[0] = 1.0
+    y = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    d = hd.make_linear_dims(M, K, N, hd.SLSTM_BF16)
+    ws = torch.empty(hd.stacklstm_linear_fwd_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    hd.stacklstm_linear_fwd(d, x, W, None, None, y, None, ws)
+    assert all(torch.equal(y[:, n], x[:, 0]) for n in range(N))
+    if N == 1:
+        dx = torch.full((M, K), 7.0, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(hd.stacklstm_linear_bwd_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+        hd.stacklstm_linear_bwd(d, x, W, None, x, dx, None, None, ws)
+        assert torch.equal(dx, x)
+
+
+@pytest.mark.parametrize("M,N", [(130, 520), (130, 513), (3, 515)])
+def test_linear_weight_gradient_of_many_inputs(M, N):
+    """More tiles of dW than a launch has, sums of db beside them; one row of x and dy is not zero."""
+    hd = _hd()
+    K, r = 1 << 24, M // 2
+    x, dy = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda"), torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    x[r] = torch.arange(K, device="cuda", dtype=torch.int32).remainder_(13).to(torch.bfloat16)
+    dy[r] = torch.arange(N, device="cuda").remainder_(11).to(torch.bfloat16)
+    d = hd.make_linear_dims(M, K, N, hd.SLSTM_BF16)
+    ws = torch.empty(hd.stacklstm_linear_bwd_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    dW, db = torch.full((K, N), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((N,), 7.0, dtype=torch.bfloat16, device="cuda")
+    hd.stacklstm_linear_bwd(d, x, None, None, dy, None, dW, db, ws)
+    assert torch.equal(db, dy[r])
+    assert torch.equal(dW, x[r][:, None] * dy[r])        # whole numbers up to 120
