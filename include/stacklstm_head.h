@@ -169,7 +169,7 @@ int stacklstm_beam_select(const slstm_beam_dims* d, const void* logits, const ui
 /* One array of per-beam state: [B K] rows of `slots` slots of slot_bytes bytes. */
 typedef struct {
   const void* src;
-  void* dst;               /* must not overlap any src or live of the call, nor parent (SLSTM_EINVAL) */
+  void* dst;               /* must not overlap any src, live or other dst of the call, nor parent (SLSTM_EINVAL) */
   int64_t slot_bytes;      /* >= 1; slots * slot_bytes <= 2^31 */
   int32_t slots;           /* >= 1; a stack of T + 1 states, or 1 */
   int32_t reserved;        /* 0 */

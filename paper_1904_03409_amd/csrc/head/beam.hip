@@ -604,7 +604,7 @@ extern "C" int stacklstm_beam_reorder(const slstm_beam_dims* d, const int32_t* p
       return SLSTM_EINVAL;
     const int64_t pitch = s.slot_bytes * s.slots;
     const char* d0 = (const char*)s.dst;
-    // nothing is read from where a state is written
+    // nothing is read from where a state is written, and no other state is written there
     auto meets = [&](const void* p, int64_t bytes) {
       const char* s0 = (const char*)p;
       return p && d0 < s0 + bytes && s0 < d0 + pitch * rows;
@@ -614,6 +614,7 @@ extern "C" int stacklstm_beam_reorder(const slstm_beam_dims* d, const int32_t* p
       const slstm_beam_state& o = states[j];
       if (o.slots < 1 || o.slot_bytes < 1 || o.slot_bytes > kMostBytes / o.slots) return SLSTM_EINVAL;
       if (meets(o.src, o.slot_bytes * o.slots * rows) || meets(o.live, rows * 4)) return SLSTM_EINVAL;
+      if (j != i && meets(o.dst, o.slot_bytes * o.slots * rows)) return SLSTM_EINVAL;
     }
     CopyState& c = a.st[i];
     c.src = (const char*)s.src, c.dst = (char*)s.dst, c.live = s.live, c.slot_bytes = s.slot_bytes, c.slots = s.slots;
