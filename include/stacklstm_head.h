@@ -73,11 +73,16 @@ typedef enum {
   SLSTM_ACT_GELU = 4       /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
 } slstm_act;
 
+/* Beside an slstm_act: with SLSTM_BF16 the backward's products take dz with 16 significant bits instead of 8, as two
+ * bfloat16 matrices with a product each, summed in 32 bits before the one rounding. Twice the products' time. The forward,
+ * SLSTM_F32 and SLSTM_ACT_NONE (dz is dy) have nothing to do with it. */
+#define SLSTM_LINEAR_WIDE_DZ 0x100
+
 typedef struct {
   int64_t M;               /* rows, 0 .. 2^30 */
   int32_t K, N;            /* inputs and outputs, 1 .. 2^24 */
   int32_t type;            /* slstm_type of every array */
-  int32_t act;             /* slstm_act */
+  int32_t act;             /* slstm_act, or that and SLSTM_LINEAR_WIDE_DZ */
   int64_t ld_x, ld_w, ld_res, ld_y, ld_dy;
 } slstm_linear_dims;
 
@@ -97,7 +102,7 @@ int stacklstm_linear_fwd(const slstm_linear_dims* d, const void* x, const void* 
  *  dy [M, N]                                                                 (read)
  *  dx [M, K], dW [K, N], db [N], each or NULL (dense)                        (written)
  * The gradient of res is dy. With SLSTM_BF16, dz is rounded to bfloat16 for the products of dx and dW (the
- * operands of the matrix units); db sums it unrounded. */
+ * operands of the matrix units), unless SLSTM_LINEAR_WIDE_DZ is asked for; db sums it unrounded. */
 int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, const void* W, const void* z, const void* dy, void* dx,
                          void* dW, void* db, void* workspace, size_t ws_bytes, void* stream);
 

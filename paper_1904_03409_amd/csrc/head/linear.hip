@@ -586,11 +586,11 @@ __global__ void __launch_bounds__((Tile<T, BM, BN>::NT), 2) k_linear_any(GemmArg
 // The parts of a split product, and the epilogue: 64 vectors to a workgroup, each wave adds every fourth part, the first one the
 // waves' sums, always in the same order (dW of 26751 x 176 x 416 bf16: 6.9 us; with all parts added by one wave 18).
 template <typename T>
-__global__ void __launch_bounds__(256) k_linear_join(GemmArgs g) {
+__global__ void __launch_bounds__(256) k_linear_join(GemmArgs g, int64_t first) {
   constexpr int V = vec<T>::N;
   __shared__ float red[3][V][64];
   const int nv = (g.N + V - 1) / V, q = threadIdx.x >> 6, l = threadIdx.x & 63;
-  const int64_t all = (int64_t)g.M * nv, at = (int64_t)blockIdx.x * 64 + l, i = min(at, all - 1), m = i / nv;
+  const int64_t all = (int64_t)g.M * nv, at = first + (int64_t)blockIdx.x * 64 + l, i = min(at, all - 1), m = i / nv;
   const int n = (int)(i - m * nv) * V;
   float b[V], v[V];
   u32x4 res = {0u, 0u, 0u, 0u};
@@ -627,7 +627,7 @@ struct DzArgs {
   int M, N, act, rows;                                 // rows of a workgroup
   const void *dy, *z;
   int64_t ldd, ldz;
-  void* dz;                                            // NULL: dy serves
+  void *dz, *lo;                                       // dz NULL: dy serves; lo: what rounding took off dz, or NULL
   float* part;                                         // [row blocks][N], NULL: no sums, or
   void* db;                                            // one block of rows: the sums themselves
 };
@@ -665,6 +665,13 @@ __device__ __forceinline__ void dz_strip(const DzArgs& a, int bx, int by) {
 #pragma unroll
         for (int k = 0; k < V; ++k) s[k] += d[k];
         if (a.dz) store_vec((T*)a.dz + n * a.ldz, c, (int)a.ldz, d);     // (zeros to the end of the padded row)
+        if (a.lo) {
+          float hi[V];
+          vec<T>::unpack(vec<T>::pack(d), hi);
+#pragma unroll
+          for (int k = 0; k < V; ++k) d[k] = fabsf(hi[k]) < INFINITY ? d[k] - hi[k] : 0.f;
+          store_vec((T*)a.lo + n * a.ldz, c, (int)a.ldz, d);
+        }
       }
     }
   }
@@ -816,6 +823,11 @@ size_t gemm_bytes(int64_t M, int64_t N, int64_t K, int type) {
   const size_t a = part_bytes(gemm_plan(M, N, K, type, false), M, N);
   return type == SLSTM_F32 ? a : std::max(a, part_bytes(gemm_plan(M, N, K, type, true), M, N));
 }
+// The parts of a product with dz in two planes.
+size_t wide_bytes(int64_t M, int64_t N, int64_t K, int type) {
+  const int splits = std::max(gemm_plan(M, N, K, type, false).splits, gemm_plan(M, N, K, type, true).splits);
+  return (size_t)2 * splits * M * N * 4;
+}
 
 // A kernel's LDS limit is raised once to a device, not at every call.
 hipError_t allow_lds(const void* kern, int lds, std::atomic<uint64_t>& devices) {
@@ -844,6 +856,7 @@ hipError_t tile_launch(const void* kern, const GemmArgs& g, int tile, int thread
     a.tiles = (int)((m + tile - 1) / tile * across);
     a.A = (const T*)g.A + (AT ? m0 : m0 * g.lda);
     a.y = offset((T*)g.y, m0 * g.ldy), a.z = offset((T*)g.z, m0 * g.N), a.res = offset((const T*)g.res, m0 * g.ldr);
+    a.part = offset(g.part, m0 * g.N);                 // (of one split, where m0 is not 0)
     if (m0) a.dbpart = nullptr;
     void* args[] = {&a};
     if (e == hipSuccess)
@@ -916,9 +929,11 @@ struct Copies {
 hipError_t join_launch(const GemmArgs& g, int type, hipStream_t st) {
   const int V = granule(type);
   const int64_t n = (int64_t)g.M * ((g.N + V - 1) / V);
-  const dim3 grid((unsigned)((n + 63) / 64));          // (a product that is split has at most 2048 tiles)
-  if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_join<float>, grid, dim3(256), 0, st, g);
-  else hipLaunchKernelGGL(k_linear_join<bf16_t>, grid, dim3(256), 0, st, g);
+  in_pieces(n, 64 * kMostGroups, [&](int64_t first, int64_t m) {
+    const dim3 grid((unsigned)((m + 63) / 64));
+    if (type == SLSTM_F32) hipLaunchKernelGGL(k_linear_join<float>, grid, dim3(256), 0, st, g, first);
+    else hipLaunchKernelGGL(k_linear_join<bf16_t>, grid, dim3(256), 0, st, g, first);
+  });
   return hipGetLastError();
 }
 template <typename T, int TILE, int SA, int SB>
@@ -937,26 +952,43 @@ hipError_t launch_both(GemmArgs x, GemmArgs w, hipStream_t st) {
   return hipLaunchKernel(kern, dim3(x.tiles + w.tiles + (w.dbpart ? (w.N + 31) / 32 : 0)), dim3(S::NT), args, lds, st);
 }
 
+// The tiles of a product by a plan.
+template <bool AT, bool BT>
+hipError_t gemm_tiles(GemmArgs g, const Operand& A, const Operand& B, const Plan& p, int type, hipStream_t st) {
+  g.A = A.p, g.lda = A.ld, g.B = B.p, g.ldb = B.ld, g.splits = p.splits, g.chunk = p.chunk;
+  const bool dma = A.whole && B.whole, big = p.tile == 128;
+  if (type == SLSTM_F32) {
+    if (dma) return big ? launch_dma<float, AT, BT, 128, 3, 2>(g, st) : launch_dma<float, AT, BT, 64, 3, 3>(g, st);
+    return big ? launch_any<float, AT, BT, 128>(g, st) : launch_any<float, AT, BT, 64>(g, st);
+  }
+  if (!dma) return big ? launch_any<bf16_t, AT, BT, 128>(g, st) : launch_any<bf16_t, AT, BT, 64>(g, st);
+  if (p.tile == 256) return launch_dma<bf16_t, AT, BT, 256, 3, 2>(g, st);
+  return big ? launch_dma<bf16_t, AT, BT, 128, 3, 2>(g, st) : launch_dma<bf16_t, AT, BT, 64, 3, 3>(g, st);
+}
 // One product with its epilogue; g has the sizes and the outputs.
 template <bool AT, bool BT>
 hipError_t gemm(GemmArgs g, const Operand& A, const Operand& B, int type, float* part, hipStream_t st) {
-  const bool dma = A.whole && B.whole;
-  g.A = A.p, g.lda = A.ld, g.B = B.p, g.ldb = B.ld;
-  const Plan p = gemm_plan(g.M, g.N, g.K, type, dma);
+  const Plan p = gemm_plan(g.M, g.N, g.K, type, A.whole && B.whole);
+  if (p.splits > 1) g.part = part;
+  const hipError_t e = gemm_tiles<AT, BT>(g, A, B, p, type, st);
   g.splits = p.splits;
-  g.chunk = p.chunk;
-  g.part = p.splits > 1 ? part : nullptr;
-  hipError_t e;
-  const bool big = p.tile == 128;
-  if (type == SLSTM_F32) {
-    if (dma) e = big ? launch_dma<float, AT, BT, 128, 3, 2>(g, st) : launch_dma<float, AT, BT, 64, 3, 3>(g, st);
-    else e = big ? launch_any<float, AT, BT, 128>(g, st) : launch_any<float, AT, BT, 64>(g, st);
-  } else {
-    if (!dma) e = big ? launch_any<bf16_t, AT, BT, 128>(g, st) : launch_any<bf16_t, AT, BT, 64>(g, st);
-    else if (p.tile == 256) e = launch_dma<bf16_t, AT, BT, 256, 3, 2>(g, st);
-    else e = big ? launch_dma<bf16_t, AT, BT, 128, 3, 2>(g, st) : launch_dma<bf16_t, AT, BT, 64, 3, 3>(g, st);
-  }
   return e != hipSuccess || p.splits == 1 ? e : join_launch(g, type, st);
+}
+// The same with dz (A, or with AT B) in two planes, `lo` the second: two products whose parts are added together. 16-bit matrix
+// units take dz with 8 significant bits, as the caller gives dy; that is the choice unless a caller asks for this one: dx and dW of
+// 61440 x 1024 x 4096 are then 0.0024 off of their size, where their own rounding alone is 0.0017, and the backward takes 1220 us
+// instead of 2340 (6000 x 176 x 416: 23 and 54).
+template <bool AT, bool BT>
+hipError_t gemm_wide(GemmArgs g, const Operand& A, const Operand& B, const Operand& lo, int type, float* part, hipStream_t st) {
+  const Plan p = gemm_plan(g.M, g.N, g.K, type, A.whole && B.whole);
+  g.part = part;
+  hipError_t e = gemm_tiles<AT, BT>(g, A, B, p, type, st);
+  g.part = part + (int64_t)p.splits * g.M * g.N;
+  g.dbpart = nullptr;
+  if (e == hipSuccess) e = gemm_tiles<AT, BT>(g, AT ? A : lo, AT ? lo : B, p, type, st);
+  g.part = part;
+  g.splits = 2 * p.splits;
+  return e != hipSuccess ? e : join_launch(g, type, st);
 }
 // Both products of a backward, dW's split in p.
 hipError_t gemm_both(GemmArgs x, GemmArgs w, const Operand& dz, const Operand& W, const Operand& X, const Plan& p, int type, float* part,
@@ -978,10 +1010,14 @@ bool both_pays(const slstm_linear_dims* d, const Plan& b) {
   return d->M > 0 && b.us * (d->type == SLSTM_F32 ? 0.8 : 1.) < two;
 }
 
+int act_of(const slstm_linear_dims* d) { return d->act & ~SLSTM_LINEAR_WIDE_DZ; }
+bool wide_dz(const slstm_linear_dims* d) {
+  return d->type == SLSTM_BF16 && act_of(d) != SLSTM_ACT_NONE && (d->act & SLSTM_LINEAR_WIDE_DZ);
+}
 bool linear_ok(const slstm_linear_dims* d) {
   if (!d || d->M < 0 || d->M > (1 << 30) || d->K < 1 || d->K > (1 << 24) || d->N < 1 || d->N > (1 << 24)) return false;
   if (d->type != SLSTM_F32 && d->type != SLSTM_BF16) return false;
-  if (d->act < SLSTM_ACT_NONE || d->act > SLSTM_ACT_GELU) return false;
+  if (act_of(d) < SLSTM_ACT_NONE || act_of(d) > SLSTM_ACT_GELU) return false;
   if (!stride_ok(d->ld_x, d->K) || !stride_ok(d->ld_w, d->N) || !stride_ok(d->ld_res, d->N) || !stride_ok(d->ld_y, d->N) ||
       !stride_ok(d->ld_dy, d->N))
     return false;
@@ -1009,7 +1045,7 @@ DzPlan dz_plan(const slstm_linear_dims* d) {
 // Work space of a forward: copies of x and W, parts; of a backward: dz (or a copy of dy), copies of W and x, sums of
 // columns, parts.
 struct Spaces {
-  size_t dz, x, W, db, part, total;
+  size_t dz, lo, x, W, db, part, total;
 };
 Spaces fwd_spaces(const slstm_linear_dims* d) {
   Spaces s = {};
@@ -1021,11 +1057,16 @@ Spaces fwd_spaces(const slstm_linear_dims* d) {
 }
 Spaces bwd_spaces(const slstm_linear_dims* d) {
   Spaces s = {};
-  const bool dz = d->act != SLSTM_ACT_NONE || needs_copy(d->M, d->N, row_stride(d->ld_dy, d->N), d->type);
-  s.x = dz ? copy_bytes(d->M, d->N, d->type) : 0;
+  const bool dz = act_of(d) != SLSTM_ACT_NONE || needs_copy(d->M, d->N, row_stride(d->ld_dy, d->N), d->type);
+  s.lo = dz ? copy_bytes(d->M, d->N, d->type) : 0;
+  s.x = s.lo + (wide_dz(d) ? copy_bytes(d->M, d->N, d->type) : 0);
   s.W = s.x + (needs_copy(d->M, d->K, row_stride(d->ld_x, d->K), d->type) ? copy_bytes(d->M, d->K, d->type) : 0);
   s.db = s.W + (needs_copy(d->M, d->N, row_stride(d->ld_w, d->N), d->type) ? copy_bytes(d->K, d->N, d->type) : 0);
   s.part = s.db + (((size_t)dz_plan(d).blocks * d->N * 4 + 255) & ~(size_t)255);
+  if (wide_dz(d)) {
+    s.total = s.part + std::max(wide_bytes(d->M, d->K, d->N, d->type), wide_bytes(d->K, d->N, d->M, d->type));
+    return s;
+  }
   s.total = s.part + std::max({gemm_bytes(d->M, d->K, d->N, d->type), gemm_bytes(d->K, d->N, d->M, d->type),
                                part_bytes(both_plan(d->M, d->K, d->N, d->type), d->K, d->N)});
   return s;
@@ -1057,7 +1098,7 @@ extern "C" int stacklstm_linear_fwd(const slstm_linear_dims* d, const void* x, c
   hipError_t e = cp.run(d->type, st);
   GemmArgs g = {};
   g.M = (int)d->M, g.N = d->N, g.K = d->K;
-  g.bias = b, g.res = res, g.y = y, g.z = z, g.act = d->act;
+  g.bias = b, g.res = res, g.y = y, g.z = z, g.act = act_of(d);
   g.ldy = row_stride(d->ld_y, d->N), g.ldr = row_stride(d->ld_res, d->N);
   if (e == hipSuccess) e = gemm<false, true>(g, ox, ow, d->type, (float*)(ws + s.part), st);
   return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
@@ -1066,7 +1107,7 @@ extern "C" int stacklstm_linear_fwd(const slstm_linear_dims* d, const void* x, c
 extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, const void* W, const void* z, const void* dy,
                                     void* dx, void* dW, void* db, void* workspace, size_t ws_bytes, void* stream) {
   if (!linear_ok(d)) return SLSTM_EINVAL;
-  const bool act = d->act != SLSTM_ACT_NONE;
+  const bool act = act_of(d) != SLSTM_ACT_NONE, wide = wide_dz(d);
   if (!workspace || !al16(workspace)) return SLSTM_EINVAL;
   if (d->M > 0 && (!dy || (act && !z) || (dW && !x) || (dx && !W))) return SLSTM_EINVAL;
   const Spaces s = bwd_spaces(d);
@@ -1075,16 +1116,16 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
   const hipStream_t st = as_stream(stream);
   char* ws = (char*)workspace;
   const int64_t ldx = row_stride(d->ld_x, d->K), ldw = row_stride(d->ld_w, d->N), ldd = row_stride(d->ld_dy, d->N);
-  const bool product = dx || dW, own = s.x > s.dz && product && d->M > 0;
-  if (few_rows(d)) {
+  const bool product = dx || dW, own = s.lo > s.dz && product && d->M > 0;
+  if (few_rows(d) && !wide) {
     auto tiles = [](int64_t m, int64_t n) { return (int)(((m + 63) / 64) * ((n + 63) / 64)); };
     GemmArgs gx = {}, gw = {};
     gx.M = (int)d->M, gx.N = d->K, gx.K = d->N, gx.A = dy, gx.lda = ldd, gx.B = W, gx.ldb = ldw, gx.y = dx, gx.ldy = d->K;
     gw.M = d->K, gw.N = d->N, gw.K = (int)d->M, gw.A = x, gw.lda = ldx, gw.B = dy, gw.ldb = ldd, gw.y = dW, gw.ldy = d->N;
     gx.splits = gw.splits = 1, gx.chunk = gx.K, gw.chunk = gw.K;
-    if (act) gx.dz = gw.dz = z, gx.lddz = gw.lddz = d->N, gx.dzact = gw.dzact = d->act;
+    if (act) gx.dz = gw.dz = z, gx.lddz = gw.lddz = d->N, gx.dzact = gw.dzact = act_of(d);
     DzArgs a = {};
-    a.M = (int)d->M, a.N = d->N, a.act = d->act, a.rows = (int)d->M, a.dy = dy, a.z = act ? z : nullptr, a.ldd = ldd, a.db = db;
+    a.M = (int)d->M, a.N = d->N, a.act = act_of(d), a.rows = (int)d->M, a.dy = dy, a.z = act ? z : nullptr, a.ldd = ldd, a.db = db;
     const int nx = dx ? tiles(d->M, d->K) : 0, nw = dW ? tiles(d->K, d->N) : 0, nb = db ? dz_plan(d).strips : 0;
     if (nx + nw + nb == 0) return SLSTM_OK;
     const dim3 grid(nx + nw + nb);
@@ -1104,8 +1145,8 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
   hipError_t e = hipSuccess;
   if (nd + cp.blocks > 0) {
     DzArgs a = {};
-    a.M = (int)d->M, a.N = d->N, a.act = d->act, a.rows = p.rows, a.dy = dy, a.z = act ? z : nullptr;
-    a.ldd = ldd, a.ldz = padded(d->N, d->type), a.dz = own ? ws + s.dz : nullptr, a.part = db && p.blocks > 1 ? (float*)(ws + s.db) : nullptr;
+    a.M = (int)d->M, a.N = d->N, a.act = act_of(d), a.rows = p.rows, a.dy = dy, a.z = act ? z : nullptr;
+    a.ldd = ldd, a.ldz = padded(d->N, d->type), a.dz = own ? ws + s.dz : nullptr, a.lo = own && wide ? ws + s.lo : nullptr, a.part = db && p.blocks > 1 ? (float*)(ws + s.db) : nullptr;
     a.db = db && p.blocks == 1 ? db : nullptr;
     const dim3 grid((unsigned)(nd + cp.blocks));
     auto run = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, p.strips, nd, cp.a); };
@@ -1123,6 +1164,12 @@ extern "C" int stacklstm_linear_bwd(const slstm_linear_dims* d, const void* x, c
   gx.M = (int)d->M, gx.N = d->K, gx.K = d->N, gx.y = dx, gx.ldy = d->K;
   gw.M = d->K, gw.N = d->N, gw.K = (int)d->M, gw.y = dW, gw.ldy = d->N;
   if (db && p.blocks > 1) gw.dbpart = (const float*)(ws + s.db), gw.dbrows = p.blocks, gw.db = db;
+  if (wide && own) {
+    const Operand lo = {ws + s.lo, oz.ld, oz.whole};
+    if (e == hipSuccess && dx) e = gemm_wide<false, false>(gx, oz, ow, lo, d->type, part, st);
+    if (e == hipSuccess && dW) e = gemm_wide<true, true>(gw, ox, oz, lo, d->type, part, st);
+    return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+  }
   if (dx && dW && ox.whole && ow.whole && oz.whole) {
     const Plan b = both_plan(d->M, d->K, d->N, d->type);
     if (both_pays(d, b)) {

@@ -22,6 +22,7 @@ SLSTM_F32, SLSTM_BF16 = 0, 1
 TYPES = {torch.float32: SLSTM_F32, torch.bfloat16: SLSTM_BF16}
 DTYPES = {SLSTM_F32: torch.float32, SLSTM_BF16: torch.bfloat16}
 ACTS = {"none": 0, "relu": 1, "tanh": 2, "silu": 3, "gelu": 4}
+SLSTM_LINEAR_WIDE_DZ = 0x100
 SLSTM_BEAM_MAX_STATES = 8
 EXPORTS = ("stacklstm_norm_workspace_bytes", "stacklstm_norm_fwd", "stacklstm_norm_bwd",
            "stacklstm_linear_fwd_workspace_bytes", "stacklstm_linear_bwd_workspace_bytes", "stacklstm_linear_fwd",
@@ -284,13 +285,15 @@ class LinearRun:
     workspace: torch.Tensor
 
     @classmethod
-    def of(cls, x, W, b=None, res=None, act="none", dy=None, y=None, train=None):
-        """y: where the outputs go (by default a buffer of its own); train: as in NormRun.of."""
+    def of(cls, x, W, b=None, res=None, act="none", dy=None, y=None, train=None, wide_dz=False):
+        """y: where the outputs go (by default a buffer of its own); train: as in NormRun.of; wide_dz: the backward's 16-bit
+        products take dz with 16 significant bits, for twice their time."""
         (M, K), N = x.shape, W.shape[1]
         train = dy is not None if train is None else train
         e = lambda *s, dtype=x.dtype: torch.empty(*s, dtype=dtype, device=x.device)
         y = e(M, N) if y is None else y
-        d = make_linear_dims(M, K, N, _type(x), ACTS[act], _ld(x), _ld(W), _ld(res), _ld(y), _ld(dy))
+        d = make_linear_dims(M, K, N, _type(x), ACTS[act] | (SLSTM_LINEAR_WIDE_DZ if wide_dz else 0), _ld(x), _ld(W), _ld(res),
+                             _ld(y), _ld(dy))
         n = _bytes("stacklstm_linear_fwd_workspace_bytes", d)
         if train:
             n = max(n, _bytes("stacklstm_linear_bwd_workspace_bytes", d))
