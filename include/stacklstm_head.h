@@ -80,7 +80,7 @@ typedef enum {
 
 typedef struct {
   int64_t M;               /* rows, 0 .. 2^30 */
-  int32_t K, N;            /* inputs and outputs, 1 .. 2^24 */
+  int32_t K, N;            /* inputs and outputs, 1 .. 2^24; y, x and W each of less than 2^31 - 2^19 tiles of 64 x 64 */
   int32_t type;            /* slstm_type of every array */
   int32_t act;             /* slstm_act, or that and SLSTM_LINEAR_WIDE_DZ */
   int64_t ld_x, ld_w, ld_res, ld_y, ld_dy;
@@ -152,7 +152,7 @@ int stacklstm_distill_step(const slstm_distill_dims* d, const void* logits, cons
  * of -inf or NaN is no continuation: a beam without legal tokens, with score -inf, or whose logits hold NaN or +inf
  * has none. */
 typedef struct {
-  int32_t B;               /* searches, >= 0 */
+  int32_t B;               /* searches, >= 0; B K <= 2^31 - 1 */
   int32_t K;               /* beams, 1 .. 64 */
   int32_t V;               /* tokens or actions, 1 .. 2^22 */
   int32_t type;            /* slstm_type of logits */

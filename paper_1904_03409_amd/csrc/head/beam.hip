@@ -9,8 +9,10 @@
 // taken one after the other.
 // Rows that are too long for registers, or too few to fill the chip, are cut into chunks with a pass for the
 // sums before (k_beam_part). Small vocabularies take one workgroup to a search (k_beam_small).
-// 64 searches of 16 x 64001 bf16: rows 41 us (3.2 TB/s: as many exponentials as elements beside the loads), k_beam_merge 4.9; 64 of
-// 8 x 83 f32 5.9; one of 4 x 131072 f32 in chunks 3.2 + 4.8 + 3.5 us.
+// 64 searches of 16 x 64001 bf16: rows 41 us (3.2 TB/s; vector units 43% busy, a quarter of the wave slots taken), k_beam_merge 4.8; 64
+// of 8 x 83 f32 6.1; one of 4 x 131072 f32 in chunks 3.2 + 4.8 + 3.5 us. With more than 48 beams the bound is near the least group's
+// largest and the list overflows on ordinary logits: k_beam_merge of 4 searches of 64 x 131072 takes 8 ms, the
+// whole selection of 32 beams 0.16.
 #include <algorithm>
 
 #include "../../../include/stacklstm_head.h"

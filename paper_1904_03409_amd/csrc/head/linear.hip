@@ -9,9 +9,9 @@
 // of odd widths are first copied to padded rows in the work space (k_linear_pad; dz is written there anyhow). For few rows,
 // where a copy of W would cost more than it gives, slices go through registers, with the rows' ends cut off there.
 // Where the tiles do not fill the chip the sum over k is split, and k_linear_join adds the parts and applies the
-// epilogue. Bound by the matrix units where rows are many: 61440 x 1024 x 4096 bf16 forward 690 us (747 TFLOP/s with gelu, z and
-// residual, 1.6 GB moved), dx 412 (1250), dW 430 (1198); 7680 x 500 x 333 f32 forward 36 us (72 TFLOP/s), dx and dW 64 (80); by W's
-// bytes where they are few: 64 x 1024 x 32000 bf16 14.3 us (4.9 TB/s).
+// epilogue. Bound by the matrix units where rows are many: 61440 x 1024 x 4096 bf16 forward 691 us (746 TFLOP/s with gelu, z and
+// residual, 2.3 GB past L2), dx 431 (1196), dW 436 (1182); 7680 x 500 x 333 f32 forward 37 us (69 TFLOP/s), dx and dW 64 (80); by W's
+// bytes where they are few: 64 x 1024 x 32000 bf16 14.2 us (5.0 TB/s).
 #include <algorithm>
 #include <atomic>
 
@@ -353,8 +353,8 @@ struct Mover {
 // In a slice's last step the waves meet: the next slice has landed, everybody has read what it needs of this one, and its
 // stages take later slices. The operand that comes from memory (the other one is read again and again from L2) is further
 // ahead: three stages of it and two of the other fill a CU's LDS at 256 x 256.
-// dx of 61440 x 1024 x 4096, bf16, random values: 1250 TFLOP/s; with fragments read at the start of each slice and two stages of
-// either operand 1090.
+// dx of 61440 x 1024 x 4096, bf16, random values: 1196 TFLOP/s (the best launch 1250); with fragments read at the start of each
+// slice and two stages of either operand 1090.
 template <typename T, bool AT, bool BT, int BM, int BN, int SA, int SB>
 __device__ __forceinline__ void dma_tile(const GemmArgs& g, int lid) {
   typedef Tile<T, BM, BN> S;

@@ -5,8 +5,8 @@
 // Bound by memory: a forward reads x (and res) and writes y (and the sum) once, a backward reads s, dy
 // (and dsum) and writes dx once. A row stays in registers between its loads and its stores, in the
 // fewest lanes that hold it in one or two vectors each (a wave then carries several narrow rows);
-// the variance is summed from differences to the mean, in 32 bits. 61440 x 1024 bf16 with a residual: forward 90 us
-// (5.6 TB/s), backward 112 us (4.5 TB/s) and 6 us for the columns' sums; 22912 x 200 f32: 10.2 us (3.6 TB/s), 13.6 and 3.8 us.
+// the variance is summed from differences to the mean, in 32 bits. 61440 x 1024 bf16 with a residual: forward 92 us
+// (5.5 TB/s), backward 113 us (4.6 TB/s) and 6 us for the columns' sums; 22912 x 200 f32: 10.2 us (3.6 TB/s), 13.7 and 3.9 us.
 #include <algorithm>
 
 #include "../../../include/stacklstm_head.h"
