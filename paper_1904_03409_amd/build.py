@@ -22,7 +22,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstacklstm.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "scan.hip", "plan.hip", "prep.hip", "contract.hip", "level_fwd.hip", "level_bwd.hip",
-           "head/norm.hip", "head/linear.hip", "head/distill.hip", "head/beam.hip"]
+           "head/norm.hip", "head/linear.hip", "head/distill.hip", "head/beam.hip",
+           "layers/attend_fwd.hip", "layers/attend_bwd.hip", "layers/dropout.hip", "layers/logprob.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # packed fp32 instructions stay off: only scalar fp32 ALU code is generated
@@ -49,7 +50,7 @@ def resource_report(text: str) -> dict:
 
 
 # wait states between an MFMA and a read of its result that hipcc inserts in straight-line code
-MFMA_WAITS = {"v_mfma_f32_16x16x32_bf16": 8, "v_mfma_f32_16x16x32_f16": 8}
+MFMA_WAITS = {"v_mfma_f32_16x16x32_bf16": 8, "v_mfma_f32_16x16x32_f16": 8, "v_mfma_f32_16x16x4_f32": 10}
 
 
 def _regs(tok: str) -> set:

@@ -1,0 +1,293 @@
+// What the attention kernels share: tiles of rows in LDS, fragments of the matrix instructions, work-space layout.
+//
+// Every product is a 16x16 matrix instruction (bf16: k of 32; fp32: the fp32 instruction, k of 4) of two kinds:
+//   scores: rows of a tile in LDS times rows that a wave keeps in registers, over the width of a head. The result of a lane is
+//     four rows of the tile (4 lq ..) for one of its own rows (l16), so softmax values need no exchange but with three lanes.
+//   sums: (the tile's columns)^T times such results, over the rows of the tile. Which tile row a result belongs to is free:
+//     rows are taken in an order that makes a lane's results, as they are, the fragment that the second product wants (bf16: eight
+//     neighbouring rows of a unit of 32; fp32: one of four).
+// l16 = lane % 16, lq = lane / 16.
+#pragma once
+#include <atomic>
+
+#include "../../../include/stacklstm_layers.h"
+#include "../head/head.h"
+
+namespace {
+
+struct AttendArgs {
+  int B, Tq, Tk, Hq, Hk, G, D;                         // G: query heads to a key's
+  float c, scale;                                      // c: scale log2 e
+  const void *q, *k, *v, *y, *dy;
+  slstm_strides sq, sk, sv, sy, sdy, sdq, sdk, sdv;
+  const int32_t *q_len, *k_len;
+  const uint8_t* mask;
+  void *out, *dq, *dk, *dv;
+  float* stats;                                        // [B, Hq, Tq, 2]: reference of the row's exponents (base 2), 1 / sum
+  const float* stats_in;
+  float *delta;                                        // [B, Hq, Tq]: dy . y
+  float *part, *ml;                                    // splits: [splits][B Hk][rows][D] sums, [splits][B Hk][rows][2] references and sums
+  int tiles, splits, chunk;                            // row tiles of a (sequence, key head); keys of a split
+  int64_t first;                                       // a launch's first workgroup
+  int64_t groups;                                      // all of them
+};
+
+template <typename T> struct frag_of { typedef f32x4 type; };
+template <> struct frag_of<bf16_t> { typedef bf16x8 type; };
+template <typename T> using frag_t = typename frag_of<T>::type;
+
+// A head's width padded to DP elements. Rows in LDS are 16 bytes apart more than they are long: a fragment's 16 rows lie in
+// different banks.
+template <typename T, int DP>
+struct Head {
+  typedef typename frag_of<T>::type frag;
+  static constexpr int V = vec<T>::N;
+  static constexpr int BYTES = DP * (int)sizeof(T), ROW = BYTES + 16, GPR = BYTES / 16, STEPS = GPR / 4, DT = DP / 16;
+  static constexpr int SUB = sizeof(T) == 2 ? 2 : 1, UNIT = 16 * SUB;      // tiles of 16 rows, and rows, of a unit
+};
+
+// Tile row (of a unit) that row i of score tile `sub` is; the four rows of a lane's result are row_of(sub, 4 lq) + 0 .. 3.
+template <typename T>
+__device__ __forceinline__ int row_of(int sub, int i) {
+  return sizeof(T) == 2 ? 8 * (i >> 2) + 4 * sub + (i & 3) : i;
+}
+
+// Fragments of a wave's own row: 16 bytes of every 64.
+template <typename T, int DP>
+__device__ __forceinline__ void load_own(const T* row, bool here, int D, int lq, frag_t<T> (&f)[Head<T, DP>::STEPS]) {
+  typedef Head<T, DP> H;
+#pragma unroll
+  for (int s = 0; s < H::STEPS; ++s) {
+    const int c = 4 * s + lq;
+    u32x4 r = {0u, 0u, 0u, 0u};
+    if (here && c * H::V < D) r = load_vec(row, c, D);
+    f[s] = __builtin_bit_cast(typename H::frag, r);
+  }
+}
+
+// acc += tile rows (of unit row `base`, score tile sub) times own rows.
+template <typename T, int DP, int N>
+__device__ __forceinline__ void scores(f32x4 (&acc)[N], const unsigned char* tile, int base, int sub, int l16, int lq,
+                                       const frag_t<T> (&own)[N][Head<T, DP>::STEPS]) {
+  typedef Head<T, DP> H;
+  const unsigned char* p = tile + (base + row_of<T>(sub, l16)) * H::ROW + lq * 16;
+#pragma unroll
+  for (int s = 0; s < H::STEPS; ++s) {
+    const typename H::frag a = *(const typename H::frag*)(p + s * 64);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (sizeof(T) == 2) {
+        acc[j] = mfma_bf16_16x16x32(a, own[j][s], acc[j]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], own[j][s][e], acc[j], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// A unit's results as the second product's fragment.
+template <typename T, int SUB>
+__device__ __forceinline__ frag_t<T> weights(const f32x4 (&p)[SUB]) {
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = static_cast<__bf16>(p[i >> 2][i & 3]);
+    return r;
+  } else {
+    return p[0];
+  }
+}
+// acc[j][dt] += (columns 16 dt .. of unit row `base` on)^T times the weights w[j].
+template <typename T, int DP, int N>
+__device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq,
+                                     const frag_t<T> (&w)[N]) {
+  typedef Head<T, DP> H;
+#pragma unroll
+  for (int dt = 0; dt < H::DT; ++dt) {
+    if constexpr (sizeof(T) == 2) {
+      // transposed: the lane gives the address of unit row 8 lq + l16 / 4 and columns 4 (l16 % 4) of the tile, and gets column
+      // l16, four rows
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      const unsigned char* q = tile + (base + 8 * lq + (l16 >> 2)) * H::ROW + (16 * dt + 4 * (l16 & 3)) * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * H::ROW));
+      const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int j = 0; j < N; ++j) acc[j][dt] = mfma_bf16_16x16x32(a, w[j], acc[j][dt]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a = *(const float*)(tile + (base + 4 * lq + e) * H::ROW + (16 * dt + l16) * 4);
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[j][e], acc[j][dt], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// ROWS rows on their way from memory to LDS through registers: zeros where ok(row) is false and past a head's end.
+template <typename T, int DP, int ROWS>
+struct Stage {
+  typedef Head<T, DP> H;
+  static constexpr int ALL = ROWS * H::GPR, I = (ALL + 255) / 256;
+  u32x4 r[I];
+  template <typename Ok>
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int D, Ok ok) {
+    const bool whole = D % H::V == 0;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int L = i * 256 + threadIdx.x, row = L / H::GPR, c = L % H::GPR;
+      r[i] = u32x4{0u, 0u, 0u, 0u};
+      if ((ALL % 256 == 0 || L < ALL) && c * H::V < D && ok(row)) {
+        const T* p = base + row * stride;
+        if (whole) r[i] = *(const u32x4_any*)(p + c * H::V);
+        else r[i] = load_vec(p, c, D);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* tile) const {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int L = i * 256 + threadIdx.x, row = L / H::GPR, c = L % H::GPR;
+      if (ALL % 256 == 0 || L < ALL) *(u32x4*)(tile + row * H::ROW + c * 16) = r[i];
+    }
+  }
+};
+
+// v to four neighbouring elements of a row from column n on.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int n, int D, const f32x4& v) {
+  if (n + 4 <= D) {
+    if constexpr (sizeof(T) == 4) {
+      *(u32x4_any*)(row + n) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+      typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+      *(u32x2_any*)(row + n) = u32x2_any{(uint32_t)f32_to_bf16_bits(v[0]) | (uint32_t)f32_to_bf16_bits(v[1]) << 16,
+                                         (uint32_t)f32_to_bf16_bits(v[2]) | (uint32_t)f32_to_bf16_bits(v[3]) << 16};
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 3; ++r)
+      if (n + r < D) from_f32(row[n + r], v[r]);
+  }
+}
+
+__device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
+  return len ? max(0, min(len[b], most)) : most;
+}
+// Over the lanes that hold the same own row.
+__device__ __forceinline__ float rows_max(float v) { return half_swap(row_swap(v, op_max()), op_max()); }
+__device__ __forceinline__ float rows_sum(float v) { return half_swap(row_swap(v, op_sum()), op_sum()); }
+
+// Workgroup -> (sequence and key head, split, row tile): workgroups go to the 8 XCDs in turn, and an XCD takes a contiguous run, so
+// that the row tiles that share keys find them in its L2.
+struct Place {
+  int bh, split, tile;
+};
+__device__ __forceinline__ Place place_of(const AttendArgs& a) {
+  int64_t id = a.first + blockIdx.x;
+  const int64_t full = a.groups & ~(int64_t)7;
+  if (id < full) id = (id & 7) * (full >> 3) + (id >> 3);
+  Place p;
+  const int64_t per = (int64_t)a.tiles * a.splits;
+  p.bh = (int)(id / per);
+  const int rest = (int)(id - p.bh * per);
+  p.split = rest / a.tiles;
+  p.tile = rest % a.tiles;
+  return p;
+}
+
+// ----------------------------------------------------------------------------- host
+
+inline bool strides_zero(const slstm_strides& s) { return s.b == 0 && s.t == 0 && s.h == 0; }
+inline slstm_strides strides_of(const slstm_strides& s, int T, int H, int D) {
+  if (!strides_zero(s)) return s;
+  return slstm_strides{(int64_t)T * H * D, (int64_t)H * D, D};
+}
+inline bool stride_range(const slstm_strides& s) {
+  const int64_t most = (int64_t)1 << 40;
+  return s.b >= 0 && s.t >= 0 && s.h >= 0 && s.b < most && s.t < most && s.h < most;
+}
+// No two elements of an output at one place: in the order of the strides each step passes all that lies within it.
+inline bool strides_apart(const slstm_strides& s, int B, int T, int H, int D) {
+  int64_t st[3] = {s.b, s.t, s.h}, n[3] = {B, T, H};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (st[j] < st[i]) {
+        int64_t x = st[i]; st[i] = st[j]; st[j] = x;
+        x = n[i]; n[i] = n[j]; n[j] = x;
+      }
+  int64_t extent = D;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] < 2) continue;
+    if (st[i] < extent) return false;
+    extent = st[i] * (n[i] - 1) + extent;
+  }
+  return true;
+}
+inline bool attend_ok(const slstm_attend_dims* d) {
+  if (!d || d->B < 0 || d->Tq < 0 || d->Tk < 0 || d->Tq > (1 << 24) || d->Tk > (1 << 24) || d->Hq < 1 || d->Hk < 1 ||
+      d->Hq > (1 << 16) || d->Hk > (1 << 16) || d->Hq % d->Hk || d->D < 1 || d->D > 256)
+    return false;
+  if (d->type != SLSTM_F32 && d->type != SLSTM_BF16) return false;
+  if (!(fabsf(d->scale) <= 3.4028234e38f)) return false;
+  if ((int64_t)d->Tq * d->Hq > 0x7fffffff || (int64_t)d->Tk * d->Hk > 0x7fffffff) return false;
+  if ((int64_t)d->Tq * d->Hq * d->B > 0x7fffffff || (int64_t)d->Tk * d->Hk * d->B > 0x7fffffff) return false;
+  const slstm_strides* s[8] = {&d->q, &d->k, &d->v, &d->dy, &d->y, &d->dq, &d->dk, &d->dv};
+  for (int i = 0; i < 8; ++i) {
+    if (!stride_range(*s[i])) return false;
+    const bool keys = i == 1 || i == 2 || i >= 6;
+    if (i >= 4 && !strides_zero(*s[i]) && !strides_apart(*s[i], d->B, keys ? d->Tk : d->Tq, keys ? d->Hk : d->Hq, d->D)) return false;
+  }
+  return true;
+}
+inline AttendArgs attend_args(const slstm_attend_dims* d) {
+  AttendArgs a = {};
+  a.B = d->B, a.Tq = d->Tq, a.Tk = d->Tk, a.Hq = d->Hq, a.Hk = d->Hk, a.G = d->Hq / d->Hk, a.D = d->D;
+  a.scale = d->scale, a.c = (float)((double)d->scale * 1.4426950408889634);
+  const int Tq = d->Tq, Tk = d->Tk, Hq = d->Hq, Hk = d->Hk, D = d->D;
+  a.sq = strides_of(d->q, Tq, Hq, D), a.sy = strides_of(d->y, Tq, Hq, D), a.sdy = strides_of(d->dy, Tq, Hq, D);
+  a.sdq = strides_of(d->dq, Tq, Hq, D), a.sk = strides_of(d->k, Tk, Hk, D), a.sv = strides_of(d->v, Tk, Hk, D);
+  a.sdk = strides_of(d->dk, Tk, Hk, D), a.sdv = strides_of(d->dv, Tk, Hk, D);
+  a.splits = 1;
+  return a;
+}
+// f(type, width): the kernels' variants.
+template <typename F>
+int attend_dispatch(const slstm_attend_dims* d, F f) {
+  auto width = [&](auto t) {
+    if (d->D <= 32) return f(t, std::integral_constant<int, 32>());
+    if (d->D <= 64) return f(t, std::integral_constant<int, 64>());
+    if (d->D <= 128) return f(t, std::integral_constant<int, 128>());
+    return f(t, std::integral_constant<int, 256>());
+  };
+  return d->type == SLSTM_F32 ? width(float()) : width(bf16_t());
+}
+// A kernel's LDS limit is raised once to a device, not at every call.
+inline hipError_t allow_lds(const void* kern, int lds, std::atomic<uint64_t>& devices) {
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (bit && (devices.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  const hipError_t s = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (s == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+  return s;
+}
+// All workgroups of a kernel, in as many launches as they need.
+template <typename K>
+hipError_t attend_launch(K kern, AttendArgs a, int64_t groups, int lds, std::atomic<uint64_t>& devices, hipStream_t st) {
+  if (lds > 65536) {
+    const hipError_t e = allow_lds((const void*)kern, lds, devices);
+    if (e != hipSuccess) return e;
+  }
+  a.groups = groups;
+  in_pieces(groups, kMostGroups, [&](int64_t g0, int64_t n) {
+    a.first = g0;
+    hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(256), (size_t)lds, st, a);
+  });
+  return hipGetLastError();
+}
+
+}  // namespace

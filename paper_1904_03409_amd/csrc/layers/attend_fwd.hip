@@ -1,0 +1,321 @@
+// Attention, forward: one pass over the keys with the running reference and sum of the softmax.
+//   x = c q . k (base 2),  l = sum 2^(x - m),  o = sum 2^(x - m) v,  y = o / l
+// The reference m of a row need not be its largest x: any number within 2^8 of it serves as well, and o and l are only brought
+// to a new one when a row's largest has risen by more than 8 (rarely behind the first tiles).
+// A wave has 16 QT queries (query and head of those that share a key's head) and all of a key tile, or, where there are few
+// queries, a quarter of the tile (WK = 4), whose parts are joined through LDS. Where the row tiles do not fill the chip the
+// keys are split over workgroups and k_attend_join joins their sums.
+#include <algorithm>
+
+#include "attend.h"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+template <typename T, int DP, int WK>
+struct Fwd {
+  typedef Head<T, DP> H;
+  // keys of a tile: two tiles (keys and values) of 32 KB at most, with four waves along the keys a unit to each
+  static constexpr int KT = WK == 4 ? 4 * H::UNIT : H::BYTES <= 256 ? 64 : H::BYTES <= 512 ? 32 : 16;
+  static constexpr int KW = KT / WK, NU = KW / H::UNIT;                  // keys and units of a wave
+  static constexpr int TILE = KT * H::ROW;
+  static constexpr int JOIN = WK == 4 ? 4 * 16 * (DP + 4) * 4 + 4 * 2 * 16 * 4 : 0;
+  static constexpr int LDS = 2 * TILE > JOIN ? 2 * TILE : JOIN;
+};
+
+// A row's outputs: o its sums (columns 16 dt + 4 lq ..), of reference m and sum l.
+template <typename T, int DP>
+__device__ __forceinline__ void fwd_row(const AttendArgs& a, int b, int t, int h, int lq, const f32x4 (&o)[DP / 16], float m, float l) {
+  // (l: 0 where no key is there; NaN stays)
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
+#pragma unroll
+  for (int dt = 0; dt < DP / 16; ++dt)
+    if (16 * dt + 4 * lq < a.D) store4(y, 16 * dt + 4 * lq, a.D, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * inv);
+  if (a.stats && lq == 0) {
+    float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * 2;
+    s[0] = l == 0.f ? INFINITY : m;
+    s[1] = inv;
+  }
+}
+
+}  // namespace
+
+template <typename T, int DP, int QT, int WK>
+__global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
+  typedef Head<T, DP> H;
+  typedef Fwd<T, DP, WK> F;
+  typedef typename H::frag frag;
+  extern __shared__ __align__(16) unsigned char sm[];
+  unsigned char *kt = sm, *vt = sm + F::TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
+  const int wk = WK == 4 ? wave : 0, wq = WK == 4 ? 0 : wave;
+  const Place pl = place_of(a);
+  const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk), rows = a.Tq * a.G;
+  constexpr int ROWS = 16 * QT * (4 / WK);
+  const int qlen = clamp_len(a.q_len, b, a.Tq), klen = clamp_len(a.k_len, b, a.Tk);
+  const int kbeg = pl.split * a.chunk;
+  // (no query of the tile is there: no keys)
+  const int kend = pl.tile * ROWS / a.G < qlen ? min(klen, kbeg + a.chunk) : kbeg;
+  int qt_[QT], qh_[QT];
+  bool here[QT];
+  frag q[QT][H::STEPS];
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    const int r = pl.tile * ROWS + 16 * (QT * wq + j) + l16;
+    qt_[j] = r / a.G;
+    qh_[j] = hk * a.G + r % a.G;
+    here[j] = r < rows;
+    load_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h,
+                    here[j] && qt_[j] < qlen, a.D, lq, q[j]);
+  }
+  const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
+  const T* vp = (const T*)a.v + (int64_t)b * a.sv.b + (int64_t)hk * a.sv.h;
+  const uint8_t* mask = a.mask ? a.mask + (int64_t)b * a.Tk : nullptr;
+  Stage<T, DP, F::KT> sk, sv;
+  auto load = [&](int k0) {
+    auto ok = [&](int r) { return k0 + r < kend && (!mask || mask[k0 + r]); };
+    sk.load(kp + (int64_t)k0 * a.sk.t, a.sk.t, a.D, ok);
+    sv.load(vp + (int64_t)k0 * a.sv.t, a.sv.t, a.D, ok);
+  };
+  f32x4 o[QT][H::DT];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    m[j] = -INFINITY, l[j] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (kbeg < kend) load(kbeg);
+  for (int k0 = kbeg; k0 < kend; k0 += F::KT) {
+    sk.store(kt);
+    sv.store(vt);
+    const int first = k0 + wk * F::KW;
+    const bool mine = lane < F::KW && first + lane < kend && (!mask || mask[first + lane]);
+    const unsigned long long there = __ballot(mine);
+    __syncthreads();
+    if (k0 + F::KT < kend) load(k0 + F::KT);
+    if (there) {
+      f32x4 s[F::NU][H::SUB][QT];
+#pragma unroll
+      for (int u = 0; u < F::NU; ++u)
+#pragma unroll
+        for (int i = 0; i < H::SUB; ++i) {
+#pragma unroll
+          for (int j = 0; j < QT; ++j) s[u][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          scores<T, DP, QT>(s[u][i], kt, wk * F::KW + u * H::UNIT, i, l16, lq, q);
+        }
+      const bool all = there == (F::KW == 64 ? ~0ull : (1ull << (F::KW & 63)) - 1);
+      float top[QT];
+#pragma unroll
+      for (int j = 0; j < QT; ++j) top[j] = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < F::NU; ++u)
+#pragma unroll
+        for (int i = 0; i < H::SUB; ++i) {
+          const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+#pragma unroll
+          for (int j = 0; j < QT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float x = s[u][i][j][r] * a.c;
+              if (!all) x = bits >> r & 1 ? x : -INFINITY;
+              s[u][i][j][r] = x;
+              top[j] = fmaxf(top[j], x);
+            }
+        }
+      bool rise = false;
+#pragma unroll
+      for (int j = 0; j < QT; ++j) {
+        top[j] = rows_max(top[j]);
+        rise |= top[j] > m[j] + 8.f;
+      }
+      if (__any(rise)) {
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+          const float to = top[j] > m[j] + 8.f ? top[j] : m[j];
+          // (-inf: nothing has come yet)
+          const float f = m[j] == to ? 1.f : __builtin_amdgcn_exp2f(m[j] - to);
+          m[j] = to;
+          l[j] *= f;
+#pragma unroll
+          for (int dt = 0; dt < H::DT; ++dt) o[j][dt] *= f;
+        }
+      }
+      frag w[F::NU][QT];
+#pragma unroll
+      for (int j = 0; j < QT; ++j) {
+        const float ref = m[j] == -INFINITY ? 0.f : m[j];
+#pragma unroll
+        for (int u = 0; u < F::NU; ++u) {
+          f32x4 p[H::SUB];
+#pragma unroll
+          for (int i = 0; i < H::SUB; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              p[i][r] = __builtin_amdgcn_exp2f(s[u][i][j][r] - ref);
+              l[j] += p[i][r];
+            }
+          w[u][j] = weights<T, H::SUB>(p);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < F::NU; ++u) sums<T, DP, QT>(o, vt, wk * F::KW + u * H::UNIT, l16, lq, w[u]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < QT; ++j) l[j] = rows_sum(l[j]);
+  if constexpr (WK == 4) {
+    // the waves' parts, [wave][16][DP + 4], and their references and sums, [wave][2][16], in the tiles' place
+    float *po = (float*)sm, *pm = po + 4 * 16 * (DP + 4);
+    float* mine = po + (wave * 16 + l16) * (DP + 4) + 4 * lq;
+#pragma unroll
+    for (int dt = 0; dt < H::DT; ++dt) *(f32x4*)(mine + 16 * dt) = o[0][dt];
+    if (lq == 0) pm[wave * 32 + l16] = m[0], pm[wave * 32 + 16 + l16] = l[0];
+    __syncthreads();
+    // the first wave has a place for every result (few queries: their sums are small)
+    if (wave) return;
+    m[0] = -INFINITY, l[0] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m[0] = fmaxf(m[0], pm[w * 32 + l16]);
+#pragma unroll
+    for (int dt = 0; dt < H::DT; ++dt) o[0][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = pm[w * 32 + l16], f = mw == m[0] ? 1.f : __builtin_amdgcn_exp2f(mw - m[0]);
+      l[0] += pm[w * 32 + 16 + l16] * f;
+      const float* part = po + (w * 16 + l16) * (DP + 4) + 4 * lq;
+#pragma unroll
+      for (int dt = 0; dt < H::DT; ++dt) o[0][dt] += *(const f32x4*)(part + 16 * dt) * f;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    if (!here[j]) continue;
+    // (behind its sequence's last query)
+    if (qt_[j] >= qlen) m[j] = -INFINITY, l[j] = 0.f;
+    if (a.splits == 1) {
+      fwd_row<T, DP>(a, b, qt_[j], qh_[j], lq, o[j], m[j], l[j]);
+    } else {
+      const int64_t r = ((int64_t)pl.split * a.B * a.Hk + pl.bh) * rows + qt_[j] * a.G + qh_[j] - hk * a.G;
+#pragma unroll
+      for (int dt = 0; dt < H::DT; ++dt)
+        if (16 * dt + 4 * lq < a.D) store4(a.part + r * a.D, 16 * dt + 4 * lq, a.D, o[j][dt]);
+      if (lq == 0) a.ml[2 * r] = m[j], a.ml[2 * r + 1] = l[j];
+    }
+  }
+}
+
+// A row's splits joined, a wave to a row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t rows = (int64_t)a.Tq * a.G, all = (int64_t)a.B * a.Hk * rows;
+  const int64_t row = a.first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= all) return;
+  float m = -INFINITY, l = 0.f;
+  for (int s = lane; s < a.splits; s += 64) m = fmaxf(m, a.ml[2 * (s * all + row)]);
+  m = lanes<64>(m, op_max());
+  auto factor = [&](float ms) { return ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m); };
+  for (int s = lane; s < a.splits; s += 64) l += a.ml[2 * (s * all + row) + 1] * factor(a.ml[2 * (s * all + row)]);
+  l = lanes<64>(l, op_sum());
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int bh = (int)(row / rows), r = (int)(row % rows), b = bh / a.Hk, t = r / a.G, h = bh % a.Hk * a.G + r % a.G;
+  T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
+  for (int n = lane; n < a.D; n += 64) {
+    float v = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) v += a.part[(s * all + row) * a.D + n] * factor(a.ml[2 * (s * all + row)]);
+    from_f32(y[n], l == 0.f ? 0.f : v * inv);
+  }
+  if (a.stats && lane == 0) {
+    float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * 2;
+    s[0] = l == 0.f ? INFINITY : m;
+    s[1] = inv;
+  }
+}
+
+namespace {
+
+// Row tiles and splits. Up to 16 rows (queries times heads of a key) share their keys in a tile; more rows go 16 or 32 to a wave.
+struct FwdPlan {
+  int qt, wk, rows, tiles, splits, chunk;
+};
+FwdPlan fwd_plan(const slstm_attend_dims* d) {
+  FwdPlan p;
+  const int64_t R = (int64_t)d->Tq * (d->Hq / d->Hk);
+  // (heads of 256: 32 rows to a wave need more registers than there are)
+  const bool wide = d->D > 128;
+  if (R <= 16) p.qt = 1, p.wk = 4;
+  else if (R <= 64 || wide) p.qt = 1, p.wk = 1;
+  else p.qt = 2, p.wk = 1;
+  p.rows = 16 * p.qt * (4 / p.wk);
+  p.tiles = (int)((R + p.rows - 1) / p.rows);
+  // splits of 256 keys at least, until there are two workgroups to a compute unit
+  const int64_t groups = (int64_t)p.tiles * d->B * d->Hk;
+  const int64_t want = groups ? 512 / groups : 1, most = ((int64_t)d->Tk + 255) / 256;
+  p.splits = (int)std::max<int64_t>(1, std::min(want, most));
+  p.chunk = (((d->Tk + p.splits - 1) / p.splits) + 127) / 128 * 128;
+  if (p.chunk < 128) p.chunk = 128;
+  p.splits = std::max(1, (d->Tk + p.chunk - 1) / p.chunk);
+  return p;
+}
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+extern "C" size_t stacklstm_attend_fwd_workspace_bytes(const slstm_attend_dims* d) {
+  if (!attend_ok(d)) return 0;
+  const FwdPlan p = fwd_plan(d);
+  if (p.splits == 1) return 16;
+  const size_t rows = (size_t)p.splits * d->B * d->Tq * d->Hq;
+  return up256(rows * d->D * 4) + rows * 8;
+}
+
+extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, const void* k, const void* v, const int32_t* q_len,
+                                    const int32_t* k_len, const uint8_t* mask, void* y, float* stats, void* workspace, size_t ws_bytes,
+                                    void* stream) {
+  if (!attend_ok(d)) return SLSTM_EINVAL;
+  if (d->B == 0 || d->Tq == 0) return SLSTM_OK;
+  if (!q || !y || (d->Tk && (!k || !v))) return SLSTM_EINVAL;
+  if (y == q || (d->Tk && (y == k || y == v))) return SLSTM_EINVAL;
+  AttendArgs a = attend_args(d);
+  a.q = q, a.k = k, a.v = v, a.q_len = q_len, a.k_len = k_len, a.mask = mask, a.out = y, a.stats = stats;
+  const FwdPlan p = fwd_plan(d);
+  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
+  if (p.splits > 1) {
+    if (!workspace || ((uintptr_t)workspace & 15u)) return SLSTM_EINVAL;
+    if (ws_bytes < stacklstm_attend_fwd_workspace_bytes(d)) return SLSTM_EWORKSPACE;
+    a.part = (float*)workspace;
+    a.ml = (float*)((char*)workspace + up256((size_t)p.splits * d->B * d->Tq * d->Hq * d->D * 4));
+  }
+  const hipStream_t st = as_stream(stream);
+  const int64_t groups = (int64_t)p.tiles * d->B * d->Hk * p.splits;
+  return attend_dispatch(d, [&](auto t, auto dp) {
+    typedef decltype(t) T;
+    constexpr int DP = decltype(dp)::value;
+    hipError_t e;
+    if (p.wk == 4) {
+      static std::atomic<uint64_t> dev;
+      e = attend_launch(k_attend_fwd<T, DP, 1, 4>, a, groups, Fwd<T, DP, 4>::LDS, dev, st);
+    } else if (p.qt == 1) {
+      static std::atomic<uint64_t> dev;
+      e = attend_launch(k_attend_fwd<T, DP, 1, 1>, a, groups, Fwd<T, DP, 1>::LDS, dev, st);
+    } else if constexpr (DP <= 128) {
+      static std::atomic<uint64_t> dev;
+      e = attend_launch(k_attend_fwd<T, DP, 2, 1>, a, groups, Fwd<T, DP, 1>::LDS, dev, st);
+    } else {
+      e = hipErrorInvalidValue;
+    }
+    if (e == hipSuccess && p.splits > 1) {
+      in_pieces((int64_t)d->B * d->Tq * d->Hq, 4 * kMostGroups, [&](int64_t r0, int64_t n) {
+        a.first = r0;
+        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, a);
+      });
+      e = hipGetLastError();
+    }
+    return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
+  });
+}
