@@ -36,15 +36,25 @@ template <typename T> struct frag_of { typedef f32x4 type; };
 template <> struct frag_of<bf16_t> { typedef bf16x8 type; };
 template <typename T> using frag_t = typename frag_of<T>::type;
 
-// A head's width padded to DP elements. Rows in LDS are 16 bytes apart more than they are long: a fragment's 16 rows lie in
-// different banks.
+// A head's width padded to DP elements.
 template <typename T, int DP>
 struct Head {
   typedef typename frag_of<T>::type frag;
   static constexpr int V = vec<T>::N;
-  static constexpr int BYTES = DP * (int)sizeof(T), ROW = BYTES + 16, GPR = BYTES / 16, STEPS = GPR / 4, DT = DP / 16;
+  static constexpr int BYTES = DP * (int)sizeof(T), GPR = BYTES / 16, STEPS = GPR / 4, DT = DP / 16;
   static constexpr int SUB = sizeof(T) == 2 ? 2 : 1, UNIT = 16 * SUB;      // tiles of 16 rows, and rows, of a unit
 };
+
+// Rows of a tile lie densely in LDS; 16-byte granule c of row r is at place c ^ swz(r) of its row, so that neither the 16 rows of a
+// score's fragment nor the rows of a transposed one meet in a bank. bf16: fragments take rows 0 .. 3, 8 .. 11, 16 .. 19, 24 .. 27 (+ 4) of a unit;
+// a transposed read takes pairs of granules of eight of them. fp32: rows 0 .. 15; every fourth row, four granules.
+template <typename T, int GPR>
+__device__ __forceinline__ int swz(int r) {
+  if constexpr (sizeof(T) == 4) return GPR >= 16 ? r & 15 : (r >> 1) & 7;
+  else if constexpr (GPR >= 16) return (r & 3) << 1 | (r & 8) | (r >> 4 & 1);
+  else if constexpr (GPR == 8) return (r & 2) | (r >> 1 & 4) | (r >> 4 & 1);
+  else return (r >> 2 & 2) | (r >> 4 & 1);
+}
 
 // Tile row (of a unit) that row i of score tile `sub` is; the four rows of a lane's result are row_of(sub, 4 lq) + 0 .. 3.
 template <typename T>
@@ -65,15 +75,15 @@ __device__ __forceinline__ void load_own(const T* row, bool here, int D, int lq,
   }
 }
 
-// acc += tile rows (of unit row `base`, score tile sub) times own rows.
+// acc += tile rows (of unit row `base`, a multiple of the unit, score tile sub) times own rows.
 template <typename T, int DP, int N>
 __device__ __forceinline__ void scores(f32x4 (&acc)[N], const unsigned char* tile, int base, int sub, int l16, int lq,
                                        const frag_t<T> (&own)[N][Head<T, DP>::STEPS]) {
   typedef Head<T, DP> H;
-  const unsigned char* p = tile + (base + row_of<T>(sub, l16)) * H::ROW + lq * 16;
+  const int row = row_of<T>(sub, l16), f = swz<T, H::GPR>(row);
 #pragma unroll
   for (int s = 0; s < H::STEPS; ++s) {
-    const typename H::frag a = *(const typename H::frag*)(p + s * 64);
+    const typename H::frag a = *(const typename H::frag*)(tile + (base + row) * H::BYTES + ((4 * s + lq) ^ f) * 16);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if constexpr (sizeof(T) == 2) {
@@ -109,16 +119,18 @@ __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned ch
       // transposed: the lane gives the address of unit row 8 lq + l16 / 4 and columns 4 (l16 % 4) of the tile, and gets column
       // l16, four rows
       typedef short s16x4 __attribute__((ext_vector_type(4)));
-      const unsigned char* q = tile + (base + 8 * lq + (l16 >> 2)) * H::ROW + (16 * dt + 4 * (l16 & 3)) * 2;
+      const int row = 8 * lq + (l16 >> 2);
+      const unsigned char* q = tile + (base + row) * H::BYTES + ((2 * dt + (l16 >> 1 & 1)) ^ swz<T, H::GPR>(row)) * 16 + (l16 & 1) * 8;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * H::ROW));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * H::BYTES));
       const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int j = 0; j < N; ++j) acc[j][dt] = mfma_bf16_16x16x32(a, w[j], acc[j][dt]);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float a = *(const float*)(tile + (base + 4 * lq + e) * H::ROW + (16 * dt + l16) * 4);
+        const int row = 4 * lq + e;
+        const float a = *(const float*)(tile + (base + row) * H::BYTES + ((4 * dt + (l16 >> 2)) ^ swz<T, H::GPR>(base + row)) * 16 + (l16 & 3) * 4);
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[j][e], acc[j][dt], 0, 0, 0);
       }
@@ -126,31 +138,68 @@ __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned ch
   }
 }
 
-// ROWS rows on their way from memory to LDS through registers: zeros where ok(row) is false and past a head's end.
-template <typename T, int DP, int ROWS>
-struct Stage {
+// ROWS rows on their way from memory to LDS: zeros where a row is not there and past a head's end. With DMA straight to LDS (rows
+// of whole, aligned granules), else through registers: go() starts a tile, land() puts it in place.
+template <typename T, int DP, int ROWS, bool DMA>
+struct Mover {
   typedef Head<T, DP> H;
   static constexpr int ALL = ROWS * H::GPR, I = (ALL + 255) / 256;
-  u32x4 r[I];
-  template <typename Ok>
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int D, Ok ok) {
-    const bool whole = D % H::V == 0;
+  static_assert(!DMA || ALL % 256 == 0, "whole waves");
+  u32x4 r[DMA ? 1 : I];
+  uint32_t off[DMA ? I : 1];
+  static __device__ __forceinline__ void place(int i, int& row, int& c) {
+    const int L = i * 256 + threadIdx.x;
+    row = L / H::GPR;
+    c = (L % H::GPR) ^ swz<T, H::GPR>(row);
+  }
+  __device__ __forceinline__ void start(int64_t stride, int D) {
+    if constexpr (DMA) {
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const int L = i * 256 + threadIdx.x, row = L / H::GPR, c = L % H::GPR;
-      r[i] = u32x4{0u, 0u, 0u, 0u};
-      if ((ALL % 256 == 0 || L < ALL) && c * H::V < D && ok(row)) {
-        const T* p = base + row * stride;
-        if (whole) r[i] = *(const u32x4_any*)(p + c * H::V);
-        else r[i] = load_vec(p, c, D);
+      for (int i = 0; i < I; ++i) {
+        int row, c;
+        place(i, row, c);
+        off[i] = c * H::V < D ? (uint32_t)(row * stride + c * H::V) * (uint32_t)sizeof(T) : kOOB;
       }
     }
   }
-  __device__ __forceinline__ void store(unsigned char* tile) const {
+  // rows 0 .. n of base (more than 0), those with mask byte 0 (mask not NULL) left out
+  __device__ __forceinline__ void go(const T* base, int64_t stride, int D, int n, const uint8_t* mask, unsigned char* tile) {
+    n = min(n, ROWS);
+    if constexpr (DMA) {
+      const rsrc_t rs = make_rsrc(base, (size_t)((n - 1) * stride + D) * sizeof(T));
+      const int wave = uni(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const int L = i * 256 + threadIdx.x, row = L / H::GPR, c = L % H::GPR;
-      if (ALL % 256 == 0 || L < ALL) *(u32x4*)(tile + row * H::ROW + c * 16) = r[i];
+      for (int i = 0; i < I; ++i) {
+        uint32_t o = off[i];
+        if (mask) {
+          int row, c;
+          place(i, row, c);
+          if (row >= n || !mask[row]) o = kOOB;
+        }
+        bdma16(rs, o, 0, lds_addr(tile + (i * 4 + wave) * 1024));
+      }
+    } else {
+      const bool whole = D % H::V == 0;
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        int row, c;
+        place(i, row, c);
+        r[i] = u32x4{0u, 0u, 0u, 0u};
+        if (row < n && c * H::V < D && (!mask || mask[row])) {
+          const T* p = base + row * stride;
+          if (whole) r[i] = *(const u32x4_any*)(p + c * H::V);
+          else r[i] = load_vec(p, c, D);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void land(unsigned char* tile) const {
+    if constexpr (!DMA) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        const int L = i * 256 + threadIdx.x;
+        if (ALL % 256 == 0 || L < ALL) *(u32x4*)(tile + L * 16) = r[i];
+      }
     }
   }
 };
@@ -274,6 +323,13 @@ inline hipError_t allow_lds(const void* kern, int lds, std::atomic<uint64_t>& de
   const hipError_t s = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (s == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
   return s;
+}
+// Whether rows may go by DMA: whole granules of 16 bytes at aligned places, rows that do not overlap (a row behind the last is then
+// past the descriptor's end), a tile of at most 64 (of few queries 128) rows within 2^31 bytes.
+inline bool dma_ok(const slstm_attend_dims* d, const void* p, const slstm_strides& s) {
+  const int e = d->type == SLSTM_F32 ? 4 : 2, V = 16 / e;
+  return d->D % V == 0 && ((uintptr_t)p & 15u) == 0 && s.b % V == 0 && s.t % V == 0 && s.h % V == 0 && s.t >= d->D &&
+         s.t * 128 * e < ((int64_t)1 << 31);
 }
 // All workgroups of a kernel, in as many launches as they need.
 template <typename K>

@@ -11,25 +11,28 @@
 
 namespace {
 
-template <typename T, int DP>
+template <typename T, int DP, bool DMA>
 struct Bwd {
   typedef Head<T, DP> H;
   // rows of a tile in LDS: two tiles of 32 KB at most together with what is kept in registers; 16 own rows to a wave at 256
   static constexpr int R = H::BYTES <= 256 ? 64 : H::BYTES <= 512 ? 32 : 16, NU = R / H::UNIT;
-  static constexpr int TILE = R * H::ROW, LDS = 2 * TILE + 3 * R * 4;
-  static constexpr int QT = DP <= 128 ? 2 : 1, OWN = 64 * QT;            // own rows of a wave / 16, of a workgroup
+  static constexpr int TILE = R * H::BYTES, LDS = 4 * TILE + 2 * 3 * R * 4;
+  // own rows of a wave / 16, of a workgroup (fp32 heads of 128 by way of registers: two would not fit)
+  static constexpr int QT = DP <= 64 || (DP == 128 && (DMA || sizeof(T) == 2)) ? 2 : 1, OWN = 64 * QT;
+  // waves on a SIMD that the registers are to leave room for: two hide each other's waits (bf16 heads of 128, dq: 230 registers)
+  static constexpr int WDQ = H::BYTES <= 128 || (DMA && H::BYTES <= 256 && sizeof(T) == 2) ? 2 : 1;
+  static constexpr int WDKV = H::BYTES <= 128 ? 2 : 1;
 };
 
 }  // namespace
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(256) k_attend_dq(AttendArgs a) {
+template <typename T, int DP, bool DMA>
+__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Bwd<T, DP> F;
+  typedef Bwd<T, DP, DMA> F;
   typedef frag_t<T> frag;
   constexpr int QT = F::QT;
   extern __shared__ __align__(16) unsigned char sm[];
-  unsigned char *kt = sm, *vt = sm + F::TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
   const Place pl = place_of(a);
   const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk), rows = a.Tq * a.G;
@@ -66,24 +69,28 @@ __global__ void __launch_bounds__(256) k_attend_dq(AttendArgs a) {
   const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
   const T* vp = (const T*)a.v + (int64_t)b * a.sv.b + (int64_t)hk * a.sv.h;
   const uint8_t* mask = a.mask ? a.mask + (int64_t)b * a.Tk : nullptr;
-  Stage<T, DP, F::R> sk, sv;
-  auto load = [&](int k0) {
-    auto ok = [&](int r) { return k0 + r < kend && (!mask || mask[k0 + r]); };
-    sk.load(kp + (int64_t)k0 * a.sk.t, a.sk.t, a.D, ok);
-    sv.load(vp + (int64_t)k0 * a.sv.t, a.sv.t, a.D, ok);
+  Mover<T, DP, F::R, DMA> mk, mv;
+  mk.start(a.sk.t, a.D);
+  mv.start(a.sv.t, a.D);
+  auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
+  auto go = [&](int k0, int n) {
+    const uint8_t* there = mask ? mask + k0 : nullptr;
+    mk.go(kp + (int64_t)k0 * a.sk.t, a.sk.t, a.D, kend - k0, there, stage(n));
+    mv.go(vp + (int64_t)k0 * a.sv.t, a.sv.t, a.D, kend - k0, there, stage(n) + F::TILE);
   };
   f32x4 o[QT][H::DT];
 #pragma unroll
   for (int j = 0; j < QT; ++j)
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (kend > 0) load(0);
-  for (int k0 = 0; k0 < kend; k0 += F::R) {
-    sk.store(kt);
-    sv.store(vt);
+  if (kend > 0) go(0, 0);
+  for (int k0 = 0, n = 0; k0 < kend; k0 += F::R, ++n) {
+    const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const unsigned long long there = __ballot(lane < F::R && k0 + lane < kend && (!mask || mask[k0 + lane]));
+    if constexpr (DMA) wait_vm<0>();
+    else mk.land(stage(n)), mv.land(stage(n) + F::TILE);
     __syncthreads();
-    if (k0 + F::R < kend) load(k0 + F::R);
+    if (k0 + F::R < kend) go(k0 + F::R, n + 1);
 #pragma unroll
     for (int u = 0; u < F::NU; ++u) {
       f32x4 s[H::SUB][QT], dp[H::SUB][QT];
@@ -112,7 +119,6 @@ __global__ void __launch_bounds__(256) k_attend_dq(AttendArgs a) {
       }
       sums<T, DP, QT>(o, kt, u * H::UNIT, l16, lq, w);
     }
-    __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
@@ -124,15 +130,14 @@ __global__ void __launch_bounds__(256) k_attend_dq(AttendArgs a) {
   }
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(256) k_attend_dkv(AttendArgs a) {
+template <typename T, int DP, bool DMA>
+__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDKV)) k_attend_dkv(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Bwd<T, DP> F;
+  typedef Bwd<T, DP, DMA> F;
   typedef frag_t<T> frag;
   constexpr int KN = F::QT;
   extern __shared__ __align__(16) unsigned char sm[];
-  unsigned char *qt = sm, *gt = sm + F::TILE;
-  float* st = (float*)(sm + 2 * F::TILE);              // [3][R]: m, 1 / l, delta
+  float* stats = (float*)(sm + 4 * F::TILE);           // two stages of [3][R]: m, 1 / l, delta
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
   const Place pl = place_of(a);
   const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk);
@@ -154,30 +159,35 @@ __global__ void __launch_bounds__(256) k_attend_dkv(AttendArgs a) {
   for (int j = 0; j < KN; ++j)
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) dk[j][dt] = dv[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Stage<T, DP, F::R> sq, sg;
-  float sm_ = 0.f, si_ = 0.f, sd_ = 0.f;
+  Mover<T, DP, F::R, DMA> mq, mg;
+  mq.start(a.sq.t, a.D);
+  mg.start(a.sdy.t, a.D);
+  float tm = 0.f, ti = 0.f, td = 0.f;
   // tiles of the first head's queries, then of the next one's
   const int tiles = (qend + F::R - 1) / F::R, all = tiles * a.G;
-  auto load = [&](int n) {
+  auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
+  auto go = [&](int n) {
     const int h = hk * a.G + n / tiles, t0 = n % tiles * F::R;
-    auto ok = [&](int r) { return t0 + r < qend; };
-    sq.load((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, ok);
-    sg.load((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, ok);
+    mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
+    mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
+          stage(n) + F::TILE);
     if (tid < F::R) {
-      sm_ = INFINITY, si_ = sd_ = 0.f;
+      tm = INFINITY, ti = td = 0.f;
       if (t0 + tid < qend) {
         const int64_t at = ((int64_t)b * a.Hq + h) * a.Tq + t0 + tid;
-        sm_ = a.stats_in[2 * at], si_ = a.stats_in[2 * at + 1], sd_ = a.delta[at];
+        tm = a.stats_in[2 * at], ti = a.stats_in[2 * at + 1], td = a.delta[at];
       }
     }
   };
-  if (all) load(0);
+  if (all) go(0);
   for (int n = 0; n < all; ++n) {
-    sq.store(qt);
-    sg.store(gt);
-    if (tid < F::R) st[tid] = sm_, st[F::R + tid] = si_, st[2 * F::R + tid] = sd_;
+    const unsigned char *qt = stage(n), *gt = qt + F::TILE;
+    float* st = stats + (n & 1) * 3 * F::R;
+    if constexpr (DMA) wait_vm<0>();
+    else mq.land(stage(n)), mg.land(stage(n) + F::TILE);
+    if (tid < F::R) st[tid] = tm, st[F::R + tid] = ti, st[2 * F::R + tid] = td;
     __syncthreads();
-    if (n + 1 < all) load(n + 1);
+    if (n + 1 < all) go(n + 1);
 #pragma unroll
     for (int u = 0; u < F::NU; ++u) {
       f32x4 s[H::SUB][KN], dp[H::SUB][KN];
@@ -209,7 +219,6 @@ __global__ void __launch_bounds__(256) k_attend_dkv(AttendArgs a) {
       sums<T, DP, KN>(dv, gt, u * H::UNIT, l16, lq, wp);
       sums<T, DP, KN>(dk, qt, u * H::UNIT, l16, lq, ws);
     }
-    __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < KN; ++j) {
@@ -253,16 +262,24 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
   return attend_dispatch(d, [&](auto t, auto dp) {
     typedef decltype(t) T;
     constexpr int DP = decltype(dp)::value;
-    typedef Bwd<T, DP> F;
-    static std::atomic<uint64_t> dev[2];
     hipError_t e = hipSuccess;
     if (d->Tq) {
-      a.tiles = (int)(((int64_t)d->Tq * a.G + F::OWN - 1) / F::OWN);
-      e = attend_launch(k_attend_dq<T, DP>, a, (int64_t)a.tiles * d->B * d->Hk, F::LDS, dev[0], st);
+      auto run = [&](auto dma) {
+        typedef Bwd<T, DP, decltype(dma)::value> F;
+        static std::atomic<uint64_t> dev;
+        a.tiles = (int)(((int64_t)d->Tq * a.G + F::OWN - 1) / F::OWN);
+        return attend_launch(k_attend_dq<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk, F::LDS, dev, st);
+      };
+      e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     }
     if (e == hipSuccess && d->Tk) {
-      a.tiles = (d->Tk + F::OWN - 1) / F::OWN;
-      e = attend_launch(k_attend_dkv<T, DP>, a, (int64_t)a.tiles * d->B * d->Hk, F::LDS, dev[1], st);
+      auto run = [&](auto dma) {
+        typedef Bwd<T, DP, decltype(dma)::value> F;
+        static std::atomic<uint64_t> dev;
+        a.tiles = (d->Tk + F::OWN - 1) / F::OWN;
+        return attend_launch(k_attend_dkv<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk, F::LDS, dev, st);
+      };
+      e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? run(std::true_type()) : run(std::false_type());
     }
     return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
   });

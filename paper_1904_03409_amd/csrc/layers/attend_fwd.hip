@@ -13,15 +13,18 @@
 
 namespace {
 
-template <typename T, int DP, int WK>
+template <typename T, int DP, int WK, bool DMA>
 struct Fwd {
   typedef Head<T, DP> H;
-  // keys of a tile: two tiles (keys and values) of 32 KB at most, with four waves along the keys a unit to each
+  // keys of a tile: 16 KB of keys and of values, twice, at most; with four waves along the keys a unit to each
   static constexpr int KT = WK == 4 ? 4 * H::UNIT : H::BYTES <= 256 ? 64 : H::BYTES <= 512 ? 32 : 16;
   static constexpr int KW = KT / WK, NU = KW / H::UNIT;                  // keys and units of a wave
-  static constexpr int TILE = KT * H::ROW;
+  static constexpr int TILE = KT * H::BYTES;
+  // waves on a SIMD that the registers are to leave room for: two hide each other's waits and run products beside exponentials
+  static constexpr int WAVES = H::BYTES <= 128 || (DMA && DP <= 128) ? 2 : 1;
   static constexpr int JOIN = WK == 4 ? 4 * 16 * (DP + 4) * 4 + 4 * 2 * 16 * 4 : 0;
-  static constexpr int LDS = 2 * TILE > JOIN ? 2 * TILE : JOIN;
+  static constexpr int STAGES = 4 * TILE <= 160 * 1024 ? 2 : 1;
+  static constexpr int LDS = 2 * STAGES * TILE > JOIN ? 2 * STAGES * TILE : JOIN;
 };
 
 // A row's outputs: o its sums (columns 16 dt + 4 lq ..), of reference m and sum l.
@@ -42,13 +45,12 @@ __device__ __forceinline__ void fwd_row(const AttendArgs& a, int b, int t, int h
 
 }  // namespace
 
-template <typename T, int DP, int QT, int WK>
-__global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
+template <typename T, int DP, int QT, int WK, bool DMA>
+__global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fwd(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Fwd<T, DP, WK> F;
+  typedef Fwd<T, DP, WK, DMA> F;
   typedef typename H::frag frag;
   extern __shared__ __align__(16) unsigned char sm[];
-  unsigned char *kt = sm, *vt = sm + F::TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
   const int wk = WK == 4 ? wave : 0, wq = WK == 4 ? 0 : wave;
   const Place pl = place_of(a);
@@ -73,11 +75,14 @@ __global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
   const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
   const T* vp = (const T*)a.v + (int64_t)b * a.sv.b + (int64_t)hk * a.sv.h;
   const uint8_t* mask = a.mask ? a.mask + (int64_t)b * a.Tk : nullptr;
-  Stage<T, DP, F::KT> sk, sv;
-  auto load = [&](int k0) {
-    auto ok = [&](int r) { return k0 + r < kend && (!mask || mask[k0 + r]); };
-    sk.load(kp + (int64_t)k0 * a.sk.t, a.sk.t, a.D, ok);
-    sv.load(vp + (int64_t)k0 * a.sv.t, a.sv.t, a.D, ok);
+  Mover<T, DP, F::KT, DMA> mk, mv;
+  mk.start(a.sk.t, a.D);
+  mv.start(a.sv.t, a.D);
+  auto stage = [&](int n) { return sm + (F::STAGES == 2 ? (n & 1) * 2 * F::TILE : 0); };
+  auto go = [&](int k0, int n) {
+    const uint8_t* there = mask ? mask + k0 : nullptr;
+    mk.go(kp + (int64_t)k0 * a.sk.t, a.sk.t, a.D, kend - k0, there, stage(n));
+    mv.go(vp + (int64_t)k0 * a.sv.t, a.sv.t, a.D, kend - k0, there, stage(n) + F::TILE);
   };
   f32x4 o[QT][H::DT];
   float m[QT], l[QT];
@@ -87,15 +92,15 @@ __global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (kbeg < kend) load(kbeg);
-  for (int k0 = kbeg; k0 < kend; k0 += F::KT) {
-    sk.store(kt);
-    sv.store(vt);
+  if (kbeg < kend) go(kbeg, 0);
+  for (int k0 = kbeg, n = 0; k0 < kend; k0 += F::KT, ++n) {
+    const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const int first = k0 + wk * F::KW;
-    const bool mine = lane < F::KW && first + lane < kend && (!mask || mask[first + lane]);
-    const unsigned long long there = __ballot(mine);
+    const unsigned long long there = __ballot(lane < F::KW && first + lane < kend && (!mask || mask[first + lane]));
+    if constexpr (DMA) wait_vm<0>();
+    else mk.land(stage(n)), mv.land(stage(n) + F::TILE);
     __syncthreads();
-    if (k0 + F::KT < kend) load(k0 + F::KT);
+    if (F::STAGES == 2 && k0 + F::KT < kend) go(k0 + F::KT, n + 1);
     if (there) {
       f32x4 s[F::NU][H::SUB][QT];
 #pragma unroll
@@ -106,25 +111,45 @@ __global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
           for (int j = 0; j < QT; ++j) s[u][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
           scores<T, DP, QT>(s[u][i], kt, wk * F::KW + u * H::UNIT, i, l16, lq, q);
         }
-      const bool all = there == (F::KW == 64 ? ~0ull : (1ull << (F::KW & 63)) - 1);
-      float top[QT];
+      // x = c s: where all keys are there and no row's largest is far from 0, c goes into the exponent's own step (a reference of up
+      // to 2^20 is rounded by 2^-4 at most, the same for all of a row's terms); else the products stand in the scores' place
+      float top[QT], c = a.c;
+      bool plain = there == (F::KW == 64 ? ~0ull : (1ull << (F::KW & 63)) - 1) && a.c > 0.f;
+      if (plain) {
+        bool far = false;
 #pragma unroll
-      for (int j = 0; j < QT; ++j) top[j] = -INFINITY;
+        for (int j = 0; j < QT; ++j) {
+          top[j] = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < F::NU; ++u)
+          for (int u = 0; u < F::NU; ++u)
 #pragma unroll
-        for (int i = 0; i < H::SUB; ++i) {
-          const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+            for (int i = 0; i < H::SUB; ++i)
 #pragma unroll
-          for (int j = 0; j < QT; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float x = s[u][i][j][r] * a.c;
-              if (!all) x = bits >> r & 1 ? x : -INFINITY;
-              s[u][i][j][r] = x;
-              top[j] = fmaxf(top[j], x);
-            }
+              for (int r = 0; r < 4; ++r) top[j] = fmaxf(top[j], s[u][i][j][r]);
+          top[j] *= a.c;
+          far |= !(fabsf(top[j]) < 0x1p20f);
         }
+        plain = !__any(far);
+      }
+      if (!plain) {
+        c = 1.f;
+#pragma unroll
+        for (int j = 0; j < QT; ++j) top[j] = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < F::NU; ++u)
+#pragma unroll
+          for (int i = 0; i < H::SUB; ++i) {
+            const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+#pragma unroll
+            for (int j = 0; j < QT; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float x = bits >> r & 1 ? s[u][i][j][r] * a.c : -INFINITY;
+                s[u][i][j][r] = x;
+                top[j] = fmaxf(top[j], x);
+              }
+          }
+      }
       bool rise = false;
 #pragma unroll
       for (int j = 0; j < QT; ++j) {
@@ -154,7 +179,7 @@ __global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
           for (int i = 0; i < H::SUB; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              p[i][r] = __builtin_amdgcn_exp2f(s[u][i][j][r] - ref);
+              p[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i][j][r], c, -ref));
               l[j] += p[i][r];
             }
           w[u][j] = weights<T, H::SUB>(p);
@@ -163,11 +188,15 @@ __global__ void __launch_bounds__(256) k_attend_fwd(AttendArgs a) {
 #pragma unroll
       for (int u = 0; u < F::NU; ++u) sums<T, DP, QT>(o, vt, wk * F::KW + u * H::UNIT, l16, lq, w[u]);
     }
-    __syncthreads();
+    if constexpr (F::STAGES == 1) {
+      __syncthreads();
+      if (k0 + F::KT < kend) go(k0 + F::KT, n + 1);
+    }
   }
 #pragma unroll
   for (int j = 0; j < QT; ++j) l[j] = rows_sum(l[j]);
   if constexpr (WK == 4) {
+    __syncthreads();                                   // (every wave has read its last tile)
     // the waves' parts, [wave][16][DP + 4], and their references and sums, [wave][2][16], in the tiles' place
     float *po = (float*)sm, *pm = po + 4 * 16 * (DP + 4);
     float* mine = po + (wave * 16 + l16) * (DP + 4) + 4 * lq;
@@ -296,19 +325,23 @@ extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, c
   return attend_dispatch(d, [&](auto t, auto dp) {
     typedef decltype(t) T;
     constexpr int DP = decltype(dp)::value;
-    hipError_t e;
-    if (p.wk == 4) {
+    auto run = [&](auto dma) {
+      constexpr bool DMA = decltype(dma)::value;
+      // (fp32 heads of 256 by way of registers: four waves' keys would not fit; the one tile of rows is one either way)
+      if constexpr (DMA || sizeof(T) * DP <= 512) {
+        if (p.wk == 4) {
+          static std::atomic<uint64_t> dev;
+          return attend_launch(k_attend_fwd<T, DP, 1, 4, DMA>, a, groups, Fwd<T, DP, 4, DMA>::LDS, dev, st);
+        }
+      }
+      if (DP > 128 || p.qt == 1) {
+        static std::atomic<uint64_t> dev;
+        return attend_launch(k_attend_fwd<T, DP, 1, 1, DMA>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+      }
       static std::atomic<uint64_t> dev;
-      e = attend_launch(k_attend_fwd<T, DP, 1, 4>, a, groups, Fwd<T, DP, 4>::LDS, dev, st);
-    } else if (p.qt == 1) {
-      static std::atomic<uint64_t> dev;
-      e = attend_launch(k_attend_fwd<T, DP, 1, 1>, a, groups, Fwd<T, DP, 1>::LDS, dev, st);
-    } else if constexpr (DP <= 128) {
-      static std::atomic<uint64_t> dev;
-      e = attend_launch(k_attend_fwd<T, DP, 2, 1>, a, groups, Fwd<T, DP, 1>::LDS, dev, st);
-    } else {
-      e = hipErrorInvalidValue;
-    }
+      return attend_launch(k_attend_fwd<T, DP, (DP > 128 ? 1 : 2), 1, DMA>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+    };
+    hipError_t e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     if (e == hipSuccess && p.splits > 1) {
       in_pieces((int64_t)d->B * d->Tq * d->Hq, 4 * kMostGroups, [&](int64_t r0, int64_t n) {
         a.first = r0;
