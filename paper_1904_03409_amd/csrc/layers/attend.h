@@ -26,10 +26,11 @@ struct AttendArgs {
   float* stats;                                        // [B, Hq, Tq, 2]: reference of the row's exponents (base 2), 1 / sum
   const float* stats_in;
   float *delta;                                        // [B, Hq, Tq]: dy . y
-  float *part, *ml;                                    // splits: [splits][B Hk][rows][D] sums, [splits][B Hk][rows][2] references and sums
+  // splits: [splits][B Hk][rows][D] sums, [splits][B Hk][rows][2] references and sums; of dk and dv [splits][2][B Hk][Tk][D]
+  float *part, *ml;
   int tiles, splits, chunk;                            // row tiles of a (sequence, key head); keys of a split
   int64_t first;                                       // a launch's first workgroup
-  int64_t groups;                                      // all of them
+  int64_t piece, full;                                 // neighbours on an XCD; how many are dealt out that way
 };
 
 template <typename T> struct frag_of { typedef f32x4 type; };
@@ -46,15 +47,21 @@ struct Head {
 };
 
 // Rows of a tile lie densely in LDS; 16-byte granule c of row r is at place c ^ swz(r) of its row, so that neither the 16 rows of a
-// score's fragment nor the rows of a transposed one meet in a bank. bf16: fragments take rows 0 .. 3, 8 .. 11, 16 .. 19, 24 .. 27 (+ 4) of a unit;
-// a transposed read takes pairs of granules of eight of them. fp32: rows 0 .. 15; every fourth row, four granules.
+// score's fragment nor the rows of a transposed one meet in a bank. A 16-byte read is served in four parts: lanes 0 .. 3, 12 .. 15,
+// 20 .. 23, 24 .. 27 are one of them (with parts of 16 neighbours in mind a read took 8 cycles instead of 4). bf16: fragments take
+// rows 0 .. 3, 8 .. 11, 16 .. 19, 24 .. 27 (+ 4) of a unit; a transposed read takes pairs of granules of eight of them. fp32: rows 0 .. 15;
+// every fourth row, four granules.
 template <typename T, int GPR>
 __device__ __forceinline__ int swz(int r) {
   if constexpr (sizeof(T) == 4) return GPR >= 16 ? r & 15 : (r >> 1) & 7;
-  else if constexpr (GPR >= 16) return (r & 3) << 1 | (r & 8) | (r >> 4 & 1);
-  else if constexpr (GPR == 8) return (r & 2) | (r >> 1 & 4) | (r >> 4 & 1);
-  else return (r >> 2 & 2) | (r >> 4 & 1);
+  else if constexpr (GPR >= 16) return (r & 3) << 1 | (r & 8);
+  else if constexpr (GPR == 8) return (r & 2) | (r >> 1 & 4);
+  else return r >> 2 & 2;
 }
+
+// The same for rows that are read 16 neighbours at a time.
+template <int GPR>
+__device__ __forceinline__ int own_swz(int r) { return GPR >= 16 ? r & 15 : GPR == 8 ? (r >> 1) & 7 : (r >> 2) & 3; }
 
 // Tile row (of a unit) that row i of score tile `sub` is; the four rows of a lane's result are row_of(sub, 4 lq) + 0 .. 3.
 template <typename T>
@@ -96,18 +103,30 @@ __device__ __forceinline__ void scores(f32x4 (&acc)[N], const unsigned char* til
   }
 }
 
-// A unit's results as the second product's fragment.
-template <typename T, int SUB>
-__device__ __forceinline__ frag_t<T> weights(const f32x4 (&p)[SUB]) {
-  if constexpr (sizeof(T) == 2) {
-    bf16x8 r;
+// The same with own rows in LDS too (16 j + l16 of `own`).
+template <typename T, int DP, int N>
+__device__ __forceinline__ void scores_lds(f32x4 (&acc)[N], const unsigned char* tile, int base, int sub, int l16, int lq,
+                                           const unsigned char* own) {
+  typedef Head<T, DP> H;
+  const int row = row_of<T>(sub, l16);
+  own += opaque(l16 * H::BYTES);                       // (read for every tile: the compiler would keep them in registers)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = static_cast<__bf16>(p[i >> 2][i & 3]);
-    return r;
-  } else {
-    return p[0];
+  for (int s = 0; s < H::STEPS; ++s) {
+    const typename H::frag a = *(const typename H::frag*)(tile + (base + row) * H::BYTES + ((4 * s + lq) ^ swz<T, H::GPR>(row)) * 16);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const typename H::frag b = *(const typename H::frag*)(own + 16 * j * H::BYTES + ((4 * s + lq) ^ own_swz<H::GPR>(l16)) * 16);
+      acc[j] = mfma_bf16_16x16x32(a, b, acc[j]);
+    }
   }
 }
+
+// A unit's results as the second product's fragment: score tile `sub` of it.
+__device__ __forceinline__ void put_weights(bf16x8& w, int sub, const f32x4& p) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) w[4 * sub + r] = static_cast<__bf16>(p[r]);
+}
+__device__ __forceinline__ void put_weights(f32x4& w, int, const f32x4& p) { w = p; }
 // acc[j][dt] += (columns 16 dt .. of unit row `base` on)^T times the weights w[j].
 template <typename T, int DP, int N>
 __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq,
@@ -140,15 +159,15 @@ __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned ch
 
 // ROWS rows on their way from memory to LDS: zeros where a row is not there and past a head's end. With DMA straight to LDS (rows
 // of whole, aligned granules), else through registers: go() starts a tile, land() puts it in place.
-template <typename T, int DP, int ROWS, bool DMA>
+template <typename T, int DP, int ROWS, bool DMA, int NT = 256>
 struct Mover {
   typedef Head<T, DP> H;
-  static constexpr int ALL = ROWS * H::GPR, I = (ALL + 255) / 256;
-  static_assert(!DMA || ALL % 256 == 0, "whole waves");
+  static constexpr int ALL = ROWS * H::GPR, I = (ALL + NT - 1) / NT;
+  static_assert(!DMA || ALL % NT == 0, "whole waves");
   u32x4 r[DMA ? 1 : I];
   uint32_t off[DMA ? I : 1];
   static __device__ __forceinline__ void place(int i, int& row, int& c) {
-    const int L = i * 256 + threadIdx.x;
+    const int L = i * NT + threadIdx.x;
     row = L / H::GPR;
     c = (L % H::GPR) ^ swz<T, H::GPR>(row);
   }
@@ -176,7 +195,7 @@ struct Mover {
           place(i, row, c);
           if (row >= n || !mask[row]) o = kOOB;
         }
-        bdma16(rs, o, 0, lds_addr(tile + (i * 4 + wave) * 1024));
+        bdma16(rs, o, 0, lds_addr(tile + (i * (NT / 64) + wave) * 1024));
       }
     } else {
       const bool whole = D % H::V == 0;
@@ -197,8 +216,8 @@ struct Mover {
     if constexpr (!DMA) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        const int L = i * 256 + threadIdx.x;
-        if (ALL % 256 == 0 || L < ALL) *(u32x4*)(tile + L * 16) = r[i];
+        const int L = i * NT + threadIdx.x;
+        if (ALL % NT == 0 || L < ALL) *(u32x4*)(tile + L * 16) = r[i];
       }
     }
   }
@@ -229,21 +248,21 @@ __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
 __device__ __forceinline__ float rows_max(float v) { return half_swap(row_swap(v, op_max()), op_max()); }
 __device__ __forceinline__ float rows_sum(float v) { return half_swap(row_swap(v, op_sum()), op_sum()); }
 
-// Workgroup -> (sequence and key head, split, row tile): workgroups go to the 8 XCDs in turn, and an XCD takes a contiguous run, so
-// that the row tiles that share keys find them in its L2.
+// Workgroup -> (sequence and key head, split, row tile). Workgroups go to the 8 XCDs in turn; an XCD takes every eighth run of
+// `piece` of them, so that row tiles that share keys find them in its L2, and sequences of other lengths are spread over the XCDs.
 struct Place {
   int bh, split, tile;
 };
 __device__ __forceinline__ Place place_of(const AttendArgs& a) {
-  int64_t id = a.first + blockIdx.x;
-  const int64_t full = a.groups & ~(int64_t)7;
-  if (id < full) id = (id & 7) * (full >> 3) + (id >> 3);
+  // (32 bits: 64-bit divisions took 4 us of every workgroup's start)
+  uint32_t id = (uint32_t)a.first + blockIdx.x;
+  const uint32_t piece = (uint32_t)a.piece, run = (id >> 3) / piece;
+  if (id < (uint32_t)a.full) id = (run * 8 + (id & 7)) * piece + ((id >> 3) - run * piece);
   Place p;
-  const int64_t per = (int64_t)a.tiles * a.splits;
-  p.bh = (int)(id / per);
-  const int rest = (int)(id - p.bh * per);
-  p.split = rest / a.tiles;
-  p.tile = rest % a.tiles;
+  const uint32_t per = (uint32_t)a.tiles * (uint32_t)a.splits, bh = id / per, rest = id - bh * per;
+  p.bh = (int)bh;
+  p.split = a.splits == 1 ? 0 : (int)(rest / (uint32_t)a.tiles);
+  p.tile = (int)(rest - (uint32_t)p.split * (uint32_t)a.tiles);
   return p;
 }
 
@@ -333,15 +352,19 @@ inline bool dma_ok(const slstm_attend_dims* d, const void* p, const slstm_stride
 }
 // All workgroups of a kernel, in as many launches as they need.
 template <typename K>
-hipError_t attend_launch(K kern, AttendArgs a, int64_t groups, int lds, std::atomic<uint64_t>& devices, hipStream_t st) {
+hipError_t attend_launch(K kern, AttendArgs a, int64_t groups, int lds, std::atomic<uint64_t>& devices, hipStream_t st, int threads = 256) {
   if (lds > 65536) {
     const hipError_t e = allow_lds((const void*)kern, lds, devices);
     if (e != hipSuccess) return e;
   }
-  a.groups = groups;
+  // about eight runs to an XCD: of whole sequences (whose heads lie in the same cache lines) where there are 8 of them, of parts of a head's
+  // tiles where there are few heads
+  const int64_t per = (int64_t)a.tiles * a.splits, heads = (int64_t)a.B * a.Hk;
+  a.piece = a.B >= 8 ? per * a.Hk * (a.B >= 128 ? a.B / 64 : 1) : heads >= 64 ? per * (heads / 64) : (per + 64 / heads - 1) / (64 / heads);
+  a.full = groups / (8 * a.piece) * (8 * a.piece);
   in_pieces(groups, kMostGroups, [&](int64_t g0, int64_t n) {
     a.first = g0;
-    hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(256), (size_t)lds, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(threads), (size_t)lds, st, a);
   });
   return hipGetLastError();
 }

@@ -24,6 +24,15 @@ struct Bwd {
   static constexpr int WDKV = H::BYTES <= 128 ? 2 : 1;
 };
 
+// A workgroup of k_attend_dkv. BIG: eight waves with 32 keys each, whose values stay in LDS (their registers leave room for two
+// waves on a SIMD that way: bf16 heads of 128; with everything in registers one wave has 337).
+template <typename T, int DP, bool DMA, bool BIG>
+struct Keys {
+  typedef Bwd<T, DP, DMA> F;
+  static constexpr int NT = BIG ? 512 : 256, N = BIG ? 2 : F::QT, ALL = NT / 4 * N, WAVES = BIG ? 2 : F::WDKV;
+  static constexpr int LDS = F::LDS + (BIG ? ALL * F::H::BYTES : 0);
+};
+
 }  // namespace
 
 template <typename T, int DP, bool DMA>
@@ -93,29 +102,26 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
     if (k0 + F::R < kend) go(k0 + F::R, n + 1);
 #pragma unroll
     for (int u = 0; u < F::NU; ++u) {
-      f32x4 s[H::SUB][QT], dp[H::SUB][QT];
-#pragma unroll
-      for (int i = 0; i < H::SUB; ++i) {
-#pragma unroll
-        for (int j = 0; j < QT; ++j) s[i][j] = dp[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        scores<T, DP, QT>(s[i], kt, u * H::UNIT, i, l16, lq, q);
-        scores<T, DP, QT>(dp[i], vt, u * H::UNIT, i, l16, lq, g);
-      }
       frag w[QT];
 #pragma unroll
-      for (int j = 0; j < QT; ++j) {
-        f32x4 ds[H::SUB];
+      for (int i = 0; i < H::SUB; ++i) {
+        f32x4 s[QT], dp[QT];
 #pragma unroll
-        for (int i = 0; i < H::SUB; ++i) {
-          const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+        for (int j = 0; j < QT; ++j) s[j] = dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        scores<T, DP, QT>(s, kt, u * H::UNIT, i, l16, lq, q);
+        scores<T, DP, QT>(dp, vt, u * H::UNIT, i, l16, lq, g);
+        const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+          f32x4 ds;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float x = bits >> r & 1 ? s[i][j][r] * a.c : -INFINITY;
+            const float x = bits >> r & 1 ? s[j][r] * a.c : -INFINITY;
             const float p = __builtin_amdgcn_exp2f(x - m[j]) * inv[j];
-            ds[i][r] = p * (dp[i][j][r] - delta[j]);
+            ds[r] = p * (dp[j][r] - delta[j]);
           }
+          put_weights(w[j], i, ds);
         }
-        w[j] = weights<T, H::SUB>(ds);
       }
       sums<T, DP, QT>(o, kt, u * H::UNIT, l16, lq, w);
     }
@@ -130,12 +136,13 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
   }
 }
 
-template <typename T, int DP, bool DMA>
-__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDKV)) k_attend_dkv(AttendArgs a) {
+template <typename T, int DP, bool DMA, bool BIG>
+__global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA, BIG>::WAVES)) k_attend_dkv(AttendArgs a) {
   typedef Head<T, DP> H;
   typedef Bwd<T, DP, DMA> F;
   typedef frag_t<T> frag;
-  constexpr int KN = F::QT;
+  typedef Keys<T, DP, DMA, BIG> K;
+  constexpr int KN = K::N;
   extern __shared__ __align__(16) unsigned char sm[];
   float* stats = (float*)(sm + 4 * F::TILE);           // two stages of [3][R]: m, 1 / l, delta
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
@@ -143,44 +150,61 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDKV)) k_attend_dkv(Att
   const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk);
   const int qlen = clamp_len(a.q_len, b, a.Tq), klen = clamp_len(a.k_len, b, a.Tk);
   // (no key of the tile is there: no queries)
-  const int qend = pl.tile * F::OWN < klen ? qlen : 0;
+  const int qend = pl.tile * K::ALL < klen ? qlen : 0;
   int key[KN];
   bool there[KN];
-  frag k[KN][H::STEPS], v[KN][H::STEPS];
+  frag k[KN][H::STEPS], v[BIG ? 1 : KN][H::STEPS];
+  unsigned char* own = sm + F::LDS + wave * 16 * KN * H::BYTES;          // BIG: the wave's values
 #pragma unroll
   for (int j = 0; j < KN; ++j) {
-    key[j] = pl.tile * F::OWN + 16 * (KN * wave + j) + l16;
+    key[j] = pl.tile * K::ALL + 16 * (KN * wave + j) + l16;
     there[j] = key[j] < klen && (!a.mask || a.mask[(int64_t)b * a.Tk + key[j]]);
     load_own<T, DP>((const T*)a.k + (int64_t)b * a.sk.b + (int64_t)key[j] * a.sk.t + (int64_t)hk * a.sk.h, there[j], a.D, lq, k[j]);
-    load_own<T, DP>((const T*)a.v + (int64_t)b * a.sv.b + (int64_t)key[j] * a.sv.t + (int64_t)hk * a.sv.h, there[j], a.D, lq, v[j]);
+    load_own<T, DP>((const T*)a.v + (int64_t)b * a.sv.b + (int64_t)key[j] * a.sv.t + (int64_t)hk * a.sv.h, there[j], a.D, lq, v[BIG ? 0 : j]);
+    if constexpr (BIG) {
+#pragma unroll
+      for (int s = 0; s < H::STEPS; ++s)
+        *(frag*)(own + (16 * j + l16) * H::BYTES + ((4 * s + lq) ^ own_swz<H::GPR>(l16)) * 16) = v[0][s];
+    }
   }
   f32x4 dk[KN][H::DT], dv[KN][H::DT];
 #pragma unroll
   for (int j = 0; j < KN; ++j)
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) dk[j][dt] = dv[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Mover<T, DP, F::R, DMA> mq, mg;
+  Mover<T, DP, F::R, DMA, K::NT> mq, mg;
   mq.start(a.sq.t, a.D);
   mg.start(a.sdy.t, a.D);
   float tm = 0.f, ti = 0.f, td = 0.f;
   // tiles of the first head's queries, then of the next one's
-  const int tiles = (qend + F::R - 1) / F::R, all = tiles * a.G;
+  const int tiles = (qend + F::R - 1) / F::R;
+  int n0 = 0, all = tiles * a.G;
+  int h = hk * a.G, t0 = 0;                            // of the next tile to go
+  if (a.splits > 1 && all > 0) {
+    const int each = all / a.splits, more = all - each * a.splits;
+    n0 = uni(each * pl.split + min(pl.split, more));
+    all = uni(n0 + each + (pl.split < more ? 1 : 0));
+    h += uni(n0 / tiles);
+    t0 = uni(n0 % tiles) * F::R;
+  }
   auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
   auto go = [&](int n) {
-    const int h = hk * a.G + n / tiles, t0 = n % tiles * F::R;
     mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
     mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
           stage(n) + F::TILE);
     if (tid < F::R) {
       tm = INFINITY, ti = td = 0.f;
       if (t0 + tid < qend) {
-        const int64_t at = ((int64_t)b * a.Hq + h) * a.Tq + t0 + tid;
-        tm = a.stats_in[2 * at], ti = a.stats_in[2 * at + 1], td = a.delta[at];
+        const int64_t row = ((int64_t)b * a.Hq + h) * a.Tq + t0;
+        const float *st = a.stats_in + 2 * row, *de = a.delta + row;
+        tm = st[2 * tid], ti = st[2 * tid + 1], td = de[tid];
       }
     }
+    t0 += F::R;
+    if (t0 >= qend) t0 = 0, ++h;
   };
-  if (all) go(0);
-  for (int n = 0; n < all; ++n) {
+  if (n0 < all) go(n0);
+  for (int n = n0; n < all; ++n) {
     const unsigned char *qt = stage(n), *gt = qt + F::TILE;
     float* st = stats + (n & 1) * 3 * F::R;
     if constexpr (DMA) wait_vm<0>();
@@ -190,31 +214,29 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDKV)) k_attend_dkv(Att
     if (n + 1 < all) go(n + 1);
 #pragma unroll
     for (int u = 0; u < F::NU; ++u) {
-      f32x4 s[H::SUB][KN], dp[H::SUB][KN];
-#pragma unroll
-      for (int i = 0; i < H::SUB; ++i) {
-#pragma unroll
-        for (int j = 0; j < KN; ++j) s[i][j] = dp[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        scores<T, DP, KN>(s[i], qt, u * H::UNIT, i, l16, lq, k);
-        scores<T, DP, KN>(dp[i], gt, u * H::UNIT, i, l16, lq, v);
-      }
       frag wp[KN], ws[KN];
 #pragma unroll
-      for (int j = 0; j < KN; ++j) {
-        f32x4 p[H::SUB], ds[H::SUB];
+      for (int i = 0; i < H::SUB; ++i) {
+        f32x4 s[KN], dp[KN];
 #pragma unroll
-        for (int i = 0; i < H::SUB; ++i) {
-          const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
-          const f32x4 m = *(const f32x4*)(st + at), inv = *(const f32x4*)(st + F::R + at), delta = *(const f32x4*)(st + 2 * F::R + at);
+        for (int j = 0; j < KN; ++j) s[j] = dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        scores<T, DP, KN>(s, qt, u * H::UNIT, i, l16, lq, k);
+        if constexpr (BIG) scores_lds<T, DP, KN>(dp, gt, u * H::UNIT, i, l16, lq, own);
+        else scores<T, DP, KN>(dp, gt, u * H::UNIT, i, l16, lq, v);
+        const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
+        const f32x4 m = *(const f32x4*)(st + at), inv = *(const f32x4*)(st + F::R + at), delta = *(const f32x4*)(st + 2 * F::R + at);
+#pragma unroll
+        for (int j = 0; j < KN; ++j) {
+          f32x4 p, ds;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float x = there[j] ? s[i][j][r] * a.c : -INFINITY;
-            p[i][r] = __builtin_amdgcn_exp2f(x - m[r]) * inv[r];
-            ds[i][r] = p[i][r] * (dp[i][j][r] - delta[r]);
+            const float x = there[j] ? s[j][r] * a.c : -INFINITY;
+            p[r] = __builtin_amdgcn_exp2f(x - m[r]) * inv[r];
+            ds[r] = p[r] * (dp[j][r] - delta[r]);
           }
+          put_weights(wp[j], i, p);
+          put_weights(ws[j], i, ds);
         }
-        wp[j] = weights<T, H::SUB>(p);
-        ws[j] = weights<T, H::SUB>(ds);
       }
       sums<T, DP, KN>(dv, gt, u * H::UNIT, l16, lq, wp);
       sums<T, DP, KN>(dk, qt, u * H::UNIT, l16, lq, ws);
@@ -223,9 +245,20 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDKV)) k_attend_dkv(Att
 #pragma unroll
   for (int j = 0; j < KN; ++j) {
     if (key[j] >= a.Tk) continue;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (a.splits > 1) {
+      const int64_t all = (int64_t)a.B * a.Hk * a.Tk * a.D;
+      float* p = a.part + (int64_t)pl.split * 2 * all + ((int64_t)pl.bh * a.Tk + key[j]) * a.D;
+#pragma unroll
+      for (int dt = 0; dt < H::DT; ++dt) {
+        if (16 * dt + 4 * lq >= a.D) continue;
+        store4(p, 16 * dt + 4 * lq, a.D, there[j] ? dk[j][dt] * a.scale : zero);
+        store4(p + all, 16 * dt + 4 * lq, a.D, there[j] ? dv[j][dt] : zero);
+      }
+      continue;
+    }
     T* ok = (T*)a.dk + (int64_t)b * a.sdk.b + (int64_t)key[j] * a.sdk.t + (int64_t)hk * a.sdk.h;
     T* ov = (T*)a.dv + (int64_t)b * a.sdv.b + (int64_t)key[j] * a.sdv.t + (int64_t)hk * a.sdv.h;
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) {
       if (16 * dt + 4 * lq >= a.D) continue;
@@ -235,9 +268,53 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDKV)) k_attend_dkv(Att
   }
 }
 
+// dk and dv from their splits: four elements of a head to a thread, blockIdx.y: dk, dv.
+template <typename T>
+__global__ void __launch_bounds__(256) k_attend_join_dkv(AttendArgs a) {
+  const int per = (a.D + 3) / 4;
+  const int64_t id = (a.first + blockIdx.x) * 256 + threadIdx.x, row = id / per, rows = (int64_t)a.B * a.Hk * a.Tk;
+  if (row >= rows) return;
+  const int n = (int)(id % per) * 4, bh = (int)(row / a.Tk), t = (int)(row % a.Tk), left = a.D - n;
+  const float* p = a.part + ((int64_t)blockIdx.y * rows + row) * a.D;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < a.splits; ++i, p += 2 * rows * a.D) {
+    float v[4];
+    vec<float>::unpack(load_vec(p, n / 4, a.D), v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] += v[k];
+  }
+  const slstm_strides st = blockIdx.y ? a.sdv : a.sdk;
+  T* to = (T*)(blockIdx.y ? a.dv : a.dk) + (int64_t)(bh / a.Hk) * st.b + (int64_t)t * st.t + (int64_t)(bh % a.Hk) * st.h;
+  if (left > 0) store4(to, n, a.D, f32x4{s[0], s[1], s[2], s[3]});
+}
+
+namespace {
+
+// Keys of a workgroup of k_attend_dkv, and splits of its queries. 256 keys with eight waves (Keys) where they are there;
+// queries are split, 256 of them at least to each part, until there are two workgroups to a compute unit (2 sequences of 4096 x 4000, 4 key
+// heads of 128, of unequal lengths: TIMES).
+struct KeyPlan {
+  bool big;
+  int tiles, splits;
+};
+KeyPlan key_plan(const slstm_attend_dims* d) {
+  KeyPlan p;
+  p.big = d->type == SLSTM_BF16 && d->D > 64 && d->D <= 128 && d->Tk > 128;
+  const int keys = p.big ? 256 : d->D > 128 || (d->D > 64 && d->type == SLSTM_F32) ? 64 : 128;
+  p.tiles = (d->Tk + keys - 1) / keys;
+  const int64_t groups = std::max<int64_t>(1, (int64_t)p.tiles * d->B * d->Hk), most = (int64_t)d->Tq * (d->Hq / d->Hk) / 256;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / groups, most), 64));
+  return p;
+}
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
 extern "C" size_t stacklstm_attend_bwd_workspace_bytes(const slstm_attend_dims* d) {
   if (!attend_ok(d)) return 0;
-  return (size_t)d->B * d->Tq * d->Hq * 4 + 16;
+  const KeyPlan p = key_plan(d);
+  const size_t delta = up256((size_t)d->B * d->Tq * d->Hq * 4 + 16);
+  return p.splits > 1 ? delta + (size_t)p.splits * 2 * d->B * d->Hk * d->Tk * d->D * 4 : delta;
 }
 
 extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, const void* k, const void* v, const int32_t* q_len,
@@ -258,6 +335,8 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
   AttendArgs a = attend_args(d);
   a.q = q, a.k = k, a.v = v, a.q_len = q_len, a.k_len = k_len, a.mask = mask, a.y = y, a.stats_in = stats, a.dy = dy;
   a.dq = dq, a.dk = dk, a.dv = dv, a.delta = (float*)workspace;
+  a.part = (float*)((char*)workspace + up256((size_t)d->B * d->Tq * d->Hq * 4 + 16));
+  const KeyPlan plan = key_plan(d);
   const hipStream_t st = as_stream(stream);
   return attend_dispatch(d, [&](auto t, auto dp) {
     typedef decltype(t) T;
@@ -273,13 +352,33 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
       e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     }
     if (e == hipSuccess && d->Tk) {
+      a.splits = plan.splits;
+      auto go = [&](auto kern, int keys, int threads, int lds, std::atomic<uint64_t>& dev) {
+        a.tiles = (d->Tk + keys - 1) / keys;
+        return attend_launch(kern, a, (int64_t)a.tiles * d->B * d->Hk * a.splits, lds, dev, st, threads);
+      };
       auto run = [&](auto dma) {
-        typedef Bwd<T, DP, decltype(dma)::value> F;
+        constexpr bool DMA = decltype(dma)::value;
+        if constexpr (DMA && sizeof(T) == 2 && DP == 128) {
+          if (plan.big) {
+            typedef Keys<T, DP, DMA, true> K;
+            static std::atomic<uint64_t> dev;
+            return go(k_attend_dkv<T, DP, DMA, true>, K::ALL, K::NT, K::LDS, dev);
+          }
+        }
+        typedef Keys<T, DP, DMA, false> K;
         static std::atomic<uint64_t> dev;
-        a.tiles = (d->Tk + F::OWN - 1) / F::OWN;
-        return attend_launch(k_attend_dkv<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk, F::LDS, dev, st);
+        return go(k_attend_dkv<T, DP, DMA, false>, K::ALL, K::NT, K::LDS, dev);
       };
       e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? run(std::true_type()) : run(std::false_type());
+    }
+    if (e == hipSuccess && d->Tk && a.splits > 1) {
+      const int64_t blocks = ((int64_t)d->B * d->Hk * d->Tk * ((d->D + 3) / 4) + 255) / 256;
+      in_pieces(blocks, kMostGroups, [&](int64_t b0, int64_t n) {
+        a.first = b0;
+        hipLaunchKernelGGL(k_attend_join_dkv<T>, dim3((unsigned)n, 2), dim3(256), 0, st, a);
+      });
+      e = hipGetLastError();
     }
     return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
   });

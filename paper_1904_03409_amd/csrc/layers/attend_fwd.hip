@@ -174,15 +174,16 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
         const float ref = m[j] == -INFINITY ? 0.f : m[j];
 #pragma unroll
         for (int u = 0; u < F::NU; ++u) {
-          f32x4 p[H::SUB];
 #pragma unroll
-          for (int i = 0; i < H::SUB; ++i)
+          for (int i = 0; i < H::SUB; ++i) {
+            f32x4 p;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              p[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i][j][r], c, -ref));
-              l[j] += p[i][r];
+              p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i][j][r], c, -ref));
+              l[j] += p[r];
             }
-          w[u][j] = weights<T, H::SUB>(p);
+            put_weights(w[u][j], i, p);
+          }
         }
       }
 #pragma unroll
