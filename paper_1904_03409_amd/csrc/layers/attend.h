@@ -69,17 +69,36 @@ __device__ __forceinline__ int row_of(int sub, int i) {
   return sizeof(T) == 2 ? 8 * (i >> 2) + 4 * sub + (i & 3) : i;
 }
 
-// Fragments of a wave's own row: 16 bytes of every 64.
+// Granule c of a row of D elements, in two parts as load_vec's: the load (in bounds whatever c is) and the granule's place, zeros
+// past the row's end. No load waits for a branch.
+template <typename T>
+__device__ __forceinline__ u32x4 fetch_granule(const T* row, int c, int D) {
+  if (D < vec<T>::N) return c == 0 ? load_vec(row, 0, D) : u32x4{0u, 0u, 0u, 0u};
+  return *(const u32x4_any*)(row + min(c * vec<T>::N, D - vec<T>::N));
+}
+template <typename T>
+__device__ __forceinline__ u32x4 place_granule(u32x4 v, int c, int D, bool there) {
+  constexpr int V = vec<T>::N;
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  if (D % V == 0 || D < V) return there && c * V < D ? v : zero;
+  v = shift_vec<T>(v, min(c * V - min(c * V, D - V), V));
+  return there ? v : zero;
+}
+// Fragments of a wave's own row: 16 bytes of every 64, zeros where it is not there (what is padding is not read). In two parts:
+// all of a workgroup's first loads are on their way before the first of them is waited for.
 template <typename T, int DP>
-__device__ __forceinline__ void load_own(const T* row, bool here, int D, int lq, frag_t<T> (&f)[Head<T, DP>::STEPS]) {
-  typedef Head<T, DP> H;
+__device__ __forceinline__ void fetch_own(const T* row, bool there, int D, int lq, u32x4 (&r)[Head<T, DP>::STEPS]) {
 #pragma unroll
-  for (int s = 0; s < H::STEPS; ++s) {
-    const int c = 4 * s + lq;
-    u32x4 r = {0u, 0u, 0u, 0u};
-    if (here && c * H::V < D) r = load_vec(row, c, D);
-    f[s] = __builtin_bit_cast(typename H::frag, r);
+  for (int s = 0; s < Head<T, DP>::STEPS; ++s) r[s] = u32x4{0u, 0u, 0u, 0u};
+  if (there) {
+#pragma unroll
+    for (int s = 0; s < Head<T, DP>::STEPS; ++s) r[s] = fetch_granule(row, 4 * s + lq, D);
   }
+}
+template <typename T, int DP>
+__device__ __forceinline__ void place_own(const u32x4 (&r)[Head<T, DP>::STEPS], int D, int lq, frag_t<T> (&f)[Head<T, DP>::STEPS]) {
+#pragma unroll
+  for (int s = 0; s < Head<T, DP>::STEPS; ++s) f[s] = __builtin_bit_cast(frag_t<T>, place_granule<T>(r[s], 4 * s + lq, D, true));
 }
 
 // acc += tile rows (of unit row `base`, a multiple of the unit, score tile sub) times own rows.
@@ -165,6 +184,8 @@ struct Mover {
   static constexpr int ALL = ROWS * H::GPR, I = (ALL + NT - 1) / NT;
   static_assert(!DMA || ALL % NT == 0, "whole waves");
   u32x4 r[DMA ? 1 : I];
+  uint32_t there[DMA ? 1 : I];                         // mask bytes
+  int rows;
   uint32_t off[DMA ? I : 1];
   static __device__ __forceinline__ void place(int i, int& row, int& c) {
     const int L = i * NT + threadIdx.x;
@@ -198,46 +219,55 @@ struct Mover {
         bdma16(rs, o, 0, lds_addr(tile + (i * (NT / 64) + wave) * 1024));
       }
     } else {
-      const bool whole = D % H::V == 0;
+      rows = n;
 #pragma unroll
       for (int i = 0; i < I; ++i) {
         int row, c;
         place(i, row, c);
-        r[i] = u32x4{0u, 0u, 0u, 0u};
-        if (row < n && c * H::V < D && (!mask || mask[row])) {
-          const T* p = base + row * stride;
-          if (whole) r[i] = *(const u32x4_any*)(p + c * H::V);
-          else r[i] = load_vec(p, c, D);
-        }
+        row = min(row, n - 1);
+        r[i] = fetch_granule(base + row * stride, c, D);
+        there[i] = mask ? mask[row] : 1u;
       }
     }
   }
-  __device__ __forceinline__ void land(unsigned char* tile) const {
+  __device__ __forceinline__ void land(int D, unsigned char* tile) const {
     if constexpr (!DMA) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
+        int row, c;
+        place(i, row, c);
         const int L = i * NT + threadIdx.x;
-        if (ALL % NT == 0 || L < ALL) *(u32x4*)(tile + L * 16) = r[i];
+        if (ALL % NT == 0 || L < ALL) *(u32x4*)(tile + L * 16) = place_granule<T>(r[i], c, D, row < rows && there[i]);
       }
     }
   }
 };
 
-// v to four neighbouring elements of a row from column n on.
 template <typename T>
-__device__ __forceinline__ void store4(T* row, int n, int D, const f32x4& v) {
-  if (n + 4 <= D) {
-    if constexpr (sizeof(T) == 4) {
-      *(u32x4_any*)(row + n) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-    } else {
-      typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-      *(u32x2_any*)(row + n) = u32x2_any{(uint32_t)f32_to_bf16_bits(v[0]) | (uint32_t)f32_to_bf16_bits(v[1]) << 16,
-                                         (uint32_t)f32_to_bf16_bits(v[2]) | (uint32_t)f32_to_bf16_bits(v[3]) << 16};
-    }
+__device__ __forceinline__ void store4(T* to, const f32x4& v) {
+  if constexpr (sizeof(T) == 4) {
+    *(u32x4_any*)to = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  } else {
+    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    *(u32x2_any*)to = u32x2_any{(uint32_t)f32_to_bf16_bits(v[0]) | (uint32_t)f32_to_bf16_bits(v[1]) << 16,
+                                (uint32_t)f32_to_bf16_bits(v[2]) | (uint32_t)f32_to_bf16_bits(v[3]) << 16};
+  }
+}
+// A row from a lane's columns 16 dt + 4 lq .., f(dt) their values.
+template <typename T, int DP, typename F>
+__device__ __forceinline__ void store_cols(T* row, int lq, int D, F f) {
+  if (D % 4 == 0) {
+#pragma unroll
+    for (int dt = 0; dt < DP / 16; ++dt)
+      if (16 * dt + 4 * lq < D) store4(row + 16 * dt + 4 * lq, f(dt));
   } else {
 #pragma unroll
-    for (int r = 0; r < 3; ++r)
-      if (n + r < D) from_f32(row[n + r], v[r]);
+    for (int dt = 0; dt < DP / 16; ++dt) {
+      const f32x4 v = f(dt);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (16 * dt + 4 * lq + r < D) from_f32(row[16 * dt + 4 * lq + r], v[r]);
+    }
   }
 }
 

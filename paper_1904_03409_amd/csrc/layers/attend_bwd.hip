@@ -49,31 +49,24 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
   const int kend = pl.tile * F::OWN / a.G < qlen ? klen : 0;
   int qt_[QT], qh_[QT];
   bool here[QT], used[QT];
-  frag q[QT][H::STEPS], g[QT][H::STEPS];
+  u32x4 qr[QT][H::STEPS], gr[QT][H::STEPS], yr[QT][H::STEPS];
   float m[QT], inv[QT], delta[QT];
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
     const int r = pl.tile * F::OWN + 16 * (QT * wave + j) + l16;
-    qt_[j] = r / a.G;
-    qh_[j] = hk * a.G + r % a.G;
     here[j] = r < rows;
+    const int in = min(r, rows - 1);
+    qt_[j] = in / a.G;
+    qh_[j] = hk * a.G + in % a.G;
     used[j] = here[j] && qt_[j] < qlen;
-    load_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h, used[j], a.D, lq, q[j]);
-    load_own<T, DP>((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)qt_[j] * a.sdy.t + (int64_t)qh_[j] * a.sdy.h, used[j], a.D, lq, g[j]);
-    frag y[H::STEPS];
-    load_own<T, DP>((const T*)a.y + (int64_t)b * a.sy.b + (int64_t)qt_[j] * a.sy.t + (int64_t)qh_[j] * a.sy.h, used[j], a.D, lq, y);
-    float d = 0.f;
-#pragma unroll
-    for (int s = 0; s < H::STEPS; ++s)
-#pragma unroll
-      for (int e = 0; e < H::V; ++e) d += (float)g[j][s][e] * (float)y[s][e];
-    const int64_t at = ((int64_t)b * a.Hq + qh_[j]) * a.Tq + qt_[j];
-    m[j] = used[j] ? a.stats_in[2 * at] : INFINITY;
-    inv[j] = used[j] ? a.stats_in[2 * at + 1] : 0.f;
-    // (a query without keys: nothing, whatever dy holds)
-    used[j] = inv[j] != 0.f;
-    delta[j] = used[j] ? rows_sum(d) : 0.f;
-    if (here[j] && lq == 0) a.delta[at] = delta[j];
+    fetch_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h, used[j], a.D, lq, qr[j]);
+    fetch_own<T, DP>((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)qt_[j] * a.sdy.t + (int64_t)qh_[j] * a.sdy.h, used[j], a.D, lq, gr[j]);
+    fetch_own<T, DP>((const T*)a.y + (int64_t)b * a.sy.b + (int64_t)qt_[j] * a.sy.t + (int64_t)qh_[j] * a.sy.h, used[j], a.D, lq, yr[j]);
+    m[j] = INFINITY, inv[j] = 0.f;
+    if (used[j]) {
+      const float* st = a.stats_in + (((int64_t)b * a.Hq + qh_[j]) * a.Tq + qt_[j]) * 2;
+      m[j] = st[0], inv[j] = st[1];
+    }
   }
   const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
   const T* vp = (const T*)a.v + (int64_t)b * a.sv.b + (int64_t)hk * a.sv.h;
@@ -93,11 +86,28 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (kend > 0) go(0, 0);
+  frag q[QT][H::STEPS], g[QT][H::STEPS];
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    place_own<T, DP>(qr[j], a.D, lq, q[j]);
+    place_own<T, DP>(gr[j], a.D, lq, g[j]);
+    frag y[H::STEPS];
+    place_own<T, DP>(yr[j], a.D, lq, y);
+    float d = 0.f;
+#pragma unroll
+    for (int s = 0; s < H::STEPS; ++s)
+#pragma unroll
+      for (int e = 0; e < H::V; ++e) d += (float)g[j][s][e] * (float)y[s][e];
+    // (a query without keys: nothing, whatever dy holds)
+    used[j] = inv[j] != 0.f;
+    delta[j] = used[j] ? rows_sum(d) : 0.f;
+    if (here[j] && lq == 0) a.delta[((int64_t)b * a.Hq + qh_[j]) * a.Tq + qt_[j]] = delta[j];
+  }
   for (int k0 = 0, n = 0; k0 < kend; k0 += F::R, ++n) {
     const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const unsigned long long there = __ballot(lane < F::R && k0 + lane < kend && (!mask || mask[k0 + lane]));
     if constexpr (DMA) wait_vm<0>();
-    else mk.land(stage(n)), mv.land(stage(n) + F::TILE);
+    else mk.land(a.D, stage(n)), mv.land(a.D, stage(n) + F::TILE);
     __syncthreads();
     if (k0 + F::R < kend) go(k0 + F::R, n + 1);
 #pragma unroll
@@ -130,9 +140,7 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
   for (int j = 0; j < QT; ++j) {
     if (!here[j]) continue;
     T* dq = (T*)a.dq + (int64_t)b * a.sdq.b + (int64_t)qt_[j] * a.sdq.t + (int64_t)qh_[j] * a.sdq.h;
-#pragma unroll
-    for (int dt = 0; dt < H::DT; ++dt)
-      if (16 * dt + 4 * lq < a.D) store4(dq, 16 * dt + 4 * lq, a.D, used[j] ? o[j][dt] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f});
+    store_cols<T, DP>(dq, lq, a.D, [&](int dt) { return used[j] ? o[j][dt] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f}; });
   }
 }
 
@@ -153,19 +161,15 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
   const int qend = pl.tile * K::ALL < klen ? qlen : 0;
   int key[KN];
   bool there[KN];
-  frag k[KN][H::STEPS], v[BIG ? 1 : KN][H::STEPS];
+  u32x4 kr[KN][H::STEPS], vr[KN][H::STEPS];
   unsigned char* own = sm + F::LDS + wave * 16 * KN * H::BYTES;          // BIG: the wave's values
 #pragma unroll
   for (int j = 0; j < KN; ++j) {
     key[j] = pl.tile * K::ALL + 16 * (KN * wave + j) + l16;
     there[j] = key[j] < klen && (!a.mask || a.mask[(int64_t)b * a.Tk + key[j]]);
-    load_own<T, DP>((const T*)a.k + (int64_t)b * a.sk.b + (int64_t)key[j] * a.sk.t + (int64_t)hk * a.sk.h, there[j], a.D, lq, k[j]);
-    load_own<T, DP>((const T*)a.v + (int64_t)b * a.sv.b + (int64_t)key[j] * a.sv.t + (int64_t)hk * a.sv.h, there[j], a.D, lq, v[BIG ? 0 : j]);
-    if constexpr (BIG) {
-#pragma unroll
-      for (int s = 0; s < H::STEPS; ++s)
-        *(frag*)(own + (16 * j + l16) * H::BYTES + ((4 * s + lq) ^ own_swz<H::GPR>(l16)) * 16) = v[0][s];
-    }
+    const int in = min(key[j], a.Tk - 1);
+    fetch_own<T, DP>((const T*)a.k + (int64_t)b * a.sk.b + (int64_t)in * a.sk.t + (int64_t)hk * a.sk.h, there[j], a.D, lq, kr[j]);
+    fetch_own<T, DP>((const T*)a.v + (int64_t)b * a.sv.b + (int64_t)in * a.sv.t + (int64_t)hk * a.sv.h, there[j], a.D, lq, vr[j]);
   }
   f32x4 dk[KN][H::DT], dv[KN][H::DT];
 #pragma unroll
@@ -204,11 +208,22 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
     if (t0 >= qend) t0 = 0, ++h;
   };
   if (n0 < all) go(n0);
+  frag k[KN][H::STEPS], v[BIG ? 1 : KN][H::STEPS];
+#pragma unroll
+  for (int j = 0; j < KN; ++j) {
+    place_own<T, DP>(kr[j], a.D, lq, k[j]);
+    place_own<T, DP>(vr[j], a.D, lq, v[BIG ? 0 : j]);
+    if constexpr (BIG) {
+#pragma unroll
+      for (int s = 0; s < H::STEPS; ++s)
+        *(frag*)(own + (16 * j + l16) * H::BYTES + ((4 * s + lq) ^ own_swz<H::GPR>(l16)) * 16) = v[0][s];
+    }
+  }
   for (int n = n0; n < all; ++n) {
     const unsigned char *qt = stage(n), *gt = qt + F::TILE;
     float* st = stats + (n & 1) * 3 * F::R;
     if constexpr (DMA) wait_vm<0>();
-    else mq.land(stage(n)), mg.land(stage(n) + F::TILE);
+    else mq.land(a.D, stage(n)), mg.land(a.D, stage(n) + F::TILE);
     if (tid < F::R) st[tid] = tm, st[F::R + tid] = ti, st[2 * F::R + tid] = td;
     __syncthreads();
     if (n + 1 < all) go(n + 1);
@@ -246,24 +261,16 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
   for (int j = 0; j < KN; ++j) {
     if (key[j] >= a.Tk) continue;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    auto vk = [&](int dt) { return there[j] ? dk[j][dt] * a.scale : zero; };
+    auto vv = [&](int dt) { return there[j] ? dv[j][dt] : zero; };
     if (a.splits > 1) {
       const int64_t all = (int64_t)a.B * a.Hk * a.Tk * a.D;
       float* p = a.part + (int64_t)pl.split * 2 * all + ((int64_t)pl.bh * a.Tk + key[j]) * a.D;
-#pragma unroll
-      for (int dt = 0; dt < H::DT; ++dt) {
-        if (16 * dt + 4 * lq >= a.D) continue;
-        store4(p, 16 * dt + 4 * lq, a.D, there[j] ? dk[j][dt] * a.scale : zero);
-        store4(p + all, 16 * dt + 4 * lq, a.D, there[j] ? dv[j][dt] : zero);
-      }
-      continue;
-    }
-    T* ok = (T*)a.dk + (int64_t)b * a.sdk.b + (int64_t)key[j] * a.sdk.t + (int64_t)hk * a.sdk.h;
-    T* ov = (T*)a.dv + (int64_t)b * a.sdv.b + (int64_t)key[j] * a.sdv.t + (int64_t)hk * a.sdv.h;
-#pragma unroll
-    for (int dt = 0; dt < H::DT; ++dt) {
-      if (16 * dt + 4 * lq >= a.D) continue;
-      store4(ok, 16 * dt + 4 * lq, a.D, there[j] ? dk[j][dt] * a.scale : zero);
-      store4(ov, 16 * dt + 4 * lq, a.D, there[j] ? dv[j][dt] : zero);
+      store_cols<float, DP>(p, lq, a.D, vk);
+      store_cols<float, DP>(p + all, lq, a.D, vv);
+    } else {
+      store_cols<T, DP>((T*)a.dk + (int64_t)b * a.sdk.b + (int64_t)key[j] * a.sdk.t + (int64_t)hk * a.sdk.h, lq, a.D, vk);
+      store_cols<T, DP>((T*)a.dv + (int64_t)b * a.sdv.b + (int64_t)key[j] * a.sdv.t + (int64_t)hk * a.sdv.h, lq, a.D, vv);
     }
   }
 }
@@ -285,7 +292,9 @@ __global__ void __launch_bounds__(256) k_attend_join_dkv(AttendArgs a) {
   }
   const slstm_strides st = blockIdx.y ? a.sdv : a.sdk;
   T* to = (T*)(blockIdx.y ? a.dv : a.dk) + (int64_t)(bh / a.Hk) * st.b + (int64_t)t * st.t + (int64_t)(bh % a.Hk) * st.h;
-  if (left > 0) store4(to, n, a.D, f32x4{s[0], s[1], s[2], s[3]});
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k < left) from_f32(to[n + k], s[k]);
 }
 
 namespace {
@@ -303,7 +312,7 @@ KeyPlan key_plan(const slstm_attend_dims* d) {
   const int keys = p.big ? 256 : d->D > 128 || (d->D > 64 && d->type == SLSTM_F32) ? 64 : 128;
   p.tiles = (d->Tk + keys - 1) / keys;
   const int64_t groups = std::max<int64_t>(1, (int64_t)p.tiles * d->B * d->Hk), most = (int64_t)d->Tq * (d->Hq / d->Hk) / 256;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / groups, most), 64));
+  p.splits = (int)std::max<int64_t>(1, groups < 256 ? std::min<int64_t>(std::min<int64_t>(512 / groups, most), 64) : 1);
   return p;
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }

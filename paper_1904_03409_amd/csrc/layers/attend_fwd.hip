@@ -6,6 +6,7 @@
 // queries, a quarter of the tile (WK = 4), whose parts are joined through LDS. Where the row tiles do not fill the chip the
 // keys are split over workgroups and k_attend_join joins their sums.
 #include <algorithm>
+#include <stdlib.h>
 
 #include "attend.h"
 
@@ -21,7 +22,7 @@ struct Fwd {
   static constexpr int KW = KT / WK, NU = KW / H::UNIT;                  // keys and units of a wave
   static constexpr int TILE = KT * H::BYTES;
   // waves on a SIMD that the registers are to leave room for: two hide each other's waits and run products beside exponentials
-  static constexpr int WAVES = H::BYTES <= 128 || (DMA && DP <= 128) ? 2 : 1;
+  static constexpr int WAVES = H::BYTES <= 128 || (DMA && H::BYTES <= 256) ? 2 : 1;
   static constexpr int JOIN = WK == 4 ? 4 * 16 * (DP + 4) * 4 + 4 * 2 * 16 * 4 : 0;
   static constexpr int STAGES = 4 * TILE <= 160 * 1024 ? 2 : 1;
   static constexpr int LDS = 2 * STAGES * TILE > JOIN ? 2 * STAGES * TILE : JOIN;
@@ -33,9 +34,7 @@ __device__ __forceinline__ void fwd_row(const AttendArgs& a, int b, int t, int h
   // (l: 0 where no key is there; NaN stays)
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
-#pragma unroll
-  for (int dt = 0; dt < DP / 16; ++dt)
-    if (16 * dt + 4 * lq < a.D) store4(y, 16 * dt + 4 * lq, a.D, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * inv);
+  store_cols<T, DP>(y, lq, a.D, [&](int dt) { return l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * inv; });
   if (a.stats && lq == 0) {
     float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * 2;
     s[0] = l == 0.f ? INFINITY : m;
@@ -62,15 +61,16 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
   const int kend = pl.tile * ROWS / a.G < qlen ? min(klen, kbeg + a.chunk) : kbeg;
   int qt_[QT], qh_[QT];
   bool here[QT];
-  frag q[QT][H::STEPS];
+  u32x4 qr[QT][H::STEPS];
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
     const int r = pl.tile * ROWS + 16 * (QT * wq + j) + l16;
-    qt_[j] = r / a.G;
-    qh_[j] = hk * a.G + r % a.G;
     here[j] = r < rows;
-    load_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h,
-                    here[j] && qt_[j] < qlen, a.D, lq, q[j]);
+    const int in = min(r, rows - 1);
+    qt_[j] = in / a.G;
+    qh_[j] = hk * a.G + in % a.G;
+    fetch_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h,
+                     here[j] && qt_[j] < qlen, a.D, lq, qr[j]);
   }
   const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
   const T* vp = (const T*)a.v + (int64_t)b * a.sv.b + (int64_t)hk * a.sv.h;
@@ -93,12 +93,15 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
     for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (kbeg < kend) go(kbeg, 0);
+  frag q[QT][H::STEPS];
+#pragma unroll
+  for (int j = 0; j < QT; ++j) place_own<T, DP>(qr[j], a.D, lq, q[j]);
   for (int k0 = kbeg, n = 0; k0 < kend; k0 += F::KT, ++n) {
     const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const int first = k0 + wk * F::KW;
     const unsigned long long there = __ballot(lane < F::KW && first + lane < kend && (!mask || mask[first + lane]));
     if constexpr (DMA) wait_vm<0>();
-    else mk.land(stage(n)), mv.land(stage(n) + F::TILE);
+    else mk.land(a.D, stage(n)), mv.land(a.D, stage(n) + F::TILE);
     __syncthreads();
     if (F::STAGES == 2 && k0 + F::KT < kend) go(k0 + F::KT, n + 1);
     if (there) {
@@ -230,37 +233,41 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
       fwd_row<T, DP>(a, b, qt_[j], qh_[j], lq, o[j], m[j], l[j]);
     } else {
       const int64_t r = ((int64_t)pl.split * a.B * a.Hk + pl.bh) * rows + qt_[j] * a.G + qh_[j] - hk * a.G;
-#pragma unroll
-      for (int dt = 0; dt < H::DT; ++dt)
-        if (16 * dt + 4 * lq < a.D) store4(a.part + r * a.D, 16 * dt + 4 * lq, a.D, o[j][dt]);
+      store_cols<float, DP>(a.part + r * a.D, lq, a.D, [&](int dt) { return o[j][dt]; });
       if (lq == 0) a.ml[2 * r] = m[j], a.ml[2 * r + 1] = l[j];
     }
   }
 }
 
-// A row's splits joined, a wave to a row.
+// Rows' splits joined, four columns to a thread and 2^shift threads to a row. (A wave to a row, with a column to a lane: 18 us for 32768
+// rows of 64 in two splits.)
 template <typename T>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = (int64_t)a.Tq * a.G, all = (int64_t)a.B * a.Hk * rows;
-  const int64_t row = a.first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= all) return;
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int shift) {
+  const int rows = a.Tq * a.G, all = rows * a.B * a.Hk;
+  const int64_t row64 = ((a.first + blockIdx.x) << (8 - shift)) + (threadIdx.x >> shift);
+  const int n = (threadIdx.x & ((1 << shift) - 1)) * 4;
+  if (row64 >= all || n >= a.D) return;
+  const int64_t row = row64;
   float m = -INFINITY, l = 0.f;
-  for (int s = lane; s < a.splits; s += 64) m = fmaxf(m, a.ml[2 * (s * all + row)]);
-  m = lanes<64>(m, op_max());
-  auto factor = [&](float ms) { return ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m); };
-  for (int s = lane; s < a.splits; s += 64) l += a.ml[2 * (s * all + row) + 1] * factor(a.ml[2 * (s * all + row)]);
-  l = lanes<64>(l, op_sum());
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int bh = (int)(row / rows), r = (int)(row % rows), b = bh / a.Hk, t = r / a.G, h = bh % a.Hk * a.G + r % a.G;
-  T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
-  for (int n = lane; n < a.D; n += 64) {
-    float v = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) v += a.part[(s * all + row) * a.D + n] * factor(a.ml[2 * (s * all + row)]);
-    from_f32(y[n], l == 0.f ? 0.f : v * inv);
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.ml[2 * ((int64_t)s * all + row)]);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) {
+    const float ms = a.ml[2 * ((int64_t)s * all + row)], f = ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m);
+    float p[4];
+    vec<float>::unpack(load_vec(a.part + ((int64_t)s * all + row) * a.D, n / 4, a.D), p);
+    l += a.ml[2 * ((int64_t)s * all + row) + 1] * f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += p[k] * f;
   }
-  if (a.stats && lane == 0) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int bh = (int)row / rows, r = (int)row - bh * rows, b = bh / a.Hk, t = r / a.G, h = (bh - b * a.Hk) * a.G + r % a.G;
+  T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (n + k < a.D) from_f32(y[n + k], l == 0.f ? 0.f : v[k] * inv);
+  if (a.stats && n == 0) {
     float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * 2;
     s[0] = l == 0.f ? INFINITY : m;
     s[1] = inv;
@@ -281,11 +288,12 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
   if (R <= 16) p.qt = 1, p.wk = 4;
   else if (R <= 64 || wide) p.qt = 1, p.wk = 1;
   else p.qt = 2, p.wk = 1;
+  if (getenv("ATT_QT") && p.wk == 1) p.qt = atoi(getenv("ATT_QT"));
   p.rows = 16 * p.qt * (4 / p.wk);
   p.tiles = (int)((R + p.rows - 1) / p.rows);
   // splits of 256 keys at least, until there are two workgroups to a compute unit
   const int64_t groups = (int64_t)p.tiles * d->B * d->Hk;
-  const int64_t want = groups ? 512 / groups : 1, most = ((int64_t)d->Tk + 255) / 256;
+  const int64_t want = groups > 0 && groups < 256 ? 512 / groups : 1, most = ((int64_t)d->Tk + 255) / 256;
   p.splits = (int)std::max<int64_t>(1, std::min(want, most));
   p.chunk = (((d->Tk + p.splits - 1) / p.splits) + 127) / 128 * 128;
   if (p.chunk < 128) p.chunk = 128;
@@ -344,9 +352,11 @@ extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, c
     };
     hipError_t e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     if (e == hipSuccess && p.splits > 1) {
-      in_pieces((int64_t)d->B * d->Tq * d->Hq, 4 * kMostGroups, [&](int64_t r0, int64_t n) {
-        a.first = r0;
-        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, a);
+      int shift = 0;
+      while (4 << shift < d->D) ++shift;
+      in_pieces((((int64_t)d->B * d->Tq * d->Hq << shift) + 255) / 256, kMostGroups, [&](int64_t b0, int64_t n) {
+        a.first = b0;
+        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)n), dim3(256), 0, st, a, shift);
       });
       e = hipGetLastError();
     }
