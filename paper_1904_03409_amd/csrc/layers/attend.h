@@ -146,32 +146,53 @@ __device__ __forceinline__ void put_weights(bf16x8& w, int sub, const f32x4& p) 
   for (int r = 0; r < 4; ++r) w[4 * sub + r] = static_cast<__bf16>(p[r]);
 }
 __device__ __forceinline__ void put_weights(f32x4& w, int, const f32x4& p) { w = p; }
+// Columns 16 dt .. of a unit (from row `base` on) as a fragment: a lane has column l16, and the unit's rows as the weights have them.
+template <typename T, int GPR>
+__device__ __forceinline__ frag_t<T> column(const unsigned char* tile, int base, int dt, int l16, int lq) {
+  if constexpr (sizeof(T) == 2) {
+    // transposed: the lane gives the address of unit row 8 lq + l16 / 4 and columns 4 (l16 % 4) of the tile, and gets column
+    // l16, four rows
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    const int row = 8 * lq + (l16 >> 2);
+    const unsigned char* q = tile + (base + row) * GPR * 16 + ((2 * dt + (l16 >> 1 & 1)) ^ swz<T, GPR>(row)) * 16 + (l16 & 1) * 8;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * GPR * 16));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = 4 * lq + e;
+      v[e] = *(const float*)(tile + (base + row) * GPR * 16 + ((4 * dt + (l16 >> 2)) ^ swz<T, GPR>(base + row)) * 16 + (l16 & 3) * 4);
+    }
+    return v;
+  }
+}
+template <typename T>
+__device__ __forceinline__ f32x4 product(const frag_t<T>& a, const frag_t<T>& b, f32x4 c) {
+  if constexpr (sizeof(T) == 2) {
+    return mfma_bf16_16x16x32(a, b, c);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+}
 // acc[j][dt] += (columns 16 dt .. of unit row `base` on)^T times the weights w[j].
 template <typename T, int DP, int N>
-__device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq,
-                                     const frag_t<T> (&w)[N]) {
+__device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq, const frag_t<T> (&w)[N]) {
   typedef Head<T, DP> H;
 #pragma unroll
   for (int dt = 0; dt < H::DT; ++dt) {
+    const frag_t<T> a = column<T, H::GPR>(tile, base, dt, l16, lq);
     if constexpr (sizeof(T) == 2) {
-      // transposed: the lane gives the address of unit row 8 lq + l16 / 4 and columns 4 (l16 % 4) of the tile, and gets column
-      // l16, four rows
-      typedef short s16x4 __attribute__((ext_vector_type(4)));
-      const int row = 8 * lq + (l16 >> 2);
-      const unsigned char* q = tile + (base + row) * H::BYTES + ((2 * dt + (l16 >> 1 & 1)) ^ swz<T, H::GPR>(row)) * 16 + (l16 & 1) * 8;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * H::BYTES));
-      const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int j = 0; j < N; ++j) acc[j][dt] = mfma_bf16_16x16x32(a, w[j], acc[j][dt]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 4 * lq + e;
-        const float a = *(const float*)(tile + (base + row) * H::BYTES + ((4 * dt + (l16 >> 2)) ^ swz<T, H::GPR>(base + row)) * 16 + (l16 & 3) * 4);
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[j][e], acc[j][dt], 0, 0, 0);
-      }
+        for (int j = 0; j < N; ++j) acc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], w[j][e], acc[j][dt], 0, 0, 0);
     }
   }
 }
@@ -253,23 +274,26 @@ __device__ __forceinline__ void store4(T* to, const f32x4& v) {
                                 (uint32_t)f32_to_bf16_bits(v[2]) | (uint32_t)f32_to_bf16_bits(v[3]) << 16};
   }
 }
-// A row from a lane's columns 16 dt + 4 lq .., f(dt) their values.
-template <typename T, int DP, typename F>
-__device__ __forceinline__ void store_cols(T* row, int lq, int D, F f) {
+// A row's columns n0 + 16 dt + 4 lq .., dt < DN, f(dt) their values.
+template <typename T, int DN, typename F>
+__device__ __forceinline__ void store_some(T* row, int n0, int lq, int D, F f) {
+  n0 += 4 * lq;
   if (D % 4 == 0) {
 #pragma unroll
-    for (int dt = 0; dt < DP / 16; ++dt)
-      if (16 * dt + 4 * lq < D) store4(row + 16 * dt + 4 * lq, f(dt));
+    for (int dt = 0; dt < DN; ++dt)
+      if (n0 + 16 * dt < D) store4(row + n0 + 16 * dt, f(dt));
   } else {
 #pragma unroll
-    for (int dt = 0; dt < DP / 16; ++dt) {
+    for (int dt = 0; dt < DN; ++dt) {
       const f32x4 v = f(dt);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (16 * dt + 4 * lq + r < D) from_f32(row[16 * dt + 4 * lq + r], v[r]);
+        if (n0 + 16 * dt + r < D) from_f32(row[n0 + 16 * dt + r], v[r]);
     }
   }
 }
+template <typename T, int DP, typename F>
+__device__ __forceinline__ void store_cols(T* row, int lq, int D, F f) { store_some<T, DP / 16>(row, 0, lq, D, f); }
 
 __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
   return len ? max(0, min(len[b], most)) : most;

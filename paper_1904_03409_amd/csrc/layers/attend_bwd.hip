@@ -33,6 +33,15 @@ struct Keys {
   static constexpr int LDS = F::LDS + (BIG ? ALL * F::H::BYTES : 0);
 };
 
+// A workgroup of k_attend_short: 64 KN keys, query tiles of 64 (fp32: 32).
+template <typename T, int DP, int KN>
+struct Short {
+  typedef Head<T, DP> H;
+  static constexpr int ALL = 64 * KN, R = sizeof(T) == 2 ? 64 : 32, NU = R / H::UNIT, TILE = R * H::BYTES, KTILE = ALL * H::BYTES;
+  static constexpr int SROW = R * (int)sizeof(T), STILE = ALL * SROW;
+  static constexpr int LDS = 4 * TILE + KTILE + STILE + 8 * R * 4, WAVES = sizeof(T) == 4 && DP == 64 && KN == 2 ? 1 : 2;
+};
+
 }  // namespace
 
 template <typename T, int DP, bool DMA>
@@ -275,6 +284,182 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
   }
 }
 
+// All keys of a (sequence, key head) in one workgroup, up to 128: the five products of a query tile at once, q and dy read once, and y
+// not at all: delta = sum p dp over the keys that are here. The waves share 32 or 16 keys each for the scores and the sums of dk and
+// dv; their s go through LDS, where dq's product takes a query tile to a wave, over all keys.
+template <typename T, int DP, bool DMA, int KN>
+__global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short(AttendArgs a) {
+  typedef Head<T, DP> H;
+  typedef Short<T, DP, KN> F;
+  typedef frag_t<T> frag;
+  constexpr int R = F::R, QN = R / 16, DN = H::DT * QN / 4;              // column tiles of dq that a wave has of its query tile
+  extern __shared__ __align__(16) unsigned char sm[];
+  unsigned char *kt = sm + 4 * F::TILE, *ds_ = kt + F::KTILE;            // keys; s: [key][query]
+  float *stats = (float*)(ds_ + F::STILE), *parts = stats + 4 * R;       // two stages of [2][R]: m, 1 / l; [4][R]: the waves' sums of p dp
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
+  const Place pl = place_of(a);
+  const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk);
+  const int qend = clamp_len(a.q_len, b, a.Tq), klen = clamp_len(a.k_len, b, a.Tk);
+  int key[KN];
+  bool there[KN];
+  u32x4 kr[KN][H::STEPS], vr[KN][H::STEPS];
+#pragma unroll
+  for (int j = 0; j < KN; ++j) {
+    key[j] = 16 * (KN * wave + j) + l16;
+    there[j] = key[j] < klen && (!a.mask || a.mask[(int64_t)b * a.Tk + key[j]]);
+    const int in = min(key[j], a.Tk - 1);
+    fetch_own<T, DP>((const T*)a.k + (int64_t)b * a.sk.b + (int64_t)in * a.sk.t + (int64_t)hk * a.sk.h, there[j], a.D, lq, kr[j]);
+    fetch_own<T, DP>((const T*)a.v + (int64_t)b * a.sv.b + (int64_t)in * a.sv.t + (int64_t)hk * a.sv.h, there[j], a.D, lq, vr[j]);
+  }
+  f32x4 dk[KN][H::DT], dv[KN][H::DT];
+#pragma unroll
+  for (int j = 0; j < KN; ++j)
+#pragma unroll
+    for (int dt = 0; dt < H::DT; ++dt) dk[j][dt] = dv[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Mover<T, DP, R, DMA> mq, mg;
+  mq.start(a.sq.t, a.D);
+  mg.start(a.sdy.t, a.D);
+  float tm = 0.f, ti = 0.f;
+  // tiles of the first head's queries, then of the next one's; those behind the last query are there for dq's zeros
+  const int tiles = (a.Tq + R - 1) / R;
+  int n0 = 0, all = tiles * a.G;
+  int h = hk * a.G, t0 = 0;                            // of the next tile to go
+  if (a.splits > 1) {
+    const int each = all / a.splits, more = all - each * a.splits;
+    n0 = uni(each * pl.split + min(pl.split, more));
+    all = uni(n0 + each + (pl.split < more ? 1 : 0));
+    h += uni(n0 / tiles);
+    t0 = uni(n0 % tiles) * R;
+  }
+  auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
+  auto go = [&](int n) {
+    if (t0 < qend) {
+      mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
+      mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
+            stage(n) + F::TILE);
+      if (tid < R) {
+        tm = INFINITY, ti = 0.f;
+        if (t0 + tid < qend) {
+          const float* st = a.stats_in + 2 * (((int64_t)b * a.Hq + h) * a.Tq + t0);
+          tm = st[2 * tid], ti = st[2 * tid + 1];
+        }
+      }
+    }
+    t0 += R;
+    if (t0 >= a.Tq) t0 = 0, ++h;
+  };
+  int oh = h, ot = t0;                                 // of the tile at hand
+  if (n0 < all) go(n0);
+  frag k[KN][H::STEPS], v[KN][H::STEPS];
+#pragma unroll
+  for (int j = 0; j < KN; ++j) {
+    place_own<T, DP>(kr[j], a.D, lq, k[j]);
+    place_own<T, DP>(vr[j], a.D, lq, v[j]);
+#pragma unroll
+    for (int s = 0; s < H::STEPS; ++s) *(frag*)(kt + key[j] * H::BYTES + ((4 * s + lq) ^ swz<T, H::GPR>(key[j])) * 16) = k[j][s];
+  }
+  for (int n = n0; n < all; ++n) {
+    const unsigned char *qt = stage(n), *gt = qt + F::TILE;
+    float* st = stats + (n & 1) * 2 * R;
+    // this wave's query tile of dq, and its columns
+    const int qn = wave % QN, d0 = wave / QN * DN, row = ot + 16 * qn + l16;
+    f32x4 o[DN];
+#pragma unroll
+    for (int dt = 0; dt < DN; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bool live = ot < qend;
+    if (live) {
+      if constexpr (DMA) wait_vm<0>();
+      else mq.land(a.D, stage(n)), mg.land(a.D, stage(n) + F::TILE);
+      if (tid < R) st[tid] = tm, st[R + tid] = ti;
+    }
+    __syncthreads();
+    if (n + 1 < all) go(n + 1);
+    if (live) {
+      f32x4 p[F::NU][H::SUB][KN], dp[F::NU][H::SUB][KN];
+#pragma unroll
+      for (int u = 0; u < F::NU; ++u)
+#pragma unroll
+        for (int i = 0; i < H::SUB; ++i) {
+#pragma unroll
+          for (int j = 0; j < KN; ++j) p[u][i][j] = dp[u][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          scores<T, DP, KN>(p[u][i], qt, u * H::UNIT, i, l16, lq, k);
+          scores<T, DP, KN>(dp[u][i], gt, u * H::UNIT, i, l16, lq, v);
+          const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
+          const f32x4 m = *(const f32x4*)(st + at), inv = *(const f32x4*)(st + R + at);
+          f32x4 part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < KN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float x = there[j] ? p[u][i][j][r] * a.c : -INFINITY;
+              p[u][i][j][r] = __builtin_amdgcn_exp2f(x - m[r]) * inv[r];
+              // (a key that is not there has v = 0, but dy may be NaN)
+              part[r] += there[j] ? p[u][i][j][r] * dp[u][i][j][r] : 0.f;
+            }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) part[r] = lanes<16>(part[r], op_sum());
+          if (l16 == 0) *(f32x4*)(parts + wave * R + at) = part;
+        }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < F::NU; ++u) {
+        frag wp[KN], ws[KN];
+#pragma unroll
+        for (int i = 0; i < H::SUB; ++i) {
+          const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
+          f32x4 delta = *(const f32x4*)(parts + at);
+#pragma unroll
+          for (int w = 1; w < 4; ++w) delta += *(const f32x4*)(parts + w * R + at);
+#pragma unroll
+          for (int j = 0; j < KN; ++j) {
+            f32x4 ds;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ds[r] = there[j] ? p[u][i][j][r] * (dp[u][i][j][r] - delta[r]) : 0.f;
+            put_weights(wp[j], i, p[u][i][j]);
+            put_weights(ws[j], i, ds);
+          }
+        }
+        // (a lane's weights are neighbours in a key's row of s: one granule)
+#pragma unroll
+        for (int j = 0; j < KN; ++j) *(frag*)(ds_ + key[j] * F::SROW + ((4 * u + lq) ^ swz<T, F::SROW / 16>(key[j])) * 16) = ws[j];
+        sums<T, DP, KN>(dv, gt, u * H::UNIT, l16, lq, wp);
+        sums<T, DP, KN>(dk, qt, u * H::UNIT, l16, lq, ws);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int ku = 0; ku < F::ALL / H::UNIT; ++ku) {
+        const frag w = column<T, F::SROW / 16>(ds_, ku * H::UNIT, qn, l16, lq);
+#pragma unroll
+        for (int dt = 0; dt < DN; ++dt) o[dt] = product<T>(column<T, H::GPR>(kt, ku * H::UNIT, d0 + dt, l16, lq), w, o[dt]);
+      }
+    }
+    if (row < a.Tq) {
+      // (a query without keys has 1 / l = 0: nothing, whatever dy holds)
+      const bool used = live && row < qend && st[R + 16 * qn + l16] != 0.f;
+      T* dq = (T*)a.dq + (int64_t)b * a.sdq.b + (int64_t)row * a.sdq.t + (int64_t)oh * a.sdq.h;
+      store_some<T, DN>(dq, 16 * d0, lq, a.D, [&](int dt) { return used ? o[dt] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f}; });
+    }
+    ot += R;
+    if (ot >= a.Tq) ot = 0, ++oh;
+  }
+#pragma unroll
+  for (int j = 0; j < KN; ++j) {
+    if (key[j] >= a.Tk) continue;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    auto vk = [&](int dt) { return there[j] ? dk[j][dt] * a.scale : zero; };
+    auto vv = [&](int dt) { return there[j] ? dv[j][dt] : zero; };
+    if (a.splits > 1) {
+      const int64_t every = (int64_t)a.B * a.Hk * a.Tk * a.D;
+      float* p = a.part + (int64_t)pl.split * 2 * every + ((int64_t)pl.bh * a.Tk + key[j]) * a.D;
+      store_cols<float, DP>(p, lq, a.D, vk);
+      store_cols<float, DP>(p + every, lq, a.D, vv);
+    } else {
+      store_cols<T, DP>((T*)a.dk + (int64_t)b * a.sdk.b + (int64_t)key[j] * a.sdk.t + (int64_t)hk * a.sdk.h, lq, a.D, vk);
+      store_cols<T, DP>((T*)a.dv + (int64_t)b * a.sdv.b + (int64_t)key[j] * a.sdv.t + (int64_t)hk * a.sdv.h, lq, a.D, vv);
+    }
+  }
+}
+
 // dk and dv from their splits: four elements of a head to a thread, blockIdx.y: dk, dv.
 template <typename T>
 __global__ void __launch_bounds__(256) k_attend_join_dkv(AttendArgs a) {
@@ -303,13 +488,14 @@ namespace {
 // queries are split, 256 of them at least to each part, until there are two workgroups to a compute unit (2 sequences of 4096 x 4000, 4 key
 // heads of 128, of unequal lengths: TIMES).
 struct KeyPlan {
-  bool big;
+  bool one, big;                                       // one: k_attend_short
   int tiles, splits;
 };
 KeyPlan key_plan(const slstm_attend_dims* d) {
   KeyPlan p;
+  p.one = d->Tk >= 1 && d->Tk <= 128 && d->D <= 64;
   p.big = d->type == SLSTM_BF16 && d->D > 64 && d->D <= 128 && d->Tk > 128;
-  const int keys = p.big ? 256 : d->D > 128 || (d->D > 64 && d->type == SLSTM_F32) ? 64 : 128;
+  const int keys = p.one ? 128 : p.big ? 256 : d->D > 128 || (d->D > 64 && d->type == SLSTM_F32) ? 64 : 128;
   p.tiles = (d->Tk + keys - 1) / keys;
   const int64_t groups = std::max<int64_t>(1, (int64_t)p.tiles * d->B * d->Hk), most = (int64_t)d->Tq * (d->Hq / d->Hk) / 256;
   p.splits = (int)std::max<int64_t>(1, groups < 256 ? std::min<int64_t>(std::min<int64_t>(512 / groups, most), 64) : 1);
@@ -351,7 +537,23 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
     typedef decltype(t) T;
     constexpr int DP = decltype(dp)::value;
     hipError_t e = hipSuccess;
-    if (d->Tq) {
+    a.splits = plan.splits;
+    if (plan.one) {
+      if constexpr (DP <= 64) {
+        a.tiles = 1;
+        auto run = [&](auto dma, auto kn) {
+          constexpr int KN = decltype(kn)::value;
+          static std::atomic<uint64_t> dev;
+          return attend_launch(k_attend_short<T, DP, decltype(dma)::value, KN>, a, (int64_t)d->B * d->Hk * a.splits, Short<T, DP, KN>::LDS, dev, st);
+        };
+        auto keys = [&](auto dma) {
+          return d->Tk <= 64 ? run(dma, std::integral_constant<int, 1>()) : run(dma, std::integral_constant<int, 2>());
+        };
+        e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? keys(std::true_type()) : keys(std::false_type());
+      }
+    }
+    if (!plan.one && d->Tq) {
+      a.splits = 1;
       auto run = [&](auto dma) {
         typedef Bwd<T, DP, decltype(dma)::value> F;
         static std::atomic<uint64_t> dev;
@@ -360,7 +562,7 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
       };
       e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     }
-    if (e == hipSuccess && d->Tk) {
+    if (e == hipSuccess && !plan.one && d->Tk) {
       a.splits = plan.splits;
       auto go = [&](auto kern, int keys, int threads, int lds, std::atomic<uint64_t>& dev) {
         a.tiles = (d->Tk + keys - 1) / keys;
