@@ -33,13 +33,13 @@ struct Keys {
   static constexpr int LDS = F::LDS + (BIG ? ALL * F::H::BYTES : 0);
 };
 
-// A workgroup of k_attend_short: 64 KN keys, query tiles of 64 (fp32: 32).
-template <typename T, int DP, int KN>
+// A workgroup of k_attend_short: NW waves with 16 KN keys each, query tiles of 64 (fp32: 32).
+template <typename T, int DP, int NW, int KN>
 struct Short {
   typedef Head<T, DP> H;
-  static constexpr int ALL = 64 * KN, R = sizeof(T) == 2 ? 64 : 32, NU = R / H::UNIT, TILE = R * H::BYTES, KTILE = ALL * H::BYTES;
+  static constexpr int ALL = 16 * NW * KN, R = sizeof(T) == 2 ? 64 : 32, NU = R / H::UNIT, TILE = R * H::BYTES, KTILE = ALL * H::BYTES;
   static constexpr int SROW = R * (int)sizeof(T), STILE = ALL * SROW;
-  static constexpr int LDS = 4 * TILE + KTILE + STILE + 8 * R * 4, WAVES = sizeof(T) == 4 && DP == 64 && KN == 2 ? 1 : 2;
+  static constexpr int LDS = 4 * TILE + KTILE + STILE + (4 + NW) * R * 4;
 };
 
 }  // namespace
@@ -202,9 +202,7 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
   }
   auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
   auto go = [&](int n) {
-    mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
-    mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
-          stage(n) + F::TILE);
+    // (ahead of the DMAs: before it writes a register that a load may be in flight for, the compiler waits for all that is)
     if (tid < F::R) {
       tm = INFINITY, ti = td = 0.f;
       if (t0 + tid < qend) {
@@ -213,6 +211,9 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
         tm = st[2 * tid], ti = st[2 * tid + 1], td = de[tid];
       }
     }
+    mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
+    mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
+          stage(n) + F::TILE);
     t0 += F::R;
     if (t0 >= qend) t0 = 0, ++h;
   };
@@ -287,15 +288,15 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
 // All keys of a (sequence, key head) in one workgroup, up to 128: the five products of a query tile at once, q and dy read once, and y
 // not at all: delta = sum p dp over the keys that are here. The waves share 32 or 16 keys each for the scores and the sums of dk and
 // dv; their s go through LDS, where dq's product takes a query tile to a wave, over all keys.
-template <typename T, int DP, bool DMA, int KN>
-__global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short(AttendArgs a) {
+template <typename T, int DP, bool DMA, int NW, int KN>
+__global__ void __launch_bounds__(64 * NW, NW == 8 && sizeof(T) == 2 && DMA ? 4 : 2) k_attend_short(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Short<T, DP, KN> F;
+  typedef Short<T, DP, NW, KN> F;
   typedef frag_t<T> frag;
-  constexpr int R = F::R, QN = R / 16, DN = H::DT * QN / 4;              // column tiles of dq that a wave has of its query tile
+  constexpr int R = F::R, QN = R / 16, DN = H::DT * QN / NW;              // column tiles of dq that a wave has of its query tile
   extern __shared__ __align__(16) unsigned char sm[];
   unsigned char *kt = sm + 4 * F::TILE, *ds_ = kt + F::KTILE;            // keys; s: [key][query]
-  float *stats = (float*)(ds_ + F::STILE), *parts = stats + 4 * R;       // two stages of [2][R]: m, 1 / l; [4][R]: the waves' sums of p dp
+  float *stats = (float*)(ds_ + F::STILE), *parts = stats + 4 * R;       // two stages of [2][R]: m, 1 / l; [NW][R]: the waves' sums of p dp
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), l16 = lane & 15, lq = lane >> 4;
   const Place pl = place_of(a);
   const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk);
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short
   for (int j = 0; j < KN; ++j)
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) dk[j][dt] = dv[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Mover<T, DP, R, DMA> mq, mg;
+  Mover<T, DP, R, DMA, 64 * NW> mq, mg;
   mq.start(a.sq.t, a.D);
   mg.start(a.sdy.t, a.D);
   float tm = 0.f, ti = 0.f;
@@ -332,21 +333,26 @@ __global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short
     t0 = uni(n0 % tiles) * R;
   }
   auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
+  // (pointers go on by steps: products of 64 bits for each tile took as long as its first matrix products)
+  const T *qp = (const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h;
+  const T *gp = (const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h;
+  const float* sp = a.stats_in + 2 * (((int64_t)b * a.Hq + h) * a.Tq + t0);
+  const int64_t qstep = R * a.sq.t, gstep = R * a.sdy.t;
   auto go = [&](int n) {
     if (t0 < qend) {
-      mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
-      mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
-            stage(n) + F::TILE);
+      // (ahead of the DMAs: before it writes a register that a load may be in flight for, the compiler waits for all that is)
       if (tid < R) {
         tm = INFINITY, ti = 0.f;
-        if (t0 + tid < qend) {
-          const float* st = a.stats_in + 2 * (((int64_t)b * a.Hq + h) * a.Tq + t0);
-          tm = st[2 * tid], ti = st[2 * tid + 1];
-        }
+        if (t0 + tid < qend) tm = sp[2 * tid], ti = sp[2 * tid + 1];
       }
+      mq.go(qp, a.sq.t, a.D, qend - t0, nullptr, stage(n));
+      mg.go(gp, a.sdy.t, a.D, qend - t0, nullptr, stage(n) + F::TILE);
     }
-    t0 += R;
-    if (t0 >= a.Tq) t0 = 0, ++h;
+    t0 += R, qp += qstep, gp += gstep, sp += 2 * R;
+    if (t0 >= a.Tq) {
+      qp += a.sq.h - tiles * qstep, gp += a.sdy.h - tiles * gstep, sp += 2 * (a.Tq - tiles * R);
+      t0 = 0;
+    }
   };
   int oh = h, ot = t0;                                 // of the tile at hand
   if (n0 < all) go(n0);
@@ -358,6 +364,9 @@ __global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short
 #pragma unroll
     for (int s = 0; s < H::STEPS; ++s) *(frag*)(kt + key[j] * H::BYTES + ((4 * s + lq) ^ swz<T, H::GPR>(key[j])) * 16) = k[j][s];
   }
+  uint32_t keep[KN], low[KN];
+#pragma unroll
+  for (int j = 0; j < KN; ++j) keep[j] = there[j] ? 0xffffffffu : 0u, low[j] = there[j] ? 0u : 0xff800000u;
   for (int n = n0; n < all; ++n) {
     const unsigned char *qt = stage(n), *gt = qt + F::TILE;
     float* st = stats + (n & 1) * 2 * R;
@@ -391,10 +400,10 @@ __global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short
           for (int j = 0; j < KN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float x = there[j] ? p[u][i][j][r] * a.c : -INFINITY;
+              // (-inf where the key is not there, without a branch: its p is 0)
+              const float x = __uint_as_float((__float_as_uint(p[u][i][j][r] * a.c) & keep[j]) | low[j]);
               p[u][i][j][r] = __builtin_amdgcn_exp2f(x - m[r]) * inv[r];
-              // (a key that is not there has v = 0, but dy may be NaN)
-              part[r] += there[j] ? p[u][i][j][r] * dp[u][i][j][r] : 0.f;
+              part[r] = __builtin_fmaf(p[u][i][j][r], dp[u][i][j][r], part[r]);
             }
 #pragma unroll
           for (int r = 0; r < 4; ++r) part[r] = lanes<16>(part[r], op_sum());
@@ -409,12 +418,12 @@ __global__ void __launch_bounds__(256, (Short<T, DP, KN>::WAVES)) k_attend_short
           const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
           f32x4 delta = *(const f32x4*)(parts + at);
 #pragma unroll
-          for (int w = 1; w < 4; ++w) delta += *(const f32x4*)(parts + w * R + at);
+          for (int w = 1; w < NW; ++w) delta += *(const f32x4*)(parts + w * R + at);
 #pragma unroll
           for (int j = 0; j < KN; ++j) {
             f32x4 ds;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) ds[r] = there[j] ? p[u][i][j][r] * (dp[u][i][j][r] - delta[r]) : 0.f;
+            for (int r = 0; r < 4; ++r) ds[r] = p[u][i][j][r] * (dp[u][i][j][r] - delta[r]);
             put_weights(wp[j], i, p[u][i][j]);
             put_weights(ws[j], i, ds);
           }
@@ -541,13 +550,17 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
     if (plan.one) {
       if constexpr (DP <= 64) {
         a.tiles = 1;
-        auto run = [&](auto dma, auto kn) {
-          constexpr int KN = decltype(kn)::value;
+        auto run = [&](auto dma, auto nw, auto kn) {
+          constexpr int NW = decltype(nw)::value, KN = decltype(kn)::value;
           static std::atomic<uint64_t> dev;
-          return attend_launch(k_attend_short<T, DP, decltype(dma)::value, KN>, a, (int64_t)d->B * d->Hk * a.splits, Short<T, DP, KN>::LDS, dev, st);
+          return attend_launch(k_attend_short<T, DP, decltype(dma)::value, NW, KN>, a, (int64_t)d->B * d->Hk * a.splits,
+                               Short<T, DP, NW, KN>::LDS, dev, st, 64 * NW);
         };
         auto keys = [&](auto dma) {
-          return d->Tk <= 64 ? run(dma, std::integral_constant<int, 1>()) : run(dma, std::integral_constant<int, 2>());
+          constexpr std::integral_constant<int, 4> four;
+          constexpr std::integral_constant<int, DP == 64 ? 8 : 4> waves;
+          if (d->Tk <= 64) return run(dma, four, std::integral_constant<int, 1>());
+          return run(dma, waves, std::integral_constant<int, 8 / decltype(waves)::value>());
         };
         e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? keys(std::true_type()) : keys(std::false_type());
       }
