@@ -83,8 +83,10 @@ __device__ __forceinline__ void load_logits(u32x4 (&raw)[NV], float& end, const 
   if (!legal) return;
   if (has_end<T>(t, we) && !legal[end_place<T>(t, we)]) end = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
     if (c0 + i * STEP < W / vec<T>::N) raw[i] = allow<T>(raw[i], legal, c0 + i * STEP);
+    __builtin_amdgcn_sched_barrier(0);                 // (one vector's bytes at a time, as below)
+  }
 }
 
 // A product that is 0 where a factor is, whatever the other (an infinity or NaN): v_mul_legacy_f32.
@@ -260,7 +262,7 @@ __device__ __forceinline__ void top_out(const LogArgs& a, int64_t row, int n, u6
 
 // Whole rows, TPR threads to each, NV vectors in a thread. TOP: best tokens are asked for (then TPR >= 64).
 template <typename T, int TPR, int NV, bool TOP>
-__global__ void __launch_bounds__(row_threads(TPR)) k_logprob_rows(LogArgs a) {
+__global__ void __launch_bounds__(row_threads(TPR), NV == 16 ? 4 : 1) k_logprob_rows(LogArgs a) {
   constexpr int V = vec<T>::N, RPB = row_count(TPR), NT = TPR < 64 ? 64 : TPR;
   __shared__ float red[5][16];
   __shared__ TopLds<NT> top[TOP ? RPB : 1];
@@ -298,21 +300,24 @@ __global__ void __launch_bounds__(row_threads(TPR)) k_logprob_rows(LogArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       float v[V];
+      opaque_vec(raw[i]);
       vec<T>::unpack(raw[i], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) mine = fmaxf(mine, v[k]);
+      __builtin_amdgcn_sched_barrier(0);
     }
     m = group_reduce<TPR>(mine, op_max(), red[0]);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
     const float m0 = m > -INFINITY ? m : 0.f;
     Sums z = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       float v[V];
+      opaque_vec(raw[i]);                              // (here, not ahead of the loop: unpacked before, all of them take 100 registers more)
       vec<T>::unpack(raw[i], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) z.add(m0, v[k]);
+      // (added up here: the compiler kept all of the second sum's terms for behind the first one's barrier)
+      asm volatile("" : "+v"(z.q));
       __builtin_amdgcn_sched_barrier(0);               // (one vector unpacked at a time)
     }
     z.add(m0, end);
@@ -335,13 +340,12 @@ __global__ void __launch_bounds__(row_threads(TPR)) k_logprob_rows(LogArgs a) {
   some = group_reduce<TPR>(some, op_max(), red[4]);
   T* dx = (T*)a.dx + row * a.ldd;
   const RowGrad g = row_grad(here && a.dent ? a.dent[row] : 0.f, A, some != 0.f, m, logs, H);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) opaque_vec(raw[i]);
   // (dx may be x: every logit that is fetched by its place, or again, has been)
   if constexpr (TPR > 64) __syncthreads();
   if (here) {
     auto put = [&](auto f) {
       store_row<TPR, T, NV>(dx, t, a.V, [&](int i, float (&v)[V]) {
+        opaque_vec(raw[i]);
         vec<T>::unpack(raw[i], v);
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = f(v[k]);

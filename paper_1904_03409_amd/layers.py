@@ -17,8 +17,7 @@ import torch
 
 from . import stacklstm as _sl
 from .head import DTYPES, SLSTM_BF16, SLSTM_F32, _arr, _ld, _mat, _type, _ws
-from .head import _here as _stream_of
-from .stacklstm import StackLSTMError, _check
+from .stacklstm import StackLSTMError, _check, _stream
 
 EXPORTS = ("stacklstm_attend_fwd_workspace_bytes", "stacklstm_attend_bwd_workspace_bytes", "stacklstm_attend_fwd",
            "stacklstm_attend_bwd", "stacklstm_logprob_workspace_bytes", "stacklstm_logprob_fwd", "stacklstm_logprob_bwd",
@@ -80,13 +79,15 @@ def _bytes(name, d):
 
 def _call(name, t, stream, check, *args):
     """The call on t's device (kernels go to the current one), its stream the one given or t's current one."""
-    at, now = t.get_device(), torch.cuda.current_device()
-    if at != now:
-        with torch.cuda.device(at):
-            rc = getattr(load_library(), name)(*args, _stream_of(stream, t))
+    at = t.get_device()
+    fn = getattr(_lib or load_library(), name)
+    stream = torch._C._cuda_getCurrentRawStream(at) if stream is None else _stream(stream)
+    if at == torch.cuda.current_device():
+        rc = fn(*args, stream)
     else:
-        rc = getattr(load_library(), name)(*args, _stream_of(stream, t))
-    if check:
+        with torch.cuda.device(at):
+            rc = fn(*args, stream)
+    if check and rc:
         _check(rc, name)
     return rc
 
@@ -94,8 +95,7 @@ def _call(name, t, stream, check, *args):
 # ----------------------------------------------------------------------------- attention
 
 def strides_of(t):
-    """A [B, T, H, D] tensor's strides for the dims (zeros: dense); its last axis has to be contiguous. An axis of one element has
-    any stride."""
+    """A [B, T, H, D] tensor's strides for the dims; its last axis has to be contiguous. An axis of one element has any stride."""
     if t is None:
         return slstm_strides(0, 0, 0)
     if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
@@ -103,7 +103,7 @@ def strides_of(t):
     B, T, H, D = t.shape
     dense = (T * H * D, H * D, D)
     s = [d if n < 2 else v for v, d, n in zip(t.stride(), dense, (B, T, H))]
-    return slstm_strides(0, 0, 0) if tuple(s) == dense else slstm_strides(*s)
+    return slstm_strides(*s)
 
 
 def make_attend_dims(B, Tq, Tk, Hq, Hk, D, type=SLSTM_F32, scale=None, **strides):
@@ -121,6 +121,9 @@ def stacklstm_attend_bwd_workspace_bytes(dims) -> int:
 
 def _heads(t, dtype, what, shape, s, optional=False):
     """Address of a [B, T, H, D] device tensor with the strides of the dims."""
+    b, n, h = s.b, s.t, s.h
+    if t is not None and t.dtype is dtype and t.is_cuda and t.shape == shape and t.stride() == (b, n, h, 1) and (b or n or h):
+        return t.data_ptr()                      # (as most are: a small call takes as long as its checks)
     if t is None:
         if optional:
             return None
@@ -132,15 +135,16 @@ def _heads(t, dtype, what, shape, s, optional=False):
     if t.shape != shape:
         raise ValueError(f"{what} must have shape {shape}, got {tuple(t.shape)}")
     B, T, H, D = shape
-    want = (s.b, s.t, s.h) if s.b or s.t or s.h else (T * H * D, H * D, D)
-    if t.numel() and (any(n > 1 and v != w for v, w, n in zip(t.stride(), want, shape)) or (D > 1 and t.stride(3) != 1)):
+    want = (b, n, h) if b or n or h else (T * H * D, H * D, D)
+    if t.numel() and (any(m > 1 and v != w for v, w, m in zip(t.stride(), want, shape)) or (D > 1 and t.stride(3) != 1)):
         raise ValueError(f"{what} must have strides {want + (1,)}, got {t.stride()}")
     return t.data_ptr()
 
 
 def _lens(d, q_len, k_len, mask):
-    return (_arr(q_len, torch.int32, "q_len", (d.B,), True), _arr(k_len, torch.int32, "k_len", (d.B,), True),
-            _arr(mask, torch.uint8, "mask", (d.B, d.Tk), True))
+    return (None if q_len is None else _arr(q_len, torch.int32, "q_len", (d.B,)),
+            None if k_len is None else _arr(k_len, torch.int32, "k_len", (d.B,)),
+            None if mask is None else _arr(mask, torch.uint8, "mask", (d.B, d.Tk)))
 
 
 def stacklstm_attend_fwd(dims, q, k, v, q_len, k_len, mask, y, stats, workspace, stream=None, check=True) -> int:

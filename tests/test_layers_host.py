@@ -134,7 +134,7 @@ def test_strides_of_views():
     s = ly.strides_of(t.transpose(0, 1))
     assert (s.b, s.t, s.h) == (16, 48, 8)
     s = ly.strides_of(t)
-    assert (s.b, s.t, s.h) == (0, 0, 0)
+    assert (s.b, s.t, s.h) == (48, 16, 8)
     # one sequence: its stride is any
     s = ly.strides_of(t[:1, :, :, :4])
     assert (s.t, s.h) == (16, 8)
