@@ -558,7 +558,7 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
         };
         auto keys = [&](auto dma) {
           constexpr std::integral_constant<int, 4> four;
-          constexpr std::integral_constant<int, DP == 64 ? 8 : 4> waves;
+          constexpr std::integral_constant<int, DP == 64 && sizeof(T) == 4 ? 8 : 4> waves;
           if (d->Tk <= 64) return run(dma, four, std::integral_constant<int, 1>());
           return run(dma, waves, std::integral_constant<int, 8 / decltype(waves)::value>());
         };

@@ -239,36 +239,67 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
   }
 }
 
-// Rows' splits joined, four columns to a thread and 2^shift threads to a row. (A wave to a row, with a column to a lane: 18 us for 32768
-// rows of 64 in two splits.)
+// Rows' splits joined: four columns to a thread, 2^cs threads to a row's columns, its splits shared by 2^gs groups of those. (The parts come
+// from other XCDs' workgroups, 2 us away: one thread for a row's columns took 8 us for 16 splits and 25 for 64.)
 template <typename T>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int shift) {
-  const int rows = a.Tq * a.G, all = rows * a.B * a.Hk;
-  const int64_t row64 = ((a.first + blockIdx.x) << (8 - shift)) + (threadIdx.x >> shift);
-  const int n = (threadIdx.x & ((1 << shift) - 1)) * 4;
-  if (row64 >= all || n >= a.D) return;
-  const int64_t row = row64;
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int cs, int gs) {
+  __shared__ f32x4 sv[256];
+  __shared__ float sml[2][256];
+  const int rows = a.Tq * a.G, all = rows * a.B * a.Hk, t = threadIdx.x;
+  const int64_t row = ((a.first + blockIdx.x) << (8 - cs - gs)) + (t >> (cs + gs));
+  const int n = (t & ((1 << cs) - 1)) * 4, g = t >> cs & ((1 << gs) - 1);
+  const bool here = row < all && n < a.D;
   float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.ml[2 * ((int64_t)s * all + row)]);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int s = 0; s < a.splits; ++s) {
-    const float ms = a.ml[2 * ((int64_t)s * all + row)], f = ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m);
-    float p[4];
-    vec<float>::unpack(load_vec(a.part + ((int64_t)s * all + row) * a.D, n / 4, a.D), p);
-    l += a.ml[2 * ((int64_t)s * all + row) + 1] * f;
+  for (int s0 = g; s0 < a.splits; s0 += 4 << gs) {
+    float ms[4], ls[4];
+    u32x4 p[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] += p[k] * f;
+    for (int i = 0; i < 4; ++i) {
+      const bool in = here && s0 + (i << gs) < a.splits;
+      const int64_t at = in ? (int64_t)(s0 + (i << gs)) * all + row : 0;
+      ms[i] = in ? a.ml[2 * at] : -INFINITY, ls[i] = in ? a.ml[2 * at + 1] : 0.f;
+      p[i] = in ? load_vec(a.part + at * a.D, n / 4, a.D) : u32x4{0u, 0u, 0u, 0u};
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, ms[i]);
+    const float back = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    m = top, l *= back;
+    v *= back;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = ms[i] == m ? 1.f : __builtin_amdgcn_exp2f(ms[i] - m);
+      float x[4];
+      vec<float>::unpack(p[i], x);
+      l += ls[i] * f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += x[k] * f;
+    }
   }
+  if (gs) {
+    sv[t] = v, sml[0][t] = m, sml[1][t] = l;
+    __syncthreads();
+    if (g) return;
+    const float m0 = m;
+    for (int i = 1; i < 1 << gs; ++i) m = fmaxf(m, sml[0][t + (i << cs)]);
+    const float f0 = m0 == m ? 1.f : __builtin_amdgcn_exp2f(m0 - m);
+    v *= f0, l *= f0;
+    for (int i = 1; i < 1 << gs; ++i) {
+      const int o = t + (i << cs);
+      const float f = sml[0][o] == m ? 1.f : __builtin_amdgcn_exp2f(sml[0][o] - m);
+      v += sv[o] * f, l += sml[1][o] * f;
+    }
+  }
+  if (!here) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int bh = (int)row / rows, r = (int)row - bh * rows, b = bh / a.Hk, t = r / a.G, h = (bh - b * a.Hk) * a.G + r % a.G;
-  T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
+  const int bh = (int)row / rows, r = (int)row - bh * rows, b = bh / a.Hk, place = r / a.G, h = (bh - b * a.Hk) * a.G + r % a.G;
+  T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)place * a.sy.t + (int64_t)h * a.sy.h;
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if (n + k < a.D) from_f32(y[n + k], l == 0.f ? 0.f : v[k] * inv);
   if (a.stats && n == 0) {
-    float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * 2;
+    float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + place) * 2;
     s[0] = l == 0.f ? INFINITY : m;
     s[1] = inv;
   }
@@ -352,11 +383,12 @@ extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, c
     };
     hipError_t e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     if (e == hipSuccess && p.splits > 1) {
-      int shift = 0;
-      while (4 << shift < d->D) ++shift;
-      in_pieces((((int64_t)d->B * d->Tq * d->Hq << shift) + 255) / 256, kMostGroups, [&](int64_t b0, int64_t n) {
+      int cs = 0, gs = 0;
+      while (4 << cs < d->D) ++cs;
+      while (cs + gs < 8 && 1 << gs < p.splits) ++gs;
+      in_pieces((((int64_t)d->B * d->Tq * d->Hq << (cs + gs)) + 255) / 256, kMostGroups, [&](int64_t b0, int64_t n) {
         a.first = b0;
-        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)n), dim3(256), 0, st, a, shift);
+        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)n), dim3(256), 0, st, a, cs, gs);
       });
       e = hipGetLastError();
     }

@@ -77,6 +77,13 @@ def _bytes(name, d):
     return n
 
 
+def _space(t):
+    """Address and size of a work space."""
+    if t is not None and t.dtype is torch.uint8 and t.is_cuda and t.is_contiguous():
+        return t.data_ptr(), t.numel()
+    return _ws(t)
+
+
 def _call(name, t, stream, check, *args):
     """The call on t's device (kernels go to the current one), its stream the one given or t's current one."""
     at = t.get_device()
@@ -150,7 +157,7 @@ def _lens(d, q_len, k_len, mask):
 def stacklstm_attend_fwd(dims, q, k, v, q_len, k_len, mask, y, stats, workspace, stream=None, check=True) -> int:
     d, t = dims, DTYPES[dims.type]
     sq, sk = (d.B, d.Tq, d.Hq, d.D), (d.B, d.Tk, d.Hk, d.D)
-    ws, n = _ws(workspace)
+    ws, n = _space(workspace)
     return _call("stacklstm_attend_fwd", q, stream, check, d, _heads(q, t, "q", sq, d.q), _heads(k, t, "k", sk, d.k),
                  _heads(v, t, "v", sk, d.v), *_lens(d, q_len, k_len, mask), _heads(y, t, "y", sq, d.y),
                  _arr(stats, torch.float32, "stats", (d.B, d.Hq, d.Tq, 2), True), ws, n)
@@ -159,7 +166,7 @@ def stacklstm_attend_fwd(dims, q, k, v, q_len, k_len, mask, y, stats, workspace,
 def stacklstm_attend_bwd(dims, q, k, v, q_len, k_len, mask, y, stats, dy, dq, dk, dv, workspace, stream=None, check=True) -> int:
     d, t = dims, DTYPES[dims.type]
     sq, sk = (d.B, d.Tq, d.Hq, d.D), (d.B, d.Tk, d.Hk, d.D)
-    ws, n = _ws(workspace)
+    ws, n = _space(workspace)
     return _call("stacklstm_attend_bwd", q, stream, check, d, _heads(q, t, "q", sq, d.q), _heads(k, t, "k", sk, d.k),
                  _heads(v, t, "v", sk, d.v), *_lens(d, q_len, k_len, mask), _heads(y, t, "y", sq, d.y),
                  _arr(stats, torch.float32, "stats", (d.B, d.Hq, d.Tq, 2)), _heads(dy, t, "dy", sq, d.dy),
@@ -246,7 +253,7 @@ def _rows_grad(d, dlogp, dentropy):
 
 
 def stacklstm_logprob_fwd(dims, logits, legal, token, logp, entropy, index, value, stats, workspace, stream=None, check=True) -> int:
-    ws, n = _ws(workspace)
+    ws, n = _space(workspace)
     return _call("stacklstm_logprob_fwd", logits, stream, check, dims, *_rows_in(dims, logits, legal, token),
                  *_rows_out(dims, logp, entropy, index, value), _arr(stats, torch.float32, "stats", (dims.rows, 3), True), ws, n)
 
@@ -259,7 +266,7 @@ def stacklstm_logprob_bwd(dims, logits, legal, token, stats, dlogp, dentropy, dl
 
 def stacklstm_logprob_step(dims, logits, legal, token, dlogp, dentropy, logp, entropy, index, value, dlogits, workspace,
                            stream=None, check=True) -> int:
-    ws, n = _ws(workspace)
+    ws, n = _space(workspace)
     return _call("stacklstm_logprob_step", logits, stream, check, dims, *_rows_in(dims, logits, legal, token),
                  *_rows_grad(dims, dlogp, dentropy), *_rows_out(dims, logp, entropy, index, value),
                  _mat(dlogits, DTYPES[dims.type], "dlogits", dims.rows, dims.V, dims.ld_dlogits), ws, n)
