@@ -28,7 +28,7 @@ struct AttendArgs {
   float *delta;                                        // [B, Hq, Tq]: dy . y
   // splits: [splits][B Hk][rows][D] sums, [splits][B Hk][rows][2] references and sums; of dk and dv [splits][2][B Hk][Tk][D]
   float *part, *ml;
-  int tiles, splits, chunk;                            // row tiles of a (sequence, key head); keys of a split
+  int tiles, splits, chunk, reps;                      // workgroups of a (sequence, key head) and split; keys of a split; row tiles of a workgroup
   int64_t first;                                       // a launch's first workgroup
   int64_t piece, full;                                 // neighbours on an XCD; how many are dealt out that way
 };
@@ -225,7 +225,7 @@ struct Mover {
   }
   // rows 0 .. n of base (more than 0), those with mask byte 0 (mask not NULL) left out
   __device__ __forceinline__ void go(const T* base, int64_t stride, int D, int n, const uint8_t* mask, unsigned char* tile) {
-    n = min(n, ROWS);
+    n = uni(min(n, ROWS));                             // (descriptors are scalar registers)
     if constexpr (DMA) {
       const rsrc_t rs = make_rsrc(base, (size_t)((n - 1) * stride + D) * sizeof(T));
       const int wave = uni(threadIdx.x >> 6);

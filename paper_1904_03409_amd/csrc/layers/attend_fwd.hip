@@ -44,7 +44,9 @@ __device__ __forceinline__ void fwd_row(const AttendArgs& a, int b, int t, int h
 
 }  // namespace
 
-template <typename T, int DP, int QT, int WK, bool DMA>
+// LOOP: keys of two tiles at most, which stay in LDS while the workgroup goes through a.reps row tiles, the next one's queries on their
+// way during this one's products: a row tile then costs neither a start nor a wait for its keys.
+template <typename T, int DP, int QT, int WK, bool DMA, bool LOOP>
 __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fwd(AttendArgs a) {
   typedef Head<T, DP> H;
   typedef Fwd<T, DP, WK, DMA> F;
@@ -57,21 +59,33 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
   constexpr int ROWS = 16 * QT * (4 / WK);
   const int qlen = clamp_len(a.q_len, b, a.Tq), klen = clamp_len(a.k_len, b, a.Tk);
   const int kbeg = pl.split * a.chunk;
+  int tile = LOOP ? pl.tile * a.reps : pl.tile;
+  const int tend = LOOP ? min(tile + a.reps, (rows + ROWS - 1) / ROWS) : tile + 1;
   // (no query of the tile is there: no keys)
-  const int kend = pl.tile * ROWS / a.G < qlen ? min(klen, kbeg + a.chunk) : kbeg;
+  auto keys_end = [&] { return uni(tile * ROWS / a.G < qlen ? min(klen, kbeg + a.chunk) : kbeg); };
+  int kend = keys_end();
+  // place, head and row of the array of a lane's queries
   int qt_[QT], qh_[QT];
   bool here[QT];
-  u32x4 qr[QT][H::STEPS];
+  auto find = [&](int tile) {
 #pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    const int r = pl.tile * ROWS + 16 * (QT * wq + j) + l16;
-    here[j] = r < rows;
-    const int in = min(r, rows - 1);
-    qt_[j] = in / a.G;
-    qh_[j] = hk * a.G + in % a.G;
-    fetch_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h,
-                     here[j] && qt_[j] < qlen, a.D, lq, qr[j]);
-  }
+    for (int j = 0; j < QT; ++j) {
+      const int r = tile * ROWS + 16 * (QT * wq + j) + l16;
+      here[j] = r < rows;
+      const int in = min(r, rows - 1);
+      qt_[j] = in / a.G;
+      qh_[j] = hk * a.G + in % a.G;
+    }
+  };
+  u32x4 qr[QT][H::STEPS];
+  auto fetch = [&] {
+#pragma unroll
+    for (int j = 0; j < QT; ++j)
+      fetch_own<T, DP>((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)qt_[j] * a.sq.t + (int64_t)qh_[j] * a.sq.h,
+                       here[j] && qt_[j] < qlen, a.D, lq, qr[j]);
+  };
+  find(tile);
+  fetch();
   const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
   const T* vp = (const T*)a.v + (int64_t)b * a.sv.b + (int64_t)hk * a.sv.h;
   const uint8_t* mask = a.mask ? a.mask + (int64_t)b * a.Tk : nullptr;
@@ -84,6 +98,9 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
     mk.go(kp + (int64_t)k0 * a.sk.t, a.sk.t, a.D, kend - k0, there, stage(n));
     mv.go(vp + (int64_t)k0 * a.sv.t, a.sv.t, a.D, kend - k0, there, stage(n) + F::TILE);
   };
+  if (kbeg < kend) go(kbeg, 0);
+  for (bool again = false; tile < tend; ++tile, again = true) {
+  if (again) kend = keys_end();
   f32x4 o[QT][H::DT];
   float m[QT], l[QT];
 #pragma unroll
@@ -92,18 +109,23 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (kbeg < kend) go(kbeg, 0);
   frag q[QT][H::STEPS];
 #pragma unroll
   for (int j = 0; j < QT; ++j) place_own<T, DP>(qr[j], a.D, lq, q[j]);
+  if (LOOP && tile + 1 < tend) {
+    find(tile + 1);
+    fetch();
+  }
   for (int k0 = kbeg, n = 0; k0 < kend; k0 += F::KT, ++n) {
     const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const int first = k0 + wk * F::KW;
     const unsigned long long there = __ballot(lane < F::KW && first + lane < kend && (!mask || mask[first + lane]));
-    if constexpr (DMA) wait_vm<0>();
-    else mk.land(a.D, stage(n)), mv.land(a.D, stage(n) + F::TILE);
-    __syncthreads();
-    if (F::STAGES == 2 && k0 + F::KT < kend) go(k0 + F::KT, n + 1);
+    if (!LOOP || !again) {
+      if constexpr (DMA) wait_vm<0>();
+      else mk.land(a.D, stage(n)), mv.land(a.D, stage(n) + F::TILE);
+      __syncthreads();
+      if (F::STAGES == 2 && k0 + F::KT < kend) go(k0 + F::KT, n + 1);
+    }
     if (there) {
       f32x4 s[F::NU][H::SUB][QT];
 #pragma unroll
@@ -224,6 +246,7 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
       for (int dt = 0; dt < H::DT; ++dt) o[0][dt] += *(const f32x4*)(part + 16 * dt) * f;
     }
   }
+  if (LOOP) find(tile);
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
     if (!here[j]) continue;
@@ -236,6 +259,7 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
       store_cols<float, DP>(a.part + r * a.D, lq, a.D, [&](int dt) { return o[j][dt]; });
       if (lq == 0) a.ml[2 * r] = m[j], a.ml[2 * r + 1] = l[j];
     }
+  }
   }
 }
 
@@ -308,8 +332,9 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int cs, int g
 namespace {
 
 // Row tiles and splits. Up to 16 rows (queries times heads of a key) share their keys in a tile; more rows go 16 or 32 to a wave.
+constexpr int kLoopKeys = 128;                         // two tiles of heads of up to 64
 struct FwdPlan {
-  int qt, wk, rows, tiles, splits, chunk;
+  int qt, wk, rows, tiles, splits, chunk, reps;
 };
 FwdPlan fwd_plan(const slstm_attend_dims* d) {
   FwdPlan p;
@@ -317,7 +342,7 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
   // (heads of 256: 32 rows to a wave need more registers than there are)
   const bool wide = d->D > 128;
   if (R <= 16) p.qt = 1, p.wk = 4;
-  else if (R <= 64 || wide) p.qt = 1, p.wk = 1;
+  else if (R <= 64 || wide || d->type == SLSTM_F32) p.qt = 1, p.wk = 1;
   else p.qt = 2, p.wk = 1;
   if (getenv("ATT_QT") && p.wk == 1) p.qt = atoi(getenv("ATT_QT"));
   p.rows = 16 * p.qt * (4 / p.wk);
@@ -329,6 +354,12 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
   p.chunk = (((d->Tk + p.splits - 1) / p.splits) + 127) / 128 * 128;
   if (p.chunk < 128) p.chunk = 128;
   p.splits = std::max(1, (d->Tk + p.chunk - 1) / p.chunk);
+  // few keys, many row tiles: several of them to a workgroup as long as there are three workgroups to a compute unit
+  p.reps = 1;
+  if (p.wk == 1 && R > 64 && d->Tk <= kLoopKeys && d->D <= 64 && p.splits == 1) {
+    p.reps = (int)std::max<int64_t>(1, std::min<int64_t>(p.tiles, groups / 768));
+    p.tiles = (p.tiles + p.reps - 1) / p.reps;
+  }
   return p;
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -353,7 +384,7 @@ extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, c
   AttendArgs a = attend_args(d);
   a.q = q, a.k = k, a.v = v, a.q_len = q_len, a.k_len = k_len, a.mask = mask, a.out = y, a.stats = stats;
   const FwdPlan p = fwd_plan(d);
-  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
+  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk, a.reps = p.reps;
   if (p.splits > 1) {
     if (!workspace || ((uintptr_t)workspace & 15u)) return SLSTM_EINVAL;
     if (ws_bytes < stacklstm_attend_fwd_workspace_bytes(d)) return SLSTM_EWORKSPACE;
@@ -371,15 +402,22 @@ extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, c
       if constexpr (DMA || sizeof(T) * DP <= 512) {
         if (p.wk == 4) {
           static std::atomic<uint64_t> dev;
-          return attend_launch(k_attend_fwd<T, DP, 1, 4, DMA>, a, groups, Fwd<T, DP, 4, DMA>::LDS, dev, st);
+          return attend_launch(k_attend_fwd<T, DP, 1, 4, DMA, false>, a, groups, Fwd<T, DP, 4, DMA>::LDS, dev, st);
+        }
+      }
+      if constexpr (DP <= 64) {
+        static_assert(2 * Fwd<T, DP, 1, DMA>::KT >= kLoopKeys && Fwd<T, DP, 1, DMA>::STAGES == 2, "all keys stay");
+        if (p.reps > 1) {
+          static std::atomic<uint64_t> dev;
+          return attend_launch(k_attend_fwd<T, DP, (sizeof(T) == 4 ? 1 : 2), 1, DMA, true>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
         }
       }
       if (DP > 128 || p.qt == 1) {
         static std::atomic<uint64_t> dev;
-        return attend_launch(k_attend_fwd<T, DP, 1, 1, DMA>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+        return attend_launch(k_attend_fwd<T, DP, 1, 1, DMA, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
       }
       static std::atomic<uint64_t> dev;
-      return attend_launch(k_attend_fwd<T, DP, (DP > 128 ? 1 : 2), 1, DMA>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+      return attend_launch(k_attend_fwd<T, DP, (DP > 128 || sizeof(T) == 4 ? 1 : 2), 1, DMA, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
     };
     hipError_t e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     if (e == hipSuccess && p.splits > 1) {
