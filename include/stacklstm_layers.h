@@ -41,6 +41,8 @@ typedef struct {
   slstm_strides y, dq, dk, dv;      /* of outputs: all three 0: dense; no two elements at one place (SLSTM_EINVAL) */
 } slstm_attend_dims;       /* B Tq Hq and B Tk Hk < 2^31; strides < 2^40 */
 
+/* Floats of `stats` for a query and head (0 for invalid dims). */
+int32_t stacklstm_attend_stats_width(const slstm_attend_dims* d);
 /* Bytes of work space (0 for invalid dims). */
 size_t stacklstm_attend_fwd_workspace_bytes(const slstm_attend_dims* d);
 size_t stacklstm_attend_bwd_workspace_bytes(const slstm_attend_dims* d);
@@ -48,7 +50,8 @@ size_t stacklstm_attend_bwd_workspace_bytes(const slstm_attend_dims* d);
 /*  q [B, Tq, Hq, D], k and v [B, Tk, Hk, D] (may be NULL with Tk = 0)                            (read)
  *  q_len, k_len [B] int32 or NULL: all (taken as 0 below 0, as Tq / Tk above)                      (read)
  *  mask [B, Tk] uint8 or NULL (0: not there)                                                      (read)
- *  y [B, Tq, Hq, D]; stats [B, Hq, Tq, 2] float or NULL, for a backward                           (written)
+ *  y [B, Tq, Hq, D]; stats [B, Hq, Tq, stacklstm_attend_stats_width] float or NULL: the softmax's
+ *  reference and sum, and what y's rounding to 16 bits takes off, for a backward                   (written)
  * With SLSTM_BF16 the p of a product with v are rounded to bfloat16, the operands of the matrix units. */
 int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, const void* k, const void* v, const int32_t* q_len,
                          const int32_t* k_len, const uint8_t* mask, void* y, float* stats, void* workspace, size_t ws_bytes,

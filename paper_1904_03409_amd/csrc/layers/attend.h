@@ -23,9 +23,11 @@ struct AttendArgs {
   const int32_t *q_len, *k_len;
   const uint8_t* mask;
   void *out, *dq, *dk, *dv;
-  float* stats;                                        // [B, Hq, Tq, 2]: reference of the row's exponents (base 2), 1 / sum
+  // [B, Hq, Tq, width]: reference of a row's exponents (base 2), 1 / sum, and (width > 2) what y's rounding took off, a byte to an element
+  float* stats;
   const float* stats_in;
-  float *delta;                                        // [B, Hq, Tq]: dy . y
+  int width;
+  float *delta;                                        // [B, Hq, Tq, 3]: what k_attend_dkv reads of a row: reference, 1 / sum, dy . y
   // splits: [splits][B Hk][rows][D] sums, [splits][B Hk][rows][2] references and sums; of dk and dv [splits][2][B Hk][Tk][D]
   float *part, *ml;
   int tiles, splits, chunk, reps;                      // workgroups of a (sequence, key head) and split; keys of a split; row tiles of a workgroup
@@ -295,6 +297,27 @@ __device__ __forceinline__ void store_some(T* row, int n0, int lq, int D, F f) {
 template <typename T, int DP, typename F>
 __device__ __forceinline__ void store_cols(T* row, int lq, int D, F f) { store_some<T, DP / 16>(row, 0, lq, D, f); }
 
+// What a 16-bit y loses, in 1/254 of the last place of the rounded value: delta = dy . y of a backward takes it back. Without it delta is
+// off by 2^-9 of its terms, and where one key outweighs the others p (dp - delta) is small beside them: gradients of 4 keys were 0.0036
+// off, twice the rounding of their outputs. (Keys of one tile alone: k_attend_dq sums p dp instead.)
+__device__ __forceinline__ float last_place(uint32_t bits) {             // of a bfloat16; 0 for zeros and what is below 2^-119
+  const int e = (int)(bits >> 7 & 0xffu) - 7;
+  return e > 0 ? __uint_as_float((uint32_t)e << 23) : 0.f;
+}
+__device__ __forceinline__ uint32_t lost_byte(float v) {
+  const uint32_t b = f32_to_bf16_bits(v);
+  const float place = last_place(b), off = v - bf16_bits_to_f32((bf16_t)b);
+  // (a power of two: 1 / place by its exponent)
+  const float q = place > 0.f && fabsf(off) <= place ? off * __uint_as_float(0x7f000000u - __float_as_uint(place)) * 254.f : 0.f;
+  return (uint32_t)(int)__builtin_rintf(q) & 0xffu;
+}
+__device__ __forceinline__ float lost_value(float y, uint32_t byte) {
+  return (float)(int8_t)byte * (last_place(__float_as_uint(y) >> 16) * (1.f / 254.f));
+}
+// A row's statistics: l = 0: no key.
+__device__ __forceinline__ float* stats_row(const AttendArgs& a, float* stats, int b, int h, int t) {
+  return stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * a.width;
+}
 __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
   return len ? max(0, min(len[b], most)) : most;
 }
@@ -364,6 +387,11 @@ inline bool attend_ok(const slstm_attend_dims* d) {
   }
   return true;
 }
+// Whether a backward takes all keys at once (k_attend_short), which needs no y.
+inline bool attend_few_keys(const slstm_attend_dims* d) { return d->Tk >= 1 && d->Tk <= 128 && d->D <= 64; }
+inline int attend_stats_width(const slstm_attend_dims* d) {
+  return d->type == SLSTM_BF16 && !attend_few_keys(d) ? 2 + (d->D + 3) / 4 : 2;
+}
 inline AttendArgs attend_args(const slstm_attend_dims* d) {
   AttendArgs a = {};
   a.B = d->B, a.Tq = d->Tq, a.Tk = d->Tk, a.Hq = d->Hq, a.Hk = d->Hk, a.G = d->Hq / d->Hk, a.D = d->D;
@@ -372,7 +400,7 @@ inline AttendArgs attend_args(const slstm_attend_dims* d) {
   a.sq = strides_of(d->q, Tq, Hq, D), a.sy = strides_of(d->y, Tq, Hq, D), a.sdy = strides_of(d->dy, Tq, Hq, D);
   a.sdq = strides_of(d->dq, Tq, Hq, D), a.sk = strides_of(d->k, Tk, Hk, D), a.sv = strides_of(d->v, Tk, Hk, D);
   a.sdk = strides_of(d->dk, Tk, Hk, D), a.sdv = strides_of(d->dv, Tk, Hk, D);
-  a.splits = 1;
+  a.splits = 1, a.width = attend_stats_width(d);
   return a;
 }
 // f(type, width): the kernels' variants.

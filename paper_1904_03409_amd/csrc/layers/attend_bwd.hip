@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
   int qt_[QT], qh_[QT];
   bool here[QT], used[QT];
   u32x4 qr[QT][H::STEPS], gr[QT][H::STEPS], yr[QT][H::STEPS];
+  uint32_t lost[sizeof(T) == 2 ? QT : 1][H::STEPS][2];                   // what y's rounding took off
   float m[QT], inv[QT], delta[QT];
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
@@ -73,8 +74,17 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
     fetch_own<T, DP>((const T*)a.y + (int64_t)b * a.sy.b + (int64_t)qt_[j] * a.sy.t + (int64_t)qh_[j] * a.sy.h, used[j], a.D, lq, yr[j]);
     m[j] = INFINITY, inv[j] = 0.f;
     if (used[j]) {
-      const float* st = a.stats_in + (((int64_t)b * a.Hq + qh_[j]) * a.Tq + qt_[j]) * 2;
+      const float* st = stats_row(a, (float*)a.stats_in, b, qh_[j], qt_[j]);
       m[j] = st[0], inv[j] = st[1];
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int s = 0; s < H::STEPS; ++s)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int w = 2 * (4 * s + lq) + i;
+            lost[j][s][i] = 4 * w < a.D ? ((const uint32_t*)st)[2 + w] : 0u;
+          }
+      }
     }
   }
   const T* kp = (const T*)a.k + (int64_t)b * a.sk.b + (int64_t)hk * a.sk.h;
@@ -106,12 +116,25 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
 #pragma unroll
     for (int s = 0; s < H::STEPS; ++s)
 #pragma unroll
-      for (int e = 0; e < H::V; ++e) d += (float)g[j][s][e] * (float)y[s][e];
+      for (int e = 0; e < H::V; ++e) {
+        float v = (float)y[s][e];
+        if constexpr (sizeof(T) == 2) v += used[j] ? lost_value(v, lost[j][s][e >> 2] >> (8 * (e & 3))) : 0.f;
+        d += (float)g[j][s][e] * v;
+      }
     // (a query without keys: nothing, whatever dy holds)
     used[j] = inv[j] != 0.f;
     delta[j] = used[j] ? rows_sum(d) : 0.f;
-    if (here[j] && lq == 0) a.delta[((int64_t)b * a.Hq + qh_[j]) * a.Tq + qt_[j]] = delta[j];
   }
+  auto put_delta = [&] {
+#pragma unroll
+    for (int j = 0; j < QT; ++j)
+      if (here[j] && lq == 0) {
+        float* to = a.delta + (((int64_t)b * a.Hq + qh_[j]) * a.Tq + qt_[j]) * 3;
+        to[0] = m[j], to[1] = inv[j], to[2] = delta[j];
+      }
+  };
+  const bool one = kend <= F::R;                       // all keys in one tile
+  if (!one || kend <= 0) put_delta();
   for (int k0 = 0, n = 0; k0 < kend; k0 += F::R, ++n) {
     const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const unsigned long long there = __ballot(lane < F::R && k0 + lane < kend && (!mask || mask[k0 + lane]));
@@ -119,26 +142,56 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
     else mk.land(a.D, stage(n)), mv.land(a.D, stage(n) + F::TILE);
     __syncthreads();
     if (k0 + F::R < kend) go(k0 + F::R, n + 1);
+    // p and dp of score tile i of unit u
+    auto probs = [&](int u, int i, f32x4 (&p)[QT], f32x4 (&dp)[QT]) {
+#pragma unroll
+      for (int j = 0; j < QT; ++j) p[j] = dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      scores<T, DP, QT>(p, kt, u * H::UNIT, i, l16, lq, q);
+      scores<T, DP, QT>(dp, vt, u * H::UNIT, i, l16, lq, g);
+      const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+#pragma unroll
+      for (int j = 0; j < QT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = bits >> r & 1 ? p[j][r] * a.c : -INFINITY;
+          p[j][r] = __builtin_amdgcn_exp2f(x - m[j]) * inv[j];
+        }
+    };
+    if (one) {
+      // delta from the same p and dp that it is taken from: with one key their difference is 0, with few as exact as they are
+      float part[QT];
+#pragma unroll
+      for (int j = 0; j < QT; ++j) part[j] = 0.f;
+#pragma unroll 1
+      for (int u = 0; u < F::NU; ++u)
+#pragma unroll
+        for (int i = 0; i < H::SUB; ++i) {
+          f32x4 p[QT], dp[QT];
+          probs(u, i, p, dp);
+#pragma unroll
+          for (int j = 0; j < QT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) part[j] += p[j][r] * dp[j][r];
+        }
+#pragma unroll
+      for (int j = 0; j < QT; ++j) {
+        part[j] = rows_sum(part[j]);
+        delta[j] = used[j] ? part[j] : 0.f;
+      }
+      put_delta();
+    }
 #pragma unroll
     for (int u = 0; u < F::NU; ++u) {
       frag w[QT];
 #pragma unroll
       for (int i = 0; i < H::SUB; ++i) {
-        f32x4 s[QT], dp[QT];
-#pragma unroll
-        for (int j = 0; j < QT; ++j) s[j] = dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        scores<T, DP, QT>(s, kt, u * H::UNIT, i, l16, lq, q);
-        scores<T, DP, QT>(dp, vt, u * H::UNIT, i, l16, lq, g);
-        const uint32_t bits = (uint32_t)(there >> (u * H::UNIT + row_of<T>(i, 4 * lq)));
+        f32x4 p[QT], dp[QT];
+        probs(u, i, p, dp);
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
           f32x4 ds;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float x = bits >> r & 1 ? s[j][r] * a.c : -INFINITY;
-            const float p = __builtin_amdgcn_exp2f(x - m[j]) * inv[j];
-            ds[r] = p * (dp[j][r] - delta[j]);
-          }
+          for (int r = 0; r < 4; ++r) ds[r] = p[j][r] * (dp[j][r] - delta[j]);
           put_weights(w[j], i, ds);
         }
       }
@@ -201,21 +254,24 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
     t0 = uni(n0 % tiles) * F::R;
   }
   auto stage = [&](int n) { return sm + (n & 1) * 2 * F::TILE; };
+  // (pointers go on by steps: products of 64 bits for each tile took as long as its first matrix products)
+  const T *qp = (const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h;
+  const T *gp = (const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h;
+  const float* sp = a.delta + (((int64_t)b * a.Hq + h) * a.Tq + t0) * 3;
+  const int64_t qstep = F::R * a.sq.t, gstep = F::R * a.sdy.t;
   auto go = [&](int n) {
     // (ahead of the DMAs: before it writes a register that a load may be in flight for, the compiler waits for all that is)
     if (tid < F::R) {
       tm = INFINITY, ti = td = 0.f;
-      if (t0 + tid < qend) {
-        const int64_t row = ((int64_t)b * a.Hq + h) * a.Tq + t0;
-        const float *st = a.stats_in + 2 * row, *de = a.delta + row;
-        tm = st[2 * tid], ti = st[2 * tid + 1], td = de[tid];
-      }
+      if (t0 + tid < qend) tm = sp[3 * tid], ti = sp[3 * tid + 1], td = sp[3 * tid + 2];
     }
-    mq.go((const T*)a.q + (int64_t)b * a.sq.b + (int64_t)t0 * a.sq.t + (int64_t)h * a.sq.h, a.sq.t, a.D, qend - t0, nullptr, stage(n));
-    mg.go((const T*)a.dy + (int64_t)b * a.sdy.b + (int64_t)t0 * a.sdy.t + (int64_t)h * a.sdy.h, a.sdy.t, a.D, qend - t0, nullptr,
-          stage(n) + F::TILE);
-    t0 += F::R;
-    if (t0 >= qend) t0 = 0, ++h;
+    mq.go(qp, a.sq.t, a.D, qend - t0, nullptr, stage(n));
+    mg.go(gp, a.sdy.t, a.D, qend - t0, nullptr, stage(n) + F::TILE);
+    t0 += F::R, qp += qstep, gp += gstep, sp += 3 * F::R;
+    if (t0 >= qend) {
+      qp += a.sq.h - tiles * qstep, gp += a.sdy.h - tiles * gstep, sp += 3 * (a.Tq - tiles * F::R);
+      t0 = 0;
+    }
   };
   if (n0 < all) go(n0);
   frag k[KN][H::STEPS], v[BIG ? 1 : KN][H::STEPS];
@@ -502,7 +558,7 @@ struct KeyPlan {
 };
 KeyPlan key_plan(const slstm_attend_dims* d) {
   KeyPlan p;
-  p.one = d->Tk >= 1 && d->Tk <= 128 && d->D <= 64;
+  p.one = attend_few_keys(d);
   p.big = d->type == SLSTM_BF16 && d->D > 64 && d->D <= 128 && d->Tk > 128;
   const int keys = p.one ? 128 : p.big ? 256 : d->D > 128 || (d->D > 64 && d->type == SLSTM_F32) ? 64 : 128;
   p.tiles = (d->Tk + keys - 1) / keys;
@@ -517,7 +573,7 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 extern "C" size_t stacklstm_attend_bwd_workspace_bytes(const slstm_attend_dims* d) {
   if (!attend_ok(d)) return 0;
   const KeyPlan p = key_plan(d);
-  const size_t delta = up256((size_t)d->B * d->Tq * d->Hq * 4 + 16);
+  const size_t delta = up256((size_t)d->B * d->Tq * d->Hq * 12 + 16);
   return p.splits > 1 ? delta + (size_t)p.splits * 2 * d->B * d->Hk * d->Tk * d->D * 4 : delta;
 }
 
@@ -539,7 +595,7 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
   AttendArgs a = attend_args(d);
   a.q = q, a.k = k, a.v = v, a.q_len = q_len, a.k_len = k_len, a.mask = mask, a.y = y, a.stats_in = stats, a.dy = dy;
   a.dq = dq, a.dk = dk, a.dv = dv, a.delta = (float*)workspace;
-  a.part = (float*)((char*)workspace + up256((size_t)d->B * d->Tq * d->Hq * 4 + 16));
+  a.part = (float*)((char*)workspace + up256((size_t)d->B * d->Tq * d->Hq * 12 + 16));
   const KeyPlan plan = key_plan(d);
   const hipStream_t st = as_stream(stream);
   return attend_dispatch(d, [&](auto t, auto dp) {

@@ -35,10 +35,19 @@ __device__ __forceinline__ void fwd_row(const AttendArgs& a, int b, int t, int h
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* y = (T*)a.out + (int64_t)b * a.sy.b + (int64_t)t * a.sy.t + (int64_t)h * a.sy.h;
   store_cols<T, DP>(y, lq, a.D, [&](int dt) { return l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * inv; });
-  if (a.stats && lq == 0) {
-    float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + t) * 2;
-    s[0] = l == 0.f ? INFINITY : m;
-    s[1] = inv;
+  if (!a.stats) return;
+  float* s = stats_row(a, a.stats, b, h, t);
+  if (lq == 0) s[0] = l == 0.f ? INFINITY : m, s[1] = inv;
+  if constexpr (sizeof(T) == 2) {
+    if (a.width == 2) return;
+#pragma unroll
+    for (int dt = 0; dt < DP / 16; ++dt) {
+      if (16 * dt + 4 * lq >= a.D) continue;
+      uint32_t w = 0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) w |= (l == 0.f ? 0u : lost_byte(o[dt][r] * inv)) << (8 * r);
+      ((uint32_t*)s)[2 + 4 * dt + lq] = w;
+    }
   }
 }
 
@@ -322,10 +331,14 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int cs, int g
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if (n + k < a.D) from_f32(y[n + k], l == 0.f ? 0.f : v[k] * inv);
-  if (a.stats && n == 0) {
-    float* s = a.stats + (((int64_t)b * a.Hq + h) * a.Tq + place) * 2;
-    s[0] = l == 0.f ? INFINITY : m;
-    s[1] = inv;
+  if (!a.stats) return;
+  float* s = stats_row(a, a.stats, b, h, place);
+  if (n == 0) s[0] = l == 0.f ? INFINITY : m, s[1] = inv;
+  if (sizeof(T) == 2 && a.width > 2) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w |= (l == 0.f || n + k >= a.D ? 0u : lost_byte(v[k] * inv)) << (8 * k);
+    ((uint32_t*)s)[2 + n / 4] = w;
   }
 }
 
@@ -365,6 +378,8 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 }  // namespace
+
+extern "C" int32_t stacklstm_attend_stats_width(const slstm_attend_dims* d) { return attend_ok(d) ? attend_stats_width(d) : 0; }
 
 extern "C" size_t stacklstm_attend_fwd_workspace_bytes(const slstm_attend_dims* d) {
   if (!attend_ok(d)) return 0;

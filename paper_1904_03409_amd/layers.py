@@ -19,7 +19,7 @@ from . import stacklstm as _sl
 from .head import DTYPES, SLSTM_BF16, SLSTM_F32, _arr, _ld, _mat, _type, _ws
 from .stacklstm import StackLSTMError, _check, _stream
 
-EXPORTS = ("stacklstm_attend_fwd_workspace_bytes", "stacklstm_attend_bwd_workspace_bytes", "stacklstm_attend_fwd",
+EXPORTS = ("stacklstm_attend_stats_width", "stacklstm_attend_fwd_workspace_bytes", "stacklstm_attend_bwd_workspace_bytes", "stacklstm_attend_fwd",
            "stacklstm_attend_bwd", "stacklstm_logprob_workspace_bytes", "stacklstm_logprob_fwd", "stacklstm_logprob_bwd",
            "stacklstm_logprob_step", "stacklstm_dropout_fwd", "stacklstm_dropout_bwd")
 
@@ -57,8 +57,8 @@ def load_library():
         dims = {"attend": slstm_attend_dims, "logprob": slstm_logprob_dims, "dropout": slstm_dropout_dims}
         for name in EXPORTS:
             fn, d = getattr(lib, name), ctypes.POINTER(dims[name.split("_")[1]])
-            if name.endswith("_workspace_bytes"):
-                fn.restype, fn.argtypes = SZ, [d]
+            if name.endswith(("_workspace_bytes", "_width")):
+                fn.restype, fn.argtypes = SZ if name.endswith("_bytes") else ctypes.c_int32, [d]
                 continue
             fn.restype = I32
             fn.argtypes = [d] + {
@@ -118,6 +118,10 @@ def make_attend_dims(B, Tq, Tk, Hq, Hk, D, type=SLSTM_F32, scale=None, **strides
     return slstm_attend_dims(B, Tq, Tk, Hq, Hk, D, type, D ** -0.5 if scale is None and D > 0 else scale or 0.0, **strides)
 
 
+def stacklstm_attend_stats_width(dims) -> int:
+    return int(load_library().stacklstm_attend_stats_width(ctypes.byref(dims)))
+
+
 def stacklstm_attend_fwd_workspace_bytes(dims) -> int:
     return int(load_library().stacklstm_attend_fwd_workspace_bytes(ctypes.byref(dims)))
 
@@ -154,13 +158,17 @@ def _lens(d, q_len, k_len, mask):
             None if mask is None else _arr(mask, torch.uint8, "mask", (d.B, d.Tk)))
 
 
+def _stats(d, stats):
+    return _arr(stats, torch.float32, "stats", (d.B, d.Hq, d.Tq, stacklstm_attend_stats_width(d)))
+
+
 def stacklstm_attend_fwd(dims, q, k, v, q_len, k_len, mask, y, stats, workspace, stream=None, check=True) -> int:
     d, t = dims, DTYPES[dims.type]
     sq, sk = (d.B, d.Tq, d.Hq, d.D), (d.B, d.Tk, d.Hk, d.D)
     ws, n = _space(workspace)
     return _call("stacklstm_attend_fwd", q, stream, check, d, _heads(q, t, "q", sq, d.q), _heads(k, t, "k", sk, d.k),
                  _heads(v, t, "v", sk, d.v), *_lens(d, q_len, k_len, mask), _heads(y, t, "y", sq, d.y),
-                 _arr(stats, torch.float32, "stats", (d.B, d.Hq, d.Tq, 2), True), ws, n)
+                 None if stats is None else _stats(d, stats), ws, n)
 
 
 def stacklstm_attend_bwd(dims, q, k, v, q_len, k_len, mask, y, stats, dy, dq, dk, dv, workspace, stream=None, check=True) -> int:
@@ -169,7 +177,7 @@ def stacklstm_attend_bwd(dims, q, k, v, q_len, k_len, mask, y, stats, dy, dq, dk
     ws, n = _space(workspace)
     return _call("stacklstm_attend_bwd", q, stream, check, d, _heads(q, t, "q", sq, d.q), _heads(k, t, "k", sk, d.k),
                  _heads(v, t, "v", sk, d.v), *_lens(d, q_len, k_len, mask), _heads(y, t, "y", sq, d.y),
-                 _arr(stats, torch.float32, "stats", (d.B, d.Hq, d.Tq, 2)), _heads(dy, t, "dy", sq, d.dy),
+                 _stats(d, stats), _heads(dy, t, "dy", sq, d.dy),
                  _heads(dq, t, "dq", sq, d.dq), _heads(dk, t, "dk", sk, d.dk), _heads(dv, t, "dv", sk, d.dv), ws, n)
 
 
@@ -213,7 +221,7 @@ class AttendRun:
         if train:
             n = max(n, _bytes("stacklstm_attend_bwd_workspace_bytes", d))
         e = lambda *s, dtype: torch.empty(*s, dtype=dtype, device=q.device)
-        return cls(d, q, k, v, q_len, k_len, mask, dy, y, e(B, Hq, Tq, 2, dtype=torch.float32) if train else None, *grads,
+        return cls(d, q, k, v, q_len, k_len, mask, dy, y, e(B, Hq, Tq, stacklstm_attend_stats_width(d), dtype=torch.float32) if train else None, *grads,
                    e(n, dtype=torch.uint8))
 
     def forward(self, stream=None):

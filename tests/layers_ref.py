@@ -22,8 +22,9 @@ def attend(q, k, v, ok, scale, dy=None, dtype="f32", bounds=False):
 
     Bounds: a dot product of D terms in 32 bits is off by 6 sqrt(D) 2^-24 of the sum of its terms' sizes (six standard deviations
     of as many independent roundings), a p by that of its x and by 16 2^-24 (its exponential, the sum and the division), a
-    sum over n rows by 6 sqrt(n) 2^-24 of its terms' sizes. bf16 outputs, weights of a product, and the y that a backward reads
-    are rounded once more, by at most 2^-8 of themselves."""
+    sum over n rows by 6 sqrt(n) 2^-24 of its terms' sizes. bf16 outputs and weights of a product are rounded once more, by at
+    most 2^-8 of themselves. A backward's dy . y is that of the forward's y before its rounding, to 2^-8 / 254 of its terms; with up
+    to 16 keys it is the sum of p (dy . v), whose p are not rounded."""
     B, Tq, Hq, D = q.shape
     Tk, Hk = k.shape[1:3]
     G, u, w = Hq // Hk, 2.0 ** -24, HALF[dtype]
@@ -66,7 +67,11 @@ def attend(q, k, v, ok, scale, dy=None, dtype="f32", bounds=False):
             if bounds:
                 ddp = s32(D) * (np.abs(g) @ np.abs(V).T)
                 yd = (np.abs(g) * np.abs(y)).sum(1, keepdims=True)
-                ddelta = (s32(D) + (w if w_in else 0)) * yd + (np.abs(g) * off["y"][b, rows, h]).sum(1, keepdims=True)
+                if Tk <= 16:
+                    ddelta = (p * ((ep + s32(Tk)) * np.abs(dp) + ddp)).sum(1, keepdims=True)
+                else:
+                    y_off = off["y"][b, rows, h] - w * np.abs(y)
+                    ddelta = (s32(D) + (w / 254 if w_in else 0)) * yd + (np.abs(g) * y_off).sum(1, keepdims=True)
                 eds = np.abs(ds) * (ep + w_in + 2 * u) + p * (ddp + ddelta)
                 off["dq"][b, rows, h] = abs(scale) * ((eds + s32(len(keys)) * np.abs(ds)) @ np.abs(K))
                 off["dk"][b, keys, c] += abs(scale) * ((eds + s32(G * len(rows)) * np.abs(ds)).T @ np.abs(Q))

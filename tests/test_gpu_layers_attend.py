@@ -95,6 +95,49 @@ def test_forward_and_backward(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(3, 40, 2, 2, 2, 200), (2, 150, 4, 4, 2, 128), (2, 30, 16, 2, 1, 256), (2, 70, 3, 1, 1, 64), (3, 21, 11, 3, 1, 72)])
+def test_few_keys(size, dtype):
+    """p (dp - delta) is small beside its terms: delta has to be as exact as they are."""
+    ly = _ly()
+    rng = rng_for("few", *size, dtype)
+    check(ly, *inputs(rng, *size, dtype), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [16, 64, 100, 128, 256])
+def test_one_key(D, dtype):
+    """Of one key (alone, or the only one that is there) y is its value, and moves with neither queries nor keys."""
+    ly = _ly()
+    rng = rng_for("one key", D, dtype)
+    for Tk in (1, 12):
+        s, _, _, _ = inputs(rng, 3, 33, Tk, 4, 2, D, dtype)
+        m = np.zeros((3, Tk), np.uint8)
+        m[:, Tk // 2] = 1
+        r = check(ly, s, None, None, m, dtype)
+        assert not r.dq.any() and not r.dk.any()
+        assert np.array_equal(get(r.y), np.repeat(s["v"][:, Tk // 2:Tk // 2 + 1], 33, 1).repeat(2, 2))
+
+
+def test_one_key_outweighs_the_others():
+    """Many keys, of which one has nearly all of the weight: what its gradient is made of is far smaller than its terms."""
+    ly = _ly()
+    rng = rng_for("peak")
+    s, _, _, _ = inputs(rng, 2, 40, 300, 2, 2, 128, "bf16")
+    at = rng.integers(0, 300, (2, 40))
+    for b in range(2):
+        for t in range(40):
+            s["q"][b, t] = rounded(s["k"][b, at[b, t]] * 0.55, "bf16")   # a score 6 above the others' spread
+    ok = ref.seen(2, 40, 300)
+    want = ref.attend(s["q"], s["k"], s["v"], ok, 128 ** -0.5, s["dy"])
+    r = ly.AttendRun.of(*(heads(s[n], "bf16") for n in "qkv"), dy=heads(s["dy"], "bf16"))
+    r.forward(), r.backward()
+    for n in ("dq", "dk"):
+        g, w = get(getattr(r, n)), want[n]
+        # roundings of p, s and the output (each 2^-9 of the value in the mean square at most, sqrt(3) together) and as much again
+        assert np.linalg.norm(g - w) <= 2 * 3 ** 0.5 * 2.0 ** -9 * np.linalg.norm(w), (n, np.linalg.norm(g - w) / np.linalg.norm(w))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("size", [(6, 9, 40, 2, 2, 24), (5, 70, 150, 4, 2, 64), (4, 140, 90, 2, 1, 120), (4, 1, 700, 4, 2, 40), (5, 33, 20, 2, 2, 256)])
 def test_lengths_and_masks(size, dtype):
     """Ragged queries and keys, masked keys, sequences without any key; what is not there holds NaN and infinities."""

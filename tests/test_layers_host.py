@@ -19,7 +19,7 @@ def _text():
 
 def test_library_exports_every_declared_function():
     names = sorted(set(re.findall(r"\b(stacklstm_\w+)\s*\(", _text())))
-    assert set(names) == set(ly.EXPORTS) and len(names) == 10
+    assert set(names) == set(ly.EXPORTS) and len(names) == 11
     lib = ly.load_library()
     assert not [n for n in names if not hasattr(lib, n)]
 
@@ -44,6 +44,10 @@ def test_work_spaces():
     n = ly.stacklstm_attend_fwd_workspace_bytes(mk(1, 1, 1 << 20, 8, 8, 64))
     assert 64 < n <= (1 << 20) // 128 * 8 * (64 + 2) * 4 + 256
     assert ly.stacklstm_attend_bwd_workspace_bytes(mk(3, 5, 7, 4, 2, 16)) >= 3 * 5 * 4 * 4
+    # a byte to an element of a 16-bit y beside a row's two statistics, but where the backward needs no y
+    width = ly.stacklstm_attend_stats_width
+    assert [width(mk(3, 5, 700, 4, 2, 50, t)) for t in (0, 1)] == [2, 2 + 13] and width(mk(3, 5, 128, 4, 2, 64, 1)) == 2
+    assert width(mk(3, 5, 128, 4, 2, 65, 1)) == 2 + 17 and width(mk(-1, 5, 128, 4, 2, 65, 1)) == 0
     # rows that fit registers need none
     assert ly.stacklstm_logprob_workspace_bytes(ly.make_logprob_dims(4096, 32000, 1, 64, 1)) <= 64
     assert ly.stacklstm_logprob_workspace_bytes(ly.make_logprob_dims(4, 131071, 3, 10)) >= 4 * 32 * (12 + 80)
