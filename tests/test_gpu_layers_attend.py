@@ -180,6 +180,9 @@ def test_outputs_in_a_wider_buffer():
     s["k"][:], s["v"][:] = s["k"][:1], s["v"][:1]
     q = heads(s["q"], "f32")
     k, v = (heads(s[n][:1], "f32").expand(4, -1, -1, -1) for n in ("k", "v"))
+    # (one key for all places, too: a stride of 0 along them)
+    one = heads(s["v"][:1, :1], "f32").expand(4, 45, -1, -1)
+    assert torch.equal(ly.AttendRun.of(q, one, one).forward(), ly.AttendRun.of(q, one.contiguous(), one.contiguous()).forward())
     big = torch.full((4, 30, 2, 47), 5.0, device="cuda")
     r = ly.AttendRun.of(q, k, v, y=big[..., 3:43])
     r.forward()

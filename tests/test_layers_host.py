@@ -65,7 +65,9 @@ def test_refusals_launch_nothing():
            mk(2, 3, 4, 2, 2, 8, q=S(-1, 8, 8)), mk(2, 3, 4, 2, 2, 8, k=S(1 << 41, 8, 8)),
            # outputs with two elements at one place: broadcast, overlapping heads, overlapping sequences
            mk(2, 3, 4, 2, 2, 8, y=S(0, 16, 8)), mk(2, 3, 4, 2, 2, 8, dq=S(48, 16, 7)), mk(2, 3, 4, 2, 2, 8, dk=S(63, 16, 8)),
-           mk(2, 3, 4, 2, 2, 8, dv=S(8, 8, 32)), None]
+           mk(2, 3, 4, 2, 2, 8, dv=S(8, 8, 32)),
+           # ... and one whose end no 64-bit offset reaches
+           mk(1 << 30, 1, 1, 1, 1, 8, y=S(1 << 39, 8, 8)), None]
     one = P(1 << 20)
     for d in bad:
         assert lib.stacklstm_attend_fwd_workspace_bytes(d) == 0 and lib.stacklstm_attend_bwd_workspace_bytes(d) == 0
