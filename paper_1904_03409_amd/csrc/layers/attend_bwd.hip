@@ -61,7 +61,8 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
   const Place pl = place_of(a);
   const int b = uni(pl.bh / a.Hk), hk = uni(pl.bh % a.Hk), rows = a.Tq * a.G;
   const int qlen = clamp_len(a.q_len, b, a.Tq), klen = clamp_len(a.k_len, b, a.Tk);
-  const int kend = pl.tile * F::OWN / a.G < qlen ? klen : 0;
+  const int kbeg = a.splits > 1 ? pl.split * a.chunk : 0;
+  const int kend = pl.tile * F::OWN / a.G < qlen ? (a.splits > 1 ? min(klen, kbeg + a.chunk) : klen) : kbeg;
   int qt_[QT], qh_[QT];
   bool here[QT], used[QT];
   u32x4 qr[QT][H::STEPS], gr[QT][H::STEPS], yr[QT][H::STEPS];
@@ -110,7 +111,7 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
   for (int j = 0; j < QT; ++j)
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) o[j][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (kend > 0) go(0, 0);
+  if (kbeg < kend) go(kbeg, 0);
   frag q[QT][H::STEPS], g[QT][H::STEPS];
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
@@ -139,9 +140,9 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
         to[0] = m[j], to[1] = inv[j], to[2] = delta[j];
       }
   };
-  const bool one = kend <= F::R;                       // all keys in one tile
-  if (!one || kend <= 0) put_delta();
-  for (int k0 = 0, n = 0; k0 < kend; k0 += F::R, ++n) {
+  const bool one = a.splits == 1 && kend <= F::R;      // all keys in one tile
+  if (pl.split == 0 && (!one || kend <= 0)) put_delta();
+  for (int k0 = kbeg, n = 0; k0 < kend; k0 += F::R, ++n) {
     const unsigned char *kt = stage(n), *vt = kt + F::TILE;
     const unsigned long long there = __ballot(lane < F::R && k0 + lane < kend && (!mask || mask[k0 + lane]));
     if constexpr (DMA) wait_vm<0>();
@@ -207,8 +208,13 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
     if (!here[j]) continue;
-    T* dq = (T*)a.dq + (int64_t)b * a.sdq.b + (int64_t)qt_[j] * a.sdq.t + (int64_t)qh_[j] * a.sdq.h;
-    store_cols<T, DP>(dq, lq, a.D, [&](int dt) { return used[j] ? o[j][dt] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f}; });
+    auto v = [&](int dt) { return used[j] ? o[j][dt] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f}; };
+    if (a.splits > 1) {
+      const int64_t row = (((int64_t)pl.split * a.B + b) * a.Hq + qh_[j]) * a.Tq + qt_[j];
+      store_cols<float, DP>(a.part + row * a.D, lq, a.D, v);
+    } else {
+      store_cols<T, DP>((T*)a.dq + (int64_t)b * a.sdq.b + (int64_t)qt_[j] * a.sdq.t + (int64_t)qh_[j] * a.sdq.h, lq, a.D, v);
+    }
   }
 }
 
@@ -531,23 +537,25 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 && sizeof(T) == 2 && DMA ? 4 
   }
 }
 
-// dk and dv from their splits: four elements of a head to a thread, blockIdx.y: dk, dv.
+// Gradients from their splits: four elements of a head to a thread. part: [splits][arrays][B, H, T, D], blockIdx.y the array.
 template <typename T>
-__global__ void __launch_bounds__(256) k_attend_join_dkv(AttendArgs a) {
-  const int per = (a.D + 3) / 4;
-  const int64_t id = (a.first + blockIdx.x) * 256 + threadIdx.x, row = id / per, rows = (int64_t)a.B * a.Hk * a.Tk;
+__global__ void __launch_bounds__(256) k_attend_sum(const float* part, int splits, int64_t first, int B, int H, int len, int D,
+                                                    T* to0, slstm_strides s0, T* to1, slstm_strides s1) {
+  const int per = (D + 3) / 4;
+  const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x, row = id / per, rows = (int64_t)B * H * len;
   if (row >= rows) return;
-  const int n = (int)(id % per) * 4, bh = (int)(row / a.Tk), t = (int)(row % a.Tk), left = a.D - n;
-  const float* p = a.part + ((int64_t)blockIdx.y * rows + row) * a.D;
+  const int n = (int)(id - row * per) * 4, bh = (int)(row / len), t = (int)(row - (int64_t)bh * len), left = D - n;
+  const float* p = part + ((int64_t)blockIdx.y * rows + row) * D;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < a.splits; ++i, p += 2 * rows * a.D) {
+#pragma unroll 8
+  for (int i = 0; i < splits; ++i) {
     float v[4];
-    vec<float>::unpack(load_vec(p, n / 4, a.D), v);
+    vec<float>::unpack(load_vec(p + (int64_t)i * gridDim.y * rows * D, n / 4, D), v);
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] += v[k];
   }
-  const slstm_strides st = blockIdx.y ? a.sdv : a.sdk;
-  T* to = (T*)(blockIdx.y ? a.dv : a.dk) + (int64_t)(bh / a.Hk) * st.b + (int64_t)t * st.t + (int64_t)(bh % a.Hk) * st.h;
+  const slstm_strides st = blockIdx.y ? s1 : s0;
+  T* to = (blockIdx.y ? to1 : to0) + (int64_t)(bh / H) * st.b + (int64_t)t * st.t + (int64_t)(bh % H) * st.h;
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if (k < left) from_f32(to[n + k], s[k]);
@@ -556,12 +564,13 @@ __global__ void __launch_bounds__(256) k_attend_join_dkv(AttendArgs a) {
 namespace {
 
 // Keys of a workgroup of k_attend_dkv, and splits of its queries. 256 keys with eight waves (Keys) where they are there;
-// queries are split, 256 of them at least to each part, until there are two workgroups to a compute unit, where there is not one to each
+// queries are split, 64 of them at least to each part, until there are two workgroups to a compute unit, where there is not one to each
 // (2 sequences of 4096 x 4000, 4 key heads of 128, of unequal lengths: eight waves and four parts 541 + 23 us; four waves with
 // everything in registers and no parts 872, eight with 16 keys each 742).
 struct KeyPlan {
   bool one, big;                                       // one: k_attend_short
   int tiles, splits;
+  int qsplits, qchunk;                                 // k_attend_dq: splits of the keys
 };
 KeyPlan key_plan(const slstm_attend_dims* d) {
   KeyPlan p;
@@ -569,8 +578,15 @@ KeyPlan key_plan(const slstm_attend_dims* d) {
   p.big = d->type == SLSTM_BF16 && d->D > 64 && d->D <= 128 && d->Tk > 128;
   const int keys = p.one ? 128 : p.big ? 256 : d->D > 128 || (d->D > 64 && d->type == SLSTM_F32) ? 64 : 128;
   p.tiles = (d->Tk + keys - 1) / keys;
-  const int64_t groups = std::max<int64_t>(1, (int64_t)p.tiles * d->B * d->Hk), most = (int64_t)d->Tq * (d->Hq / d->Hk) / 256;
-  p.splits = (int)std::max<int64_t>(1, groups < 256 ? std::min<int64_t>(std::min<int64_t>(512 / groups, most), 64) : 1);
+  const int64_t groups = std::max<int64_t>(1, (int64_t)p.tiles * d->B * d->Hk), most = (int64_t)d->Tq * (d->Hq / d->Hk) / 64;
+  p.splits = (int)std::max<int64_t>(1, groups < 256 ? std::min<int64_t>(std::min<int64_t>(512 / groups, most), 32) : 1);
+  // few row tiles, many keys: splits of 128 keys at least, likewise (1 x 9 queries of 4 heads over 16000 keys)
+  const int own = d->D <= 128 ? 128 : 64;
+  const int64_t rows = (int64_t)d->Tq * (d->Hq / d->Hk), qgroups = std::max<int64_t>(1, (rows + own - 1) / own * d->B * d->Hk);
+  int64_t parts = qgroups < 256 && !p.one ? std::min<int64_t>(std::min<int64_t>(512 / qgroups, d->Tk / 128), 64) : 1;
+  if (parts < 1) parts = 1;
+  p.qchunk = (int)(((d->Tk + parts - 1) / parts + 63) / 64 * 64);
+  p.qsplits = parts > 1 ? (d->Tk + p.qchunk - 1) / p.qchunk : 1;
   return p;
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -581,7 +597,10 @@ extern "C" size_t stacklstm_attend_bwd_workspace_bytes(const slstm_attend_dims* 
   if (!attend_ok(d)) return 0;
   const KeyPlan p = key_plan(d);
   const size_t delta = up256((size_t)d->B * d->Tq * d->Hq * 12 + 16);
-  return p.splits > 1 ? delta + (size_t)p.splits * 2 * d->B * d->Hk * d->Tk * d->D * 4 : delta;
+  // (dq's parts have been summed before dk's and dv's are written)
+  const size_t dkv = p.splits > 1 ? (size_t)p.splits * 2 * d->B * d->Hk * d->Tk * d->D * 4 : 0;
+  const size_t dq = p.qsplits > 1 ? (size_t)p.qsplits * d->B * d->Hq * d->Tq * d->D * 4 : 0;
+  return delta + std::max(dkv, dq);
 }
 
 extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, const void* k, const void* v, const int32_t* q_len,
@@ -628,15 +647,25 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
         e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? keys(std::true_type()) : keys(std::false_type());
       }
     }
+    // gradients from their splits
+    auto sum = [&](int arrays, int H, int len, T* to0, const slstm_strides& s0, T* to1, const slstm_strides& s1) {
+      const int64_t blocks = ((int64_t)d->B * H * len * ((d->D + 3) / 4) + 255) / 256;
+      in_pieces(blocks, kMostGroups, [&](int64_t b0, int64_t n) {
+        hipLaunchKernelGGL(k_attend_sum<T>, dim3((unsigned)n, arrays), dim3(256), 0, st, a.part, a.splits, b0, d->B, H, len, d->D, to0, s0,
+                           to1, s1);
+      });
+      return hipGetLastError();
+    };
     if (!plan.one && d->Tq) {
-      a.splits = 1;
+      a.splits = plan.qsplits, a.chunk = plan.qchunk;
       auto run = [&](auto dma) {
         typedef Bwd<T, DP, decltype(dma)::value> F;
         static std::atomic<uint64_t> dev;
         a.tiles = (int)(((int64_t)d->Tq * a.G + F::OWN - 1) / F::OWN);
-        return attend_launch(k_attend_dq<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk, F::LDS, dev, st);
+        return attend_launch(k_attend_dq<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk * a.splits, F::LDS, dev, st);
       };
       e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
+      if (e == hipSuccess && a.splits > 1) e = sum(1, d->Hq, d->Tq, (T*)dq, a.sdq, (T*)dq, a.sdq);
     }
     if (e == hipSuccess && !plan.one && d->Tk) {
       a.splits = plan.splits;
@@ -659,14 +688,7 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
       };
       e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? run(std::true_type()) : run(std::false_type());
     }
-    if (e == hipSuccess && d->Tk && a.splits > 1) {
-      const int64_t blocks = ((int64_t)d->B * d->Hk * d->Tk * ((d->D + 3) / 4) + 255) / 256;
-      in_pieces(blocks, kMostGroups, [&](int64_t b0, int64_t n) {
-        a.first = b0;
-        hipLaunchKernelGGL(k_attend_join_dkv<T>, dim3((unsigned)n, 2), dim3(256), 0, st, a);
-      });
-      e = hipGetLastError();
-    }
+    if (e == hipSuccess && d->Tk && plan.splits > 1) e = sum(2, d->Hk, d->Tk, (T*)dk, a.sdk, (T*)dv, a.sdv);
     return e == hipSuccess ? SLSTM_OK : SLSTM_EDEVICE;
   });
 }

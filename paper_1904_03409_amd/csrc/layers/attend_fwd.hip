@@ -365,9 +365,9 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
   if (getenv("ATT_QT") && p.wk == 1) p.qt = atoi(getenv("ATT_QT"));
   p.rows = 16 * p.qt * (4 / p.wk);
   p.tiles = (int)((R + p.rows - 1) / p.rows);
-  // splits of 256 keys at least, until there are two workgroups to a compute unit
+  // splits of 128 keys at least, until there are two workgroups to a compute unit, where there is not one to each
   const int64_t groups = (int64_t)p.tiles * d->B * d->Hk;
-  const int64_t want = groups > 0 && groups < 256 ? 512 / groups : 1, most = ((int64_t)d->Tk + 255) / 256;
+  const int64_t want = groups > 0 && groups < 256 ? 512 / groups : 1, most = ((int64_t)d->Tk + 127) / 128;
   p.splits = (int)std::max<int64_t>(1, std::min(want, most));
   p.chunk = (((d->Tk + p.splits - 1) / p.splits) + 127) / 128 * 128;
   if (p.chunk < 128) p.chunk = 128;

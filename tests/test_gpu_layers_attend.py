@@ -337,3 +337,17 @@ def test_refusals():
         ly.AttendRun.of(q.transpose(2, 3), k, k)
     with pytest.raises(Exception):
         ly.AttendRun.of(torch.randn(2, 3, 3, 8, device="cuda"), k, k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 7, 3000, 2, 1, 48), (2, 65, 1100, 2, 2, 128), (1, 300, 700, 1, 1, 100), (1, 1500, 300, 2, 1, 200)])
+def test_gradients_are_split(size, dtype):
+    """Few row or key tiles: dq's keys, dk's and dv's queries over several workgroups; ragged, strided, with equal bits each time."""
+    ly = _ly()
+    rng = rng_for("gsplit", *size, dtype)
+    s, q_len, k_len, m = inputs(rng, *size, dtype, lens=size[0] > 1, mask=True)
+    r = check(ly, s, q_len, k_len, m, dtype, steps_first=True)
+    got = [t.clone() for t in (r.dq, r.dk, r.dv)]
+    r.workspace.fill_(255)
+    r.backward()
+    assert all(torch.equal(a, b) for a, b in zip(got, (r.dq, r.dk, r.dv)))
