@@ -109,17 +109,28 @@ __device__ __forceinline__ void scores(f32x4 (&acc)[N], const unsigned char* til
                                        const frag_t<T> (&own)[N][Head<T, DP>::STEPS]) {
   typedef Head<T, DP> H;
   const int row = row_of<T>(sub, l16), f = swz<T, H::GPR>(row);
+  auto step = [&](int s) { return *(const typename H::frag*)(tile + (base + row) * H::BYTES + ((4 * s + lq) ^ f) * 16); };
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-  for (int s = 0; s < H::STEPS; ++s) {
-    const typename H::frag a = *(const typename H::frag*)(tile + (base + row) * H::BYTES + ((4 * s + lq) ^ f) * 16);
+    for (int s = 0; s < H::STEPS; ++s) {
+      const typename H::frag a = step(s);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if constexpr (sizeof(T) == 2) {
-        acc[j] = mfma_bf16_16x16x32(a, own[j][s], acc[j]);
-      } else {
+      for (int j = 0; j < N; ++j) acc[j] = mfma_bf16_16x16x32(a, own[j][s], acc[j]);
+    }
+  } else {
+    // (the next step's 16 bytes on their way during this one's products, as in sums below)
+    typename H::frag a = step(0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], own[j][s][e], acc[j], 0, 0, 0);
-      }
+    for (int s = 0; s < H::STEPS; ++s) {
+      typename H::frag next = a;
+      if (s + 1 < H::STEPS) next = step(s + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], own[j][s][e], acc[j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      a = next;
     }
   }
 }
@@ -165,7 +176,14 @@ __device__ __forceinline__ frag_t<T> column(const unsigned char* tile, int base,
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int row = 4 * lq + e;
-      v[e] = *(const float*)(tile + (base + row) * GPR * 16 + ((4 * dt + (l16 >> 2)) ^ swz<T, GPR>(base + row)) * 16 + (l16 & 3) * 4);
+      if constexpr (GPR >= 16) {
+        // (4 dt + l16 / 4) ^ (4 lq + e) taken apart, so that eight numbers and constants make all of a unit's addresses
+        static_assert(GPR % 16 == 0, "whole fours of columns");
+        const unsigned char* q = tile + row * GPR * 16 + ((l16 >> 2) ^ e) * 16 + (l16 & 3) * 4;
+        v[e] = *(const float*)(q + ((dt & 3) ^ lq) * 64 + (base * GPR * 16 + (dt >> 2) * 256));
+      } else {
+        v[e] = *(const float*)(tile + (base + row) * GPR * 16 + ((4 * dt + (l16 >> 2)) ^ swz<T, GPR>(base + row)) * 16 + (l16 & 3) * 4);
+      }
     }
     return v;
   }
@@ -184,17 +202,28 @@ __device__ __forceinline__ f32x4 product(const frag_t<T>& a, const frag_t<T>& b,
 template <typename T, int DP, int N>
 __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq, const frag_t<T> (&w)[N]) {
   typedef Head<T, DP> H;
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-  for (int dt = 0; dt < H::DT; ++dt) {
-    const frag_t<T> a = column<T, H::GPR>(tile, base, dt, l16, lq);
-    if constexpr (sizeof(T) == 2) {
+    for (int dt = 0; dt < H::DT; ++dt) {
+      const frag_t<T> a = column<T, H::GPR>(tile, base, dt, l16, lq);
 #pragma unroll
       for (int j = 0; j < N; ++j) acc[j][dt] = mfma_bf16_16x16x32(a, w[j], acc[j][dt]);
-    } else {
+    }
+  } else {
+    // (the next columns are on their way during these ones' products: left to itself the compiler read one number, waited, read the
+    // next. 2 x 2048 x 2000, 8 heads of 256, forward, dq, dk and dv: 804, 1076, 1260 us; 673, 856, 1056 this way, here and in scores)
+    frag_t<T> a = column<T, H::GPR>(tile, base, 0, l16, lq);
+#pragma unroll
+    for (int dt = 0; dt < H::DT; ++dt) {
+      frag_t<T> next = a;
+      if (dt + 1 < H::DT) next = column<T, H::GPR>(tile, base, dt + 1, l16, lq);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], w[j][e], acc[j][dt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      a = next;
     }
   }
 }

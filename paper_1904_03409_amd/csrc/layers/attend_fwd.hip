@@ -27,7 +27,7 @@ struct Fwd {
   static constexpr int KW = KT / WK, NU = KW / H::UNIT;                  // keys and units of a wave
   static constexpr int TILE = KT * H::BYTES;
   // waves on a SIMD that the registers are to leave room for: two hide each other's waits and run products beside exponentials
-  static constexpr int WAVES = H::BYTES <= 128 || (DMA && H::BYTES <= 256) ? 2 : 1;
+  static constexpr int WAVES = H::BYTES <= 128 || (DMA && (H::BYTES <= 256 || WK == 1)) ? 2 : 1;
   static constexpr int JOIN = WK == 4 ? 4 * 16 * (DP + 4) * 4 + 4 * 2 * 16 * 4 : 0;
   static constexpr int STAGES = 4 * TILE <= 160 * 1024 ? 2 : 1;
   static constexpr int LDS = 2 * STAGES * TILE > JOIN ? 2 * STAGES * TILE : JOIN;
