@@ -6,12 +6,11 @@
 // queries, a quarter of the tile (WK = 4), whose parts are joined through LDS. Where the row tiles do not fill the chip the
 // keys are split over workgroups and k_attend_join joins their sums.
 // Bound by the matrix and vector units together where queries are many (2 sequences of 4096 x 4000, 16 heads of 128 over 4, bf16: 275 us,
-// 760 TFLOP/s, matrix units 30% and vector units 40% busy; fp32 4 x 1024 x 1000, 8 heads of 64: 93 us, 90 TFLOP/s), by the keys' bytes
+// 760 TFLOP/s, matrix units 30% and vector units 40% busy; fp32 4 x 1024 x 1000, 8 heads of 64: 86 us, 97 TFLOP/s), by the keys' bytes
 // where they are few (8 beams of 8 sequences over up to 16384 keys, 16 heads of 128 over 4: 38 us, 5.5 TB/s, and 4.6 for the join), by a
 // workgroup's start and waits where both are (256 x 240 x 120, 8 heads of 64, bf16: 51 us, 3.1 TB/s).
 // With register staging, padded rows and one wave to a SIMD the first of these took 610 us.
 #include <algorithm>
-#include <stdlib.h>
 
 #include "attend.h"
 
@@ -362,7 +361,6 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
   if (R <= 16) p.qt = 1, p.wk = 4;
   else if (R <= 64 || wide || d->type == SLSTM_F32) p.qt = 1, p.wk = 1;
   else p.qt = 2, p.wk = 1;
-  if (getenv("ATT_QT") && p.wk == 1) p.qt = atoi(getenv("ATT_QT"));
   p.rows = 16 * p.qt * (4 / p.wk);
   p.tiles = (int)((R + p.rows - 1) / p.rows);
   // splits of 128 keys at least, until there are two workgroups to a compute unit, where there is not one to each
