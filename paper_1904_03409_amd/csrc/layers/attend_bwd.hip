@@ -5,10 +5,10 @@
 // in whatever order they come; these give the same bits every time. Up to 128 keys (of heads up to 64) are a workgroup's at once:
 // k_attend_short does the five products, and reads q and dy once.
 // Bound by the matrix and vector units together where keys are many (2 sequences of 4096 queries and 4000 keys, 16 heads of 128 over 4,
-// bf16: dq 382 us, 825 TFLOP/s of its three products; dk and dv 531, 790 of its four, and 23 for joining their splits); fp32 4 x 1024 x
-// 1000, 8 heads of 64: 136 and 168 us, 93 and 100 TFLOP/s of the 154 of a large product. Of few keys by a workgroup's start and the
-// waits between its phases: 256 x 240 x 120, 8 heads of 64, bf16 111 us (2.8 TB/s; two kernels took 76 + 64), 64 x 119 x 60, 4 heads of
-// 50, fp32 31 us (20 + 31).
+// bf16: dq 360 to 380 us, 850 TFLOP/s of its three products; dk and dv 510 to 530, 800 of its four, and 23 for joining their splits); fp32
+// 4 x 1024 x 1000, 8 heads of 64: 129 and 155 us, 98 and 108 TFLOP/s of the 154 of a large product. Of few keys by a workgroup's
+// start and the waits between its phases: 256 x 240 x 120, 8 heads of 64, bf16 111 us (2.8 TB/s; two kernels took 76 + 64), 64 x 119 x
+// 60, 4 heads of 50, fp32 29 us (20 + 31).
 #include <algorithm>
 
 #include "attend.h"
