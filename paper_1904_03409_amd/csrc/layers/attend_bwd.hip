@@ -583,7 +583,10 @@ KeyPlan key_plan(const slstm_attend_dims* d) {
   // few row tiles, many keys: splits of 128 keys at least, likewise (1 x 9 queries of 4 heads over 16000 keys)
   const int own = d->D <= 128 ? 128 : 64;
   const int64_t rows = (int64_t)d->Tq * (d->Hq / d->Hk), qgroups = std::max<int64_t>(1, (rows + own - 1) / own * d->B * d->Hk);
-  int64_t parts = qgroups < 256 && !p.one ? std::min<int64_t>(std::min<int64_t>(512 / qgroups, d->Tk / 128), 64) : 1;
+  // (where one of a workgroup's four waves has all the rows, four times as many workgroups: 42 x 2 queries, 4168 keys, 8 heads of 48, fp32
+  // 742 -> 545 us and 6 for the join; 12 x 8 queries, 14953 keys, 4 heads of 51 329 + 7 -> 317 + 17)
+  const int64_t goal = rows <= own / 4 ? 2048 : 512;
+  int64_t parts = qgroups < goal / 2 && !p.one ? std::min<int64_t>(std::min<int64_t>(goal / qgroups, d->Tk / 128), 64) : 1;
   if (parts < 1) parts = 1;
   p.qchunk = (int)(((d->Tk + parts - 1) / parts + 63) / 64 * 64);
   p.qsplits = parts > 1 ? (d->Tk + p.qchunk - 1) / p.qchunk : 1;

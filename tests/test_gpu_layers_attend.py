@@ -351,3 +351,13 @@ def test_gradients_are_split(size, dtype):
     r.workspace.fill_(255)
     r.backward()
     assert all(torch.equal(a, b) for a, b in zip(got, (r.dq, r.dk, r.dv)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(40, 2, 600, 8, 8, 24), (70, 3, 400, 8, 4, 50), (40, 1, 700, 7, 7, 136)])
+def test_keys_are_split_for_few_rows_of_many_heads(size, dtype):
+    """More row tiles than compute units, of which one wave has all the rows: dq's keys are split for these too."""
+    ly = _ly()
+    rng = rng_for("few rows", *size, dtype)
+    s, q_len, k_len, m = inputs(rng, *size, dtype, lens=True, mask=True)
+    check(ly, s, q_len, k_len, m, dtype)
