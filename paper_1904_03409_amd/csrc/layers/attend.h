@@ -198,33 +198,51 @@ __device__ __forceinline__ f32x4 product(const frag_t<T>& a, const frag_t<T>& b,
     return c;
   }
 }
-// acc[j][dt] += (columns 16 dt .. of unit row `base` on)^T times the weights w[j].
-template <typename T, int DP, int N>
-__device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq, const frag_t<T> (&w)[N]) {
+// acc[j][dt] += (columns 16 dt .. of the NU units from row `base` on)^T times the weights w[u][j].
+// fp32 takes a call's products from 0 on and adds what they come to, so that acc has a rounding for 16 NU rows and not for each: a chain of
+// n roundings is off by 2.5e-8 sqrt(n / 2) of a sum of random signs (16384 keys: 2.3e-6, where its terms are good to 3e-7).
+template <typename T, int DP, int N, int NU>
+__device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq, const frag_t<T> (&w)[NU][N]) {
   typedef Head<T, DP> H;
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int dt = 0; dt < H::DT; ++dt) {
-      const frag_t<T> a = column<T, H::GPR>(tile, base, dt, l16, lq);
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int j = 0; j < N; ++j) acc[j][dt] = mfma_bf16_16x16x32(a, w[j], acc[j][dt]);
-    }
+      for (int dt = 0; dt < H::DT; ++dt) {
+        const frag_t<T> a = column<T, H::GPR>(tile, base + u * H::UNIT, dt, l16, lq);
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j][dt] = mfma_bf16_16x16x32(a, w[u][j], acc[j][dt]);
+      }
   } else {
     // (the next columns are on their way during these ones' products: left to itself the compiler read one number, waited, read the
     // next. 2 x 2048 x 2000, 8 heads of 256, forward, dq, dk and dv: 804, 1076, 1260 us; 673, 856, 1056 this way, here and in scores)
     frag_t<T> a = column<T, H::GPR>(tile, base, 0, l16, lq);
+    f32x4 t[2][N];
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) {
-      frag_t<T> next = a;
-      if (dt + 1 < H::DT) next = column<T, H::GPR>(tile, base, dt + 1, l16, lq);
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int j = 0; j < N; ++j) t[dt & 1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], w[j][e], acc[j][dt], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      a = next;
+      for (int u = 0; u < NU; ++u) {
+        frag_t<T> next = a;
+        if (u + 1 < NU) next = column<T, H::GPR>(tile, base + (u + 1) * H::UNIT, dt, l16, lq);
+        else if (dt + 1 < H::DT) next = column<T, H::GPR>(tile, base, dt + 1, l16, lq);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < N; ++j) t[dt & 1][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], w[u][j][e], t[dt & 1][j], 0, 0, 0);
+        // (the columns before these: their products have ended)
+        if (u == 0 && dt > 0) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) acc[j][dt - 1] += t[(dt - 1) & 1][j];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        a = next;
+      }
     }
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j][H::DT - 1] += t[(H::DT - 1) & 1][j];
   }
 }
 

@@ -17,11 +17,17 @@
 
 namespace {
 
-template <typename T, int DP, bool DMA>
+// Units of a tile whose sums are taken in one call: fp32 has an addition for each call (sums), which takes the place of products.
+// 2 x 1024 x 1000, 8 heads, dq and dk and dv, by ones and by twos: of 64 74, 90 and 71, 87 us; of 128 151, 318 and 140, 289.
+template <typename T, int NU>
+constexpr int kPair = sizeof(T) == 4 && NU > 1 ? 2 : 1;
+
+template <typename T, int DP, bool DMA, bool DQ>
 struct Bwd {
   typedef Head<T, DP> H;
-  // rows of a tile in LDS: two tiles of 32 KB at most together with what is kept in registers; 16 own rows to a wave at 256
-  static constexpr int R = H::BYTES <= 256 ? 64 : H::BYTES <= 512 ? 32 : 16, NU = R / H::UNIT;
+  // rows of a tile in LDS: two tiles of 32 KB at most together with what is kept in registers; 16 own rows to a wave at 256 (of fp32 dk
+  // and dv by way of registers; 32 rows of these spill, and 16 elsewhere take 257 us for dq's 232, 362 for dk's and dv's 300)
+  static constexpr int R = H::BYTES <= 256 ? 64 : H::BYTES <= 512 || DMA || DQ ? 32 : 16, NU = R / H::UNIT, UP = kPair<T, NU>;
   static constexpr int TILE = R * H::BYTES, LDS = 4 * TILE + 2 * 3 * R * 4;
   // own rows of a wave / 16, of a workgroup (fp32 heads of 128 by way of registers: two would not fit)
   static constexpr int QT = DP <= 64 || (DP == 128 && (DMA || sizeof(T) == 2)) ? 2 : 1, OWN = 64 * QT;
@@ -34,7 +40,7 @@ struct Bwd {
 // waves on a SIMD that way: bf16 heads of 128; with everything in registers one wave has 337).
 template <typename T, int DP, bool DMA, bool BIG>
 struct Keys {
-  typedef Bwd<T, DP, DMA> F;
+  typedef Bwd<T, DP, DMA, false> F;
   static constexpr int NT = BIG ? 512 : 256, N = BIG ? 2 : F::QT, ALL = NT / 4 * N, WAVES = BIG ? 2 : F::WDKV;
   static constexpr int LDS = F::LDS + (BIG ? ALL * F::H::BYTES : 0);
 };
@@ -51,9 +57,9 @@ struct Short {
 }  // namespace
 
 template <typename T, int DP, bool DMA>
-__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(AttendArgs a) {
+__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA, true>::WDQ)) k_attend_dq(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Bwd<T, DP, DMA> F;
+  typedef Bwd<T, DP, DMA, true> F;
   typedef frag_t<T> frag;
   constexpr int QT = F::QT;
   extern __shared__ __align__(16) unsigned char sm[];
@@ -188,21 +194,23 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
       put_delta();
     }
 #pragma unroll
-    for (int u = 0; u < F::NU; ++u) {
-      frag w[QT];
+    for (int u0 = 0; u0 < F::NU; u0 += F::UP) {
+      frag w[F::UP][QT];
 #pragma unroll
-      for (int i = 0; i < H::SUB; ++i) {
-        f32x4 p[QT], dp[QT];
-        probs(u, i, p, dp);
+      for (int u = 0; u < F::UP; ++u)
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
-          f32x4 ds;
+        for (int i = 0; i < H::SUB; ++i) {
+          f32x4 p[QT], dp[QT];
+          probs(u0 + u, i, p, dp);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) ds[r] = p[j][r] * (dp[j][r] - delta[j]);
-          put_weights(w[j], i, ds);
+          for (int j = 0; j < QT; ++j) {
+            f32x4 ds;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ds[r] = p[j][r] * (dp[j][r] - delta[j]);
+            put_weights(w[u][j], i, ds);
+          }
         }
-      }
-      sums<T, DP, QT>(o, kt, u * H::UNIT, l16, lq, w);
+      sums<T, DP, QT, F::UP>(o, kt, u0 * H::UNIT, l16, lq, w);
     }
   }
 #pragma unroll
@@ -221,7 +229,7 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA>::WDQ)) k_attend_dq(Atten
 template <typename T, int DP, bool DMA, bool BIG>
 __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA, BIG>::WAVES)) k_attend_dkv(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Bwd<T, DP, DMA> F;
+  typedef Bwd<T, DP, DMA, false> F;
   typedef frag_t<T> frag;
   typedef Keys<T, DP, DMA, BIG> K;
   constexpr int KN = K::N;
@@ -306,33 +314,36 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
     __syncthreads();
     if (n + 1 < all) go(n + 1);
 #pragma unroll
-    for (int u = 0; u < F::NU; ++u) {
-      frag wp[KN], ws[KN];
+    for (int u0 = 0; u0 < F::NU; u0 += F::UP) {
+      frag wp[F::UP][KN], ws[F::UP][KN];
 #pragma unroll
-      for (int i = 0; i < H::SUB; ++i) {
-        f32x4 s[KN], dp[KN];
+      for (int u = 0; u < F::UP; ++u)
 #pragma unroll
-        for (int j = 0; j < KN; ++j) s[j] = dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        scores<T, DP, KN>(s, qt, u * H::UNIT, i, l16, lq, k);
-        if constexpr (BIG) scores_lds<T, DP, KN>(dp, gt, u * H::UNIT, i, l16, lq, own);
-        else scores<T, DP, KN>(dp, gt, u * H::UNIT, i, l16, lq, v);
-        const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
-        const f32x4 m = *(const f32x4*)(st + at), inv = *(const f32x4*)(st + F::R + at), delta = *(const f32x4*)(st + 2 * F::R + at);
+        for (int i = 0; i < H::SUB; ++i) {
+          const int unit = (u0 + u) * H::UNIT;
+          f32x4 s[KN], dp[KN];
 #pragma unroll
-        for (int j = 0; j < KN; ++j) {
-          f32x4 p, ds;
+          for (int j = 0; j < KN; ++j) s[j] = dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          scores<T, DP, KN>(s, qt, unit, i, l16, lq, k);
+          if constexpr (BIG) scores_lds<T, DP, KN>(dp, gt, unit, i, l16, lq, own);
+          else scores<T, DP, KN>(dp, gt, unit, i, l16, lq, v);
+          const int at = unit + row_of<T>(i, 4 * lq);
+          const f32x4 m = *(const f32x4*)(st + at), inv = *(const f32x4*)(st + F::R + at), delta = *(const f32x4*)(st + 2 * F::R + at);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float x = there[j] ? s[j][r] * a.c : -INFINITY;
-            p[r] = __builtin_amdgcn_exp2f(x - m[r]) * inv[r];
-            ds[r] = p[r] * (dp[j][r] - delta[r]);
+          for (int j = 0; j < KN; ++j) {
+            f32x4 p, ds;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float x = there[j] ? s[j][r] * a.c : -INFINITY;
+              p[r] = __builtin_amdgcn_exp2f(x - m[r]) * inv[r];
+              ds[r] = p[r] * (dp[j][r] - delta[r]);
+            }
+            put_weights(wp[u][j], i, p);
+            put_weights(ws[u][j], i, ds);
           }
-          put_weights(wp[j], i, p);
-          put_weights(ws[j], i, ds);
         }
-      }
-      sums<T, DP, KN>(dv, gt, u * H::UNIT, l16, lq, wp);
-      sums<T, DP, KN>(dk, qt, u * H::UNIT, l16, lq, ws);
+      sums<T, DP, KN, F::UP>(dv, gt, u0 * H::UNIT, l16, lq, wp);
+      sums<T, DP, KN, F::UP>(dk, qt, u0 * H::UNIT, l16, lq, ws);
     }
   }
 #pragma unroll
@@ -478,29 +489,34 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 && sizeof(T) == 2 && DMA ? 4 
           if (l16 == 0) *(f32x4*)(parts + wave * R + at) = part;
         }
       __syncthreads();
+      constexpr int UP = kPair<T, F::NU>;
 #pragma unroll
-      for (int u = 0; u < F::NU; ++u) {
-        frag wp[KN], ws[KN];
+      for (int u0 = 0; u0 < F::NU; u0 += UP) {
+        frag wp[UP][KN], ws[UP][KN];
 #pragma unroll
-        for (int i = 0; i < H::SUB; ++i) {
-          const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
-          f32x4 delta = *(const f32x4*)(parts + at);
+        for (int half = 0; half < UP; ++half) {
+          const int u = u0 + half;
 #pragma unroll
-          for (int w = 1; w < NW; ++w) delta += *(const f32x4*)(parts + w * R + at);
+          for (int i = 0; i < H::SUB; ++i) {
+            const int at = u * H::UNIT + row_of<T>(i, 4 * lq);
+            f32x4 delta = *(const f32x4*)(parts + at);
 #pragma unroll
-          for (int j = 0; j < KN; ++j) {
-            f32x4 ds;
+            for (int w = 1; w < NW; ++w) delta += *(const f32x4*)(parts + w * R + at);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) ds[r] = p[u][i][j][r] * (dp[u][i][j][r] - delta[r]);
-            put_weights(wp[j], i, p[u][i][j]);
-            put_weights(ws[j], i, ds);
+            for (int j = 0; j < KN; ++j) {
+              f32x4 ds;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) ds[r] = p[u][i][j][r] * (dp[u][i][j][r] - delta[r]);
+              put_weights(wp[half][j], i, p[u][i][j]);
+              put_weights(ws[half][j], i, ds);
+            }
           }
-        }
-        // (a lane's weights are neighbours in a key's row of s: one granule)
+          // (a lane's weights are neighbours in a key's row of s: one granule)
 #pragma unroll
-        for (int j = 0; j < KN; ++j) *(frag*)(ds_ + key[j] * F::SROW + ((4 * u + lq) ^ swz<T, F::SROW / 16>(key[j])) * 16) = ws[j];
-        sums<T, DP, KN>(dv, gt, u * H::UNIT, l16, lq, wp);
-        sums<T, DP, KN>(dk, qt, u * H::UNIT, l16, lq, ws);
+          for (int j = 0; j < KN; ++j) *(frag*)(ds_ + key[j] * F::SROW + ((4 * u + lq) ^ swz<T, F::SROW / 16>(key[j])) * 16) = ws[half][j];
+        }
+        sums<T, DP, KN, UP>(dv, gt, u0 * H::UNIT, l16, lq, wp);
+        sums<T, DP, KN, UP>(dk, qt, u0 * H::UNIT, l16, lq, ws);
       }
       __syncthreads();
 #pragma unroll
@@ -662,7 +678,7 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
     if (!plan.one && d->Tq) {
       a.splits = plan.qsplits, a.chunk = plan.qchunk;
       auto run = [&](auto dma) {
-        typedef Bwd<T, DP, decltype(dma)::value> F;
+        typedef Bwd<T, DP, decltype(dma)::value, true> F;
         static std::atomic<uint64_t> dev;
         a.tiles = (int)(((int64_t)d->Tq * a.G + F::OWN - 1) / F::OWN);
         return attend_launch(k_attend_dq<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk * a.splits, F::LDS, dev, st);

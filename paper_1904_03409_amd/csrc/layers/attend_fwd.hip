@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
 #pragma unroll
       for (int j = 0; j < QT; ++j) {
         const float ref = m[j] == -INFINITY ? 0.f : m[j];
+        float sum = 0.f;                               // (a tile's, so that l has a rounding for a tile)
 #pragma unroll
         for (int u = 0; u < F::NU; ++u) {
 #pragma unroll
@@ -218,14 +219,14 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i][j][r], c, -ref));
-              l[j] += p[r];
+              sum += p[r];
             }
             put_weights(w[u][j], i, p);
           }
         }
+        l[j] += sum;
       }
-#pragma unroll
-      for (int u = 0; u < F::NU; ++u) sums<T, DP, QT>(o, vt, wk * F::KW + u * H::UNIT, l16, lq, w[u]);
+      sums<T, DP, QT, F::NU>(o, vt, wk * F::KW, l16, lq, w);
     }
     if constexpr (F::STAGES == 1) {
       __syncthreads();
