@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
   const int qlen = clamp_len(a.q_len, b, a.Tq), klen = clamp_len(a.k_len, b, a.Tk);
   const int kbeg = pl.split * a.chunk;
   int tile = LOOP ? pl.tile * a.reps : pl.tile;
-  const int tend = LOOP ? min(tile + a.reps, (rows + ROWS - 1) / ROWS) : tile + 1;
+  const int tend = LOOP ? min(tile + a.reps, (rows - 1) / ROWS + 1) : tile + 1;        // (rows: up to 2^31 - 1)
   // (no query of the tile is there: no keys)
   auto keys_end = [&] { return uni(tile * ROWS / a.G < qlen ? min(klen, kbeg + a.chunk) : kbeg); };
   int kend = keys_end();
