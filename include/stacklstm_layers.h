@@ -36,7 +36,7 @@ typedef struct {
   int32_t Hq, Hk;          /* heads of queries and of keys and values, 1 .. 2^16; Hq a multiple of Hk */
   int32_t D;               /* width of a head, 1 .. 256 */
   int32_t type;            /* slstm_type of every matrix */
-  float scale;             /* finite */
+  float scale;             /* -2^127 .. 2^127 */
   slstm_strides q, k, v, dy;        /* of inputs: >= 0, all three 0: dense [B, T, H, D]; a stride may be 0 (broadcast) */
   slstm_strides y, dq, dk, dv;      /* of outputs: all three 0: dense; no two elements at one place (SLSTM_EINVAL) */
 } slstm_attend_dims;       /* B Tq Hq and B Tk Hk < 2^31; strides < 2^40 */

@@ -423,7 +423,7 @@ inline bool attend_ok(const slstm_attend_dims* d) {
       d->Hq > (1 << 16) || d->Hk > (1 << 16) || d->Hq % d->Hk || d->D < 1 || d->D > 256)
     return false;
   if (d->type != SLSTM_F32 && d->type != SLSTM_BF16) return false;
-  if (!(fabsf(d->scale) <= 3.4028234e38f)) return false;
+  if (!(fabsf(d->scale) <= 0x1p127f)) return false;    // (scale log2 e is finite too)
   if ((int64_t)d->Tq * d->Hq > 0x7fffffff || (int64_t)d->Tk * d->Hk > 0x7fffffff) return false;
   if ((int64_t)d->Tq * d->Hq * d->B > 0x7fffffff || (int64_t)d->Tk * d->Hk * d->B > 0x7fffffff) return false;
   const slstm_strides* s[8] = {&d->q, &d->k, &d->v, &d->dy, &d->y, &d->dq, &d->dk, &d->dv};
