@@ -116,7 +116,9 @@ __device__ __forceinline__ int given(const LogArgs& a, int64_t row, int g) {
   return a.legal && !a.legal[row * a.V + i] ? kBarred : i;
 }
 __device__ __forceinline__ float log_prob(int place, float x, float m, float logs) {
-  return place == kAbsent ? 0.f : place == kBarred || x == -INFINITY ? -INFINITY : (x - m) - logs;
+  // (a logit of -inf in a row with NaN or +inf: NaN, as its others are)
+  const bool none = place == kBarred || (x == -INFINITY && logs == logs);
+  return place == kAbsent ? 0.f : none ? -INFINITY : (x - m) - logs;
 }
 // Gradient of a row's elements: -e (c1 + c2 t), and what its tokens add.
 struct RowGrad {
