@@ -1,9 +1,13 @@
-"""Forms of the attention kernels that only certain sizes reach, and calls at the ends of what is allowed."""
+"""Forms of the layers' kernels that only certain sizes reach, and calls at the ends of what is allowed."""
+import numpy as np
 import pytest
 import torch
 
+from tests import layers_ref as ref
 from tests.gpu_helpers import need_gpu
-from tests.head_gpu import DT
+from tests.head_gpu import DT, get, rng_for, up
+from tests.test_gpu_layers_attend import check, dev, heads, inputs, within
+from tests.test_gpu_layers_logprob import _check, _inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +33,71 @@ def test_rows_up_to_31_bits(dtype):
     assert low == v.squeeze() and high == v.squeeze()
     del y
     torch.cuda.empty_cache()
+
+
+# up to 16 rows (queries times the heads that share a key), whose waves share the keys, in every width by DMA and by way of registers; two row tiles to a
+# wave by way of registers; dq and dk and dv of every width both ways, with keys in several tiles
+SIZES = [(2, 1, 300, 8, 2, 128), (1, 4, 500, 2, 1, 100), (1, 3, 200, 2, 2, 131), (2, 2, 300, 2, 1, 256), (3, 2, 150, 8, 1, 27), (2, 5, 400, 3, 3, 32), (1, 16, 170, 1, 1, 61),
+         (2, 3, 290, 4, 1, 64), (2, 70, 90, 2, 2, 50), (2, 90, 70, 2, 1, 30), (1, 50, 150, 2, 1, 63), (2, 40, 140, 2, 2, 29), (1, 80, 300, 2, 1, 121), (1, 60, 150, 1, 1, 250), (2, 34, 135, 1, 1, 32),
+         (2, 100, 140, 2, 2, 64), (1, 65, 129, 1, 1, 24), (1, 20, 130, 4, 1, 160), (2, 3, 180, 2, 1, 101),
+         (1, 20, 100, 2, 1, 121), (2, 24, 100, 2, 2, 40)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES)
+def test_forms(size, dtype):
+    ly = _ly()
+    rng = rng_for("forms", *size, dtype)
+    check(ly, *inputs(rng, *size, dtype, lens=size[0] > 1, mask=size[5] % 2 == 0), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(400, 130, 100, 4, 4, 40), (400, 130, 100, 4, 4, 37), (200, 300, 128, 4, 2, 24), (200, 300, 65, 4, 2, 21), (820, 70, 64, 2, 1, 64), (820, 70, 33, 2, 1, 17)])
+def test_several_row_tiles_over_keys_that_stay(size, dtype):
+    """A workgroup's later row tiles behind the last query, keys that end in the first tile or the second, masks, sequences without keys; NaN and
+    infinities in what is not there."""
+    ly = _ly()
+    rng = rng_for("stay", *size, dtype)
+    B, Tq, Tk, Hq, Hk, D = size
+    s, q_len, k_len, m = inputs(rng, *size, dtype, lens=True, mask=True)
+    m[4:B // 2] |= 1                                     # (all keys of these are there)
+    q_len[5:9] = Tq, 0, 65, 64
+    k_len[5:9] = Tk, Tk, 1, Tk // 2
+    ok = ref.seen(B, Tq, Tk, q_len, k_len, m)
+    clean = {n: a.copy() for n, a in s.items()}
+    no_key, no_query = ~ref.seen(B, 1, Tk, None, k_len, m)[:, 0], ~ok.any(2)
+    for n, none in (("k", no_key), ("v", no_key), ("q", no_query), ("dy", no_query)):
+        s[n][none] = rng.choice([np.nan, np.inf, -np.inf], s[n][none].shape)
+    t = {n: heads(a, dtype) for n, a in s.items()}
+    r = ly.AttendRun.of(t["q"], t["k"], t["v"], dev(q_len), dev(k_len), dev(m), dy=t["dy"])
+    for x in (r.y, r.dq, r.dk, r.dv):
+        x.fill_(7)
+    r.forward(), r.backward()
+    assert not get(r.y)[no_query].any() and not get(r.dq)[no_query].any()
+    some = np.unique(np.r_[0:10, B - 2, B - 1, rng.integers(0, B, 20)])
+    want, off = ref.attend(*(clean[n][some] for n in "qkv"), ok[some], D ** -0.5, clean["dy"][some], dtype, bounds=True)
+    for n, x in (("y", r.y), ("dq", r.dq), ("dk", r.dk), ("dv", r.dv)):
+        within(x[torch.from_numpy(some).cuda()], want[n], off[n], n)
+    # without a mask and lengths (whole tiles), against every sequence alone
+    y = ly.AttendRun.of(*(heads(clean[n], dtype) for n in "qkv")).forward()
+    for b in (0, B // 3, B - 1):
+        one = ly.AttendRun.of(*(heads(clean[n][b:b + 1], dtype) for n in "qkv")).forward()
+        want, off = ref.attend(*(clean[n][b:b + 1] for n in "qkv"), ref.seen(1, Tq, Tk), D ** -0.5, None, dtype, bounds=True)
+        within(y[b:b + 1], want["y"], off["y"], "y")
+        within(one, want["y"], off["y"], "y alone")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,V,G,N", [(30, 700, 2, 3), (513, 20001, 1, 5)])
+def test_best_tokens(R, V, G, N, dtype):
+    """Two and four vectors in a lane of a wave, a workgroup of 512 threads to a row."""
+    ly = _ly()
+    rng = rng_for("forms", R, V, G, N, dtype)
+    x, token, legal, a, h = _inputs(rng, R, V, G, dtype)
+    few = np.unique(np.r_[0:4, R - 1, rng.integers(0, R, 8)])
+    want = ref.logprob(x[few], token[few], legal[few], N, a[few].astype(np.float64), h[few].astype(np.float64))
+    r = ly.LogProbRun.of(up(x, dtype), up(token), up(legal), N, up(a), up(h))
+    r.step()
+    _check(r, few, want, dtype, a[few], h[few])
+    r.forward(), r.backward()
+    _check(r, few, want, dtype, a[few], h[few])
