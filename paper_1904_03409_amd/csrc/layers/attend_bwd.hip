@@ -368,7 +368,7 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
 // not at all: delta = sum p dp over the keys that are here. The waves share 32 or 16 keys each for the scores and the sums of dk and
 // dv; their s go through LDS, where dq's product takes a query tile to a wave, over all keys.
 template <typename T, int DP, bool DMA, int NW, int KN>
-__global__ void __launch_bounds__(64 * NW, NW == 8 && sizeof(T) == 2 && DMA ? 4 : 2) k_attend_short(AttendArgs a) {
+__global__ void __launch_bounds__(64 * NW, 2) k_attend_short(AttendArgs a) {
   typedef Head<T, DP> H;
   typedef Short<T, DP, NW, KN> F;
   typedef frag_t<T> frag;

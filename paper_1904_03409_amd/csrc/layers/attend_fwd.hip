@@ -1,7 +1,7 @@
 // Attention, forward: one pass over the keys with the running reference and sum of the softmax.
 //   x = c q . k (base 2),  l = sum 2^(x - m),  o = sum 2^(x - m) v,  y = o / l
-// The reference m of a row need not be its largest x: any number within 2^8 of it serves as well, and o and l are only brought
-// to a new one when a row's largest has risen by more than 8 (rarely behind the first tiles).
+// The reference m of a row need not be its largest x: one that is up to 8 below serves as well (weights then reach 2^8), and o and l are
+// only brought to a new one when a row's largest has risen by more than 8 (rarely behind the first tiles).
 // A wave has 16 QT queries (query and head of those that share a key's head) and all of a key tile, or, where there are few
 // queries, a quarter of the tile (WK = 4), whose parts are joined through LDS. Where the row tiles do not fill the chip the
 // keys are split over workgroups and k_attend_join joins their sums.
