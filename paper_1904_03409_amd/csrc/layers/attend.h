@@ -487,7 +487,9 @@ hipError_t attend_launch(K kern, AttendArgs a, int64_t groups, int lds, std::ato
     if (e != hipSuccess) return e;
   }
   // about eight runs to an XCD: of whole sequences (whose heads lie in the same cache lines) where there are 8 of them, of parts of a head's
-  // tiles where there are few heads
+  // tiles where there are few heads. Forward + backward us, like this, undealt, and in eight whole runs: 2 x 1000 x 1000, 64 heads of 64, bf16
+  // 54 + 143, 64 + 149, 57 + 154; 64 x 240 x 240, 8 of 64, fp32 78 + 251, 82 + 253, 76 + 248; 2 x 4096 x 4000, 16 of 128 over 4, bf16 244 + 818, 240 + 815,
+  // 276 + 925; 256 x 240 x 120, 8 of 64, bf16 48 + 109, 49 + 111, 48 + 107 (lengths ragged)
   const int64_t per = (int64_t)a.tiles * a.splits, heads = (int64_t)a.B * a.Hk;
   a.piece = a.B >= 8 ? per * a.Hk * (a.B >= 128 ? a.B / 64 : 1) : heads >= 64 ? per * (heads / 64) : (per + 64 / heads - 1) / (64 / heads);
   a.full = groups / (8 * a.piece) * (8 * a.piece);

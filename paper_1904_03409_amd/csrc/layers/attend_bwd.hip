@@ -580,7 +580,10 @@ __global__ void __launch_bounds__(256) k_attend_sum(const float* part, int split
 namespace {
 
 // Keys of a workgroup of k_attend_dkv, and splits of its queries. 256 keys with eight waves (Keys) where they are there;
-// queries are split, 64 of them at least to each part, until there are two workgroups to a compute unit, where there is not one to each
+// queries are split, 64 of them at least to each part, until there are two workgroups to a compute unit, where there is not one to each (backward
+// us: 1 x 500 x 500, 4 heads of 100, fp32 97, 118 from 128 queries on, 199 whole; 1 x 3000 x 300, 2 heads of 64, fp32 72, 75 with up to 16 parts, 85
+// with up to 64, but one head over 16384 queries of 4 and 100 keys 430, 235 with up to 64; 2 x 4096 x 1000, 4 heads of 64, bf16 65, 67 for one workgroup
+// to a compute unit, 75 for four)
 // (2 sequences of 4096 x 4000, 4 key heads of 128, of unequal lengths: eight waves and four parts 541 + 23 us; four waves with
 // everything in registers and no parts 872, eight with 16 keys each 742).
 struct KeyPlan {
@@ -596,12 +599,15 @@ KeyPlan key_plan(const slstm_attend_dims* d) {
   p.tiles = (d->Tk + keys - 1) / keys;
   const int64_t groups = std::max<int64_t>(1, (int64_t)p.tiles * d->B * d->Hk), most = (int64_t)d->Tq * (d->Hq / d->Hk) / 64;
   p.splits = (int)std::max<int64_t>(1, groups < 256 ? std::min<int64_t>(std::min<int64_t>(512 / groups, most), 32) : 1);
-  // few row tiles, many keys: splits of 128 keys at least, likewise (1 x 9 queries of 4 heads over 16000 keys)
+  // few row tiles, many keys: splits of 128 keys at least, likewise (backward us: 1 x 300 queries over 4000 keys, one head of 128, fp32
+  // 109, 878 whole, 101 from 64 keys on, 132 from 256; 1 x 9 over 16000, 4 heads of 64, 82, and 99 with up to 32 or 128 splits; 1 x 64 over 16000,
+  // 4 heads of 64 over one, bf16, 60, 55 with up to 32, 78 with up to 128)
   const int own = d->D <= 128 ? 128 : 64;
   const int64_t rows = (int64_t)d->Tq * (d->Hq / d->Hk), qgroups = std::max<int64_t>(1, (rows + own - 1) / own * d->B * d->Hk);
-  // (where one of a workgroup's four waves has all the rows, four times as many workgroups: 42 x 2 queries, 4168 keys, 8 heads of 48, fp32
-  // 742 -> 545 us and 6 for the join; 12 x 8 queries, 14953 keys, 4 heads of 51 329 + 7 -> 317 + 17)
-  const int64_t goal = rows <= own / 4 ? 2048 : 512;
+  // (where one of a workgroup's four waves has all the rows, twice as many workgroups. Backward us with 512, 1024 and 2048: 42 x 2 queries, 4168
+  // keys, 8 heads of 48, fp32 1306, 1036, 1037, bf16 331, 293, 297; of 128 2711, 2154, 2175 and 639, 608, 613; 12 x 8, 14953 keys, 4 heads of 51 823, 838,
+  // 853 and 255, 258, 264; 32 x 4, 4000 keys, 16 heads over 4, of 200, fp32 2025, 2039, 2078, of 256, bf16 779, 799, 839)
+  const int64_t goal = rows <= own / 4 ? 1024 : 512;
   int64_t parts = qgroups < goal / 2 && !p.one ? std::min<int64_t>(std::min<int64_t>(goal / qgroups, d->Tk / 128), 64) : 1;
   if (parts < 1) parts = 1;
   p.qchunk = (int)(((d->Tk + parts - 1) / parts + 63) / 64 * 64);

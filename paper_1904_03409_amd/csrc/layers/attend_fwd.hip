@@ -364,14 +364,19 @@ FwdPlan fwd_plan(const slstm_attend_dims* d) {
   else p.qt = 2, p.wk = 1;
   p.rows = 16 * p.qt * (4 / p.wk);
   p.tiles = (int)((R + p.rows - 1) / p.rows);
-  // splits of 128 keys at least, until there are two workgroups to a compute unit, where there is not one to each
+  // splits of 128 keys at least, until there are two workgroups to a compute unit, where there is not one to each (us of a call: a query over
+  // 4096 keys, 8 heads of 64, bf16 9.7, 11.1 from 64 keys on, 10.0 from 256, 28 whole; 300 queries over 4000 keys, one head of 128, fp32 23, 26, 31,
+  // 333; 8 x 8 queries over up to 16384 keys, 16 heads of 128 over 4, bf16 41, 59 for one workgroup to a compute unit, 48 for four; but a query of 32
+  // heads over 8, 16384 keys, 26, 20 for one)
   const int64_t groups = (int64_t)p.tiles * d->B * d->Hk;
   const int64_t want = groups > 0 && groups < 256 ? 512 / groups : 1, most = ((int64_t)d->Tk + 127) / 128;
   p.splits = (int)std::max<int64_t>(1, std::min(want, most));
   p.chunk = (((d->Tk + p.splits - 1) / p.splits) + 127) / 128 * 128;
   if (p.chunk < 128) p.chunk = 128;
   p.splits = std::max(1, (d->Tk + p.chunk - 1) / p.chunk);
-  // few keys, many row tiles: several of them to a workgroup as long as there are three workgroups to a compute unit
+  // few keys, many row tiles: several of them to a workgroup as long as there are three workgroups to a compute unit (with it and without: 256 x
+  // 240 x 60, 8 heads of 64, fp32 107, 132 us; 512 x 240 x 60, 8 of 50 268, 345; bf16 256 x 240 x 120, 8 of 64 48, 50; 64 x 500 x 100 28.8, 27.2; 400 x 130 x
+  // 100, 4 of 32 26.0, 24.8; as long as there are one to six 0 to 5% either way)
   p.reps = 1;
   if (p.wk == 1 && R > 64 && d->Tk <= kLoopKeys && d->D <= 64 && p.splits == 1) {
     p.reps = (int)std::max<int64_t>(1, std::min<int64_t>(p.tiles, groups / 768));
