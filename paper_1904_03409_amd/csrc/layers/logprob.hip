@@ -524,9 +524,13 @@ bool logprob_ok(const slstm_logprob_dims* d) {
          d->N <= kMost && (d->type == SLSTM_F32 || d->type == SLSTM_BF16) && stride_ok(d->ld_logits, d->V) &&
          stride_ok(d->ld_dlogits, d->V);
 }
-// Whole rows in registers hold up to 8192 vectors; rows of four chunks or more are cut where there are not two
-// of them for every compute unit.
-bool logprob_cut(const slstm_logprob_dims* d) { return row_vecs(d) > 8192 || (row_chunks(d) >= 4 && d->rows < 512); }
+// Whole rows in registers hold up to 8192 vectors. Shorter ones are cut where they are long, 16-bit (twice the work to a vector) and few. A call's
+// us, cut and whole; outputs alone, with the 16 best, with the gradient: 64 x 64001 bf16 9.8, 9.4; 12.8, 16.4; 13.1, 15.5; of 200 rows 9.8, 9.7;
+// 17.3, 16.7; 20.5, 17.2; of 400 13.4, 15.4; 24.6, 22.7; 32.6, 27.0. 64 x 32000 fp32 10.0, 7.2; 11.2, 9.9; 13.1, 8.2; of 400 rows 11.9, 11.0; 21.1, 16.9;
+// 29.1, 17.8. 64 x 32000 bf16 10.1, 7.1; 11.5, 10.5; 13.3, 9.0.
+bool logprob_cut(const slstm_logprob_dims* d) {
+  return row_vecs(d) > 8192 || (d->type == SLSTM_BF16 && row_vecs(d) > 4096 && d->rows < 128);
+}
 
 template <typename F>
 void logprob_dispatch(const slstm_logprob_dims* d, bool top, F f) {
