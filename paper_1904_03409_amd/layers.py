@@ -110,6 +110,8 @@ def strides_of(t):
     B, T, H, D = t.shape
     dense = (T * H * D, H * D, D)
     s = [d if n < 2 else v for v, d, n in zip(t.stride(), dense, (B, T, H))]
+    if not any(s) and t.numel():
+        raise ValueError("a matrix of heads may not be one head for all sequences, places and heads: such strides stand for dense")
     return slstm_strides(*s)
 
 
@@ -207,7 +209,7 @@ class AttendRun:
 
     @classmethod
     def of(cls, q, k, v, q_len=None, k_len=None, mask=None, scale=None, dy=None, y=None, train=None):
-        """q [B, Tq, Hq, D], k and v [B, Tk, Hk, D], any strides with neighbouring elements of a head; y: where the outputs go (by
+        """q [B, Tq, Hq, D], k and v [B, Tk, Hk, D], any strides with neighbouring elements of a head (not 0 for all three axes); y: where the outputs go (by
         default a buffer of its own in the order of q's axes); scale: 1 / sqrt(D) by default; train: buffers for a backward too
         (by default where dy is given; a dy that is set later has the strides of y)."""
         (B, Tq, Hq, D), (Tk, Hk) = q.shape, k.shape[1:3]
