@@ -31,8 +31,9 @@ struct Bwd {
   static constexpr int TILE = R * H::BYTES, LDS = 4 * TILE + 2 * 3 * R * 4;
   // own rows of a wave / 16, of a workgroup (fp32 heads of 128 by way of registers: two would not fit)
   static constexpr int QT = DP <= 64 || (DP == 128 && (DMA || sizeof(T) == 2)) ? 2 : 1, OWN = 64 * QT;
-  // waves on a SIMD that the registers are to leave room for: two hide each other's waits (bf16 heads of 128, dq: 230 registers)
-  static constexpr int WDQ = H::BYTES <= 128 || (DMA && H::BYTES <= 256 && sizeof(T) == 2) ? 2 : 1;
+  // waves on a SIMD that the registers are to leave room for: two hide each other's waits (bf16, dq: 237 registers of heads of 128, 253 of 256;
+  // 4 x 2048 x 2000, 8 heads of 256: 257 us, with one wave 553)
+  static constexpr int WDQ = H::BYTES <= 128 || (DMA && sizeof(T) == 2) ? 2 : 1;
   static constexpr int WDKV = H::BYTES <= 128 ? 2 : 1;
 };
 
