@@ -200,8 +200,11 @@ __device__ __forceinline__ f32x4 product(const frag_t<T>& a, const frag_t<T>& b,
 }
 // acc[j][dt] += (columns 16 dt .. of the NU units from row `base` on)^T times the weights w[u][j].
 // fp32 takes a call's products from 0 on and adds what they come to, so that acc has a rounding for 16 NU rows and not for each: a chain of
-// n roundings is off by 2.5e-8 sqrt(n / 2) of a sum of random signs (16384 keys: 2.3e-6, where its terms are good to 3e-7).
-template <typename T, int DP, int N, int NU>
+// n roundings is off by 2.5e-8 sqrt(n / 2) of a sum of random signs (16384 keys: 2.3e-6, where its terms are good to 3e-7). The additions' cost:
+// 4 x 1024 x 1000, 8 heads of 64, forward and backward 77 + 255 -> 78 + 265 us; 2 x 2048 x 2000, 8 heads of 256, 552 + 1917 -> 565 + 2045, of
+// 201 872 + 2440 -> 981 + 2902. CHAIN: one chain all the same, for sums of few rows (kChain).
+constexpr int kChain = 256;
+template <typename T, int DP, int N, int NU, bool CHAIN>
 __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned char* tile, int base, int l16, int lq, const frag_t<T> (&w)[NU][N]) {
   typedef Head<T, DP> H;
   if constexpr (sizeof(T) == 2) {
@@ -221,7 +224,7 @@ __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned ch
 #pragma unroll
     for (int dt = 0; dt < H::DT; ++dt) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) t[dt & 1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < N; ++j) t[dt & 1][j] = CHAIN ? acc[j][dt] : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         frag_t<T> next = a;
@@ -235,14 +238,14 @@ __device__ __forceinline__ void sums(f32x4 (&acc)[N][DP / 16], const unsigned ch
         // (the columns before these: their products have ended)
         if (u == 0 && dt > 0) {
 #pragma unroll
-          for (int j = 0; j < N; ++j) acc[j][dt - 1] += t[(dt - 1) & 1][j];
+          for (int j = 0; j < N; ++j) acc[j][dt - 1] = CHAIN ? t[(dt - 1) & 1][j] : acc[j][dt - 1] + t[(dt - 1) & 1][j];
         }
         __builtin_amdgcn_sched_barrier(0);
         a = next;
       }
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j][H::DT - 1] += t[(H::DT - 1) & 1][j];
+    for (int j = 0; j < N; ++j) acc[j][H::DT - 1] = CHAIN ? t[(H::DT - 1) & 1][j] : acc[j][H::DT - 1] + t[(H::DT - 1) & 1][j];
   }
 }
 

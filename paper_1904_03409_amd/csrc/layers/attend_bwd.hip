@@ -6,7 +6,7 @@
 // k_attend_short does the five products, and reads q and dy once.
 // Bound by the matrix and vector units together where keys are many (2 sequences of 4096 queries and 4000 keys, 16 heads of 128 over 4,
 // bf16: dq 360 to 380 us, 850 TFLOP/s of its three products; dk and dv 510 to 530, 800 of its four, and 23 for joining their splits); fp32
-// 4 x 1024 x 1000, 8 heads of 64: 129 and 155 us, 98 and 108 TFLOP/s of the 154 of a large product. Of few keys by a workgroup's
+// 4 x 1024 x 1000, 8 heads of 64: 133 and 165 us, 95 and 102 TFLOP/s of the 154 of a large product. Of few keys by a workgroup's
 // start and the waits between its phases: 256 x 240 x 120, 8 heads of 64, bf16 111 us (2.8 TB/s; two kernels took 76 + 64), 64 x 119 x
 // 60, 4 heads of 50, fp32 29 us (20 + 31).
 #include <algorithm>
@@ -22,12 +22,15 @@ namespace {
 template <typename T, int NU>
 constexpr int kPair = sizeof(T) == 4 && NU > 1 ? 2 : 1;
 
-template <typename T, int DP, bool DMA, bool DQ>
+template <typename T, int DP, bool DMA, bool DQ, bool FEW>
 struct Bwd {
   typedef Head<T, DP> H;
-  // rows of a tile in LDS: two tiles of 32 KB at most together with what is kept in registers; 16 own rows to a wave at 256 (of fp32 dk
-  // and dv by way of registers; 32 rows of these spill, and 16 elsewhere take 257 us for dq's 232, 362 for dk's and dv's 300)
-  static constexpr int R = H::BYTES <= 256 ? 64 : H::BYTES <= 512 || DMA || DQ ? 32 : 16, NU = R / H::UNIT, UP = kPair<T, NU>;
+  // rows of a tile in LDS: two tiles of 32 KB at most together with what is kept in registers; 16 own rows to a wave at 256. FEW: sums over
+  // up to kChain rows in fp32 heads of 256, in one chain and tiles of 16; other sums take 32 rows to a tile, but for dk and dv by way of registers,
+  // which spill (2 x 1024 x 1000, 8 heads, 16 and 32 rows: dq 257, 232 us, by way of registers 329, 306, dk and dv 362, 300).
+  static constexpr bool WIDE = H::BYTES > 512;
+  static_assert(!FEW || WIDE, "fp32 heads of 256");
+  static constexpr int R = H::BYTES <= 256 ? 64 : FEW || (WIDE && !DMA && !DQ) ? 16 : 32, NU = R / H::UNIT, UP = kPair<T, NU>;
   static constexpr int TILE = R * H::BYTES, LDS = 4 * TILE + 2 * 3 * R * 4;
   // own rows of a wave / 16, of a workgroup (fp32 heads of 128 by way of registers: two would not fit)
   static constexpr int QT = DP <= 64 || (DP == 128 && (DMA || sizeof(T) == 2)) ? 2 : 1, OWN = 64 * QT;
@@ -39,9 +42,9 @@ struct Bwd {
 
 // A workgroup of k_attend_dkv. BIG: eight waves with 32 keys each, whose values stay in LDS (their registers leave room for two
 // waves on a SIMD that way: bf16 heads of 128; with everything in registers one wave has 337).
-template <typename T, int DP, bool DMA, bool BIG>
+template <typename T, int DP, bool DMA, bool BIG, bool FEW>
 struct Keys {
-  typedef Bwd<T, DP, DMA, false> F;
+  typedef Bwd<T, DP, DMA, false, FEW> F;
   static constexpr int NT = BIG ? 512 : 256, N = BIG ? 2 : F::QT, ALL = NT / 4 * N, WAVES = BIG ? 2 : F::WDKV;
   static constexpr int LDS = F::LDS + (BIG ? ALL * F::H::BYTES : 0);
 };
@@ -57,10 +60,10 @@ struct Short {
 
 }  // namespace
 
-template <typename T, int DP, bool DMA>
-__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA, true>::WDQ)) k_attend_dq(AttendArgs a) {
+template <typename T, int DP, bool DMA, bool FEW>
+__global__ void __launch_bounds__(256, (Bwd<T, DP, DMA, true, FEW>::WDQ)) k_attend_dq(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Bwd<T, DP, DMA, true> F;
+  typedef Bwd<T, DP, DMA, true, FEW> F;
   typedef frag_t<T> frag;
   constexpr int QT = F::QT;
   extern __shared__ __align__(16) unsigned char sm[];
@@ -211,7 +214,7 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA, true>::WDQ)) k_attend_dq
             put_weights(w[u][j], i, ds);
           }
         }
-      sums<T, DP, QT, F::UP>(o, kt, u0 * H::UNIT, l16, lq, w);
+      sums<T, DP, QT, F::UP, FEW>(o, kt, u0 * H::UNIT, l16, lq, w);
     }
   }
 #pragma unroll
@@ -227,12 +230,12 @@ __global__ void __launch_bounds__(256, (Bwd<T, DP, DMA, true>::WDQ)) k_attend_dq
   }
 }
 
-template <typename T, int DP, bool DMA, bool BIG>
-__global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA, BIG>::WAVES)) k_attend_dkv(AttendArgs a) {
+template <typename T, int DP, bool DMA, bool BIG, bool FEW>
+__global__ void __launch_bounds__((Keys<T, DP, DMA, BIG, FEW>::NT), (Keys<T, DP, DMA, BIG, FEW>::WAVES)) k_attend_dkv(AttendArgs a) {
   typedef Head<T, DP> H;
-  typedef Bwd<T, DP, DMA, false> F;
+  typedef Bwd<T, DP, DMA, false, FEW> F;
   typedef frag_t<T> frag;
-  typedef Keys<T, DP, DMA, BIG> K;
+  typedef Keys<T, DP, DMA, BIG, FEW> K;
   constexpr int KN = K::N;
   extern __shared__ __align__(16) unsigned char sm[];
   float* stats = (float*)(sm + 4 * F::TILE);           // two stages of [3][R]: m, 1 / l, delta
@@ -343,8 +346,8 @@ __global__ void __launch_bounds__((Keys<T, DP, DMA, BIG>::NT), (Keys<T, DP, DMA,
             put_weights(ws[u][j], i, ds);
           }
         }
-      sums<T, DP, KN, F::UP>(dv, gt, u0 * H::UNIT, l16, lq, wp);
-      sums<T, DP, KN, F::UP>(dk, qt, u0 * H::UNIT, l16, lq, ws);
+      sums<T, DP, KN, F::UP, FEW>(dv, gt, u0 * H::UNIT, l16, lq, wp);
+      sums<T, DP, KN, F::UP, FEW>(dk, qt, u0 * H::UNIT, l16, lq, ws);
     }
   }
 #pragma unroll
@@ -516,8 +519,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_short(AttendArgs a) {
 #pragma unroll
           for (int j = 0; j < KN; ++j) *(frag*)(ds_ + key[j] * F::SROW + ((4 * u + lq) ^ swz<T, F::SROW / 16>(key[j])) * 16) = ws[half][j];
         }
-        sums<T, DP, KN, UP>(dv, gt, u0 * H::UNIT, l16, lq, wp);
-        sums<T, DP, KN, UP>(dk, qt, u0 * H::UNIT, l16, lq, ws);
+        sums<T, DP, KN, UP, false>(dv, gt, u0 * H::UNIT, l16, lq, wp);
+        sums<T, DP, KN, UP, false>(dk, qt, u0 * H::UNIT, l16, lq, ws);
       }
       __syncthreads();
 #pragma unroll
@@ -684,11 +687,22 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
     };
     if (!plan.one && d->Tq) {
       a.splits = plan.qsplits, a.chunk = plan.qchunk;
+      auto go = [&](auto kern, int own, int lds, std::atomic<uint64_t>& dev) {
+        a.tiles = (int)(((int64_t)d->Tq * a.G + own - 1) / own);
+        return attend_launch(kern, a, (int64_t)a.tiles * d->B * d->Hk * a.splits, lds, dev, st);
+      };
       auto run = [&](auto dma) {
-        typedef Bwd<T, DP, decltype(dma)::value, true> F;
+        constexpr bool DMA = decltype(dma)::value;
+        if constexpr (sizeof(T) * DP > 512) {
+          if (std::min(a.chunk, d->Tk) <= kChain) {
+            typedef Bwd<T, DP, DMA, true, true> F;
+            static std::atomic<uint64_t> dev;
+            return go(k_attend_dq<T, DP, DMA, true>, F::OWN, F::LDS, dev);
+          }
+        }
+        typedef Bwd<T, DP, DMA, true, false> F;
         static std::atomic<uint64_t> dev;
-        a.tiles = (int)(((int64_t)d->Tq * a.G + F::OWN - 1) / F::OWN);
-        return attend_launch(k_attend_dq<T, DP, decltype(dma)::value>, a, (int64_t)a.tiles * d->B * d->Hk * a.splits, F::LDS, dev, st);
+        return go(k_attend_dq<T, DP, DMA, false>, F::OWN, F::LDS, dev);
       };
       e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
       if (e == hipSuccess && a.splits > 1) e = sum(1, d->Hq, d->Tq, (T*)dq, a.sdq, (T*)dq, a.sdq);
@@ -703,14 +717,21 @@ extern "C" int stacklstm_attend_bwd(const slstm_attend_dims* d, const void* q, c
         constexpr bool DMA = decltype(dma)::value;
         if constexpr (DMA && sizeof(T) == 2 && DP == 128) {
           if (plan.big) {
-            typedef Keys<T, DP, DMA, true> K;
+            typedef Keys<T, DP, DMA, true, false> K;
             static std::atomic<uint64_t> dev;
-            return go(k_attend_dkv<T, DP, DMA, true>, K::ALL, K::NT, K::LDS, dev);
+            return go(k_attend_dkv<T, DP, DMA, true, false>, K::ALL, K::NT, K::LDS, dev);
           }
         }
-        typedef Keys<T, DP, DMA, false> K;
+        if constexpr (sizeof(T) * DP > 512) {
+          if ((int64_t)d->Tq * a.G <= (int64_t)kChain * a.splits) {
+            typedef Keys<T, DP, DMA, false, true> K;
+            static std::atomic<uint64_t> dev;
+            return go(k_attend_dkv<T, DP, DMA, false, true>, K::ALL, K::NT, K::LDS, dev);
+          }
+        }
+        typedef Keys<T, DP, DMA, false, false> K;
         static std::atomic<uint64_t> dev;
-        return go(k_attend_dkv<T, DP, DMA, false>, K::ALL, K::NT, K::LDS, dev);
+        return go(k_attend_dkv<T, DP, DMA, false, false>, K::ALL, K::NT, K::LDS, dev);
       };
       e = dma_ok(d, q, a.sq) && dma_ok(d, dy, a.sdy) ? run(std::true_type()) : run(std::false_type());
     }

@@ -6,7 +6,7 @@
 // queries, a quarter of the tile (WK = 4), whose parts are joined through LDS. Where the row tiles do not fill the chip the
 // keys are split over workgroups and k_attend_join joins their sums.
 // Bound by the matrix and vector units together where queries are many (2 sequences of 4096 x 4000, 16 heads of 128 over 4, bf16: 275 us,
-// 760 TFLOP/s, matrix units 30% and vector units 40% busy; fp32 4 x 1024 x 1000, 8 heads of 64: 86 us, 97 TFLOP/s), by the keys' bytes
+// 760 TFLOP/s, matrix units 30% and vector units 40% busy; fp32 4 x 1024 x 1000, 8 heads of 64: 88 us, 95 TFLOP/s), by the keys' bytes
 // where they are few (8 beams of 8 sequences over up to 16384 keys, 16 heads of 128 over 4: 38 us, 5.5 TB/s, and 4.6 for the join), by a
 // workgroup's start and waits where both are (256 x 240 x 120, 8 heads of 64, bf16: 51 us, 3.1 TB/s).
 // With register staging, padded rows and one wave to a SIMD the first of these took 610 us.
@@ -59,7 +59,8 @@ __device__ __forceinline__ void fwd_row(const AttendArgs& a, int b, int t, int h
 
 // LOOP: keys of two tiles at most, which stay in LDS while the workgroup goes through a.reps row tiles, the next one's queries on their
 // way during this one's products: a row tile then costs neither a start nor a wait for its keys.
-template <typename T, int DP, int QT, int WK, bool DMA, bool LOOP>
+// FEW: sums over up to kChain keys of a wave.
+template <typename T, int DP, int QT, int WK, bool DMA, bool LOOP, bool FEW>
 __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fwd(AttendArgs a) {
   typedef Head<T, DP> H;
   typedef Fwd<T, DP, WK, DMA> F;
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(256, (Fwd<T, DP, WK, DMA>::WAVES)) k_attend_fw
         }
         l[j] += sum;
       }
-      sums<T, DP, QT, F::NU>(o, vt, wk * F::KW, l16, lq, w);
+      sums<T, DP, QT, F::NU, FEW>(o, vt, wk * F::KW, l16, lq, w);
     }
     if constexpr (F::STAGES == 1) {
       __syncthreads();
@@ -349,7 +350,9 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int cs, int g
 
 namespace {
 
-// Row tiles and splits. Up to 16 rows (queries times heads of a key) share their keys in a tile; more rows go 16 or 32 to a wave.
+// Row tiles and splits. Up to 16 rows (queries times heads of a key) share their keys in a tile (64 x 16 x 2000, 4 heads of 64, fp32 47 us, a
+// wave to them 90; 16 x 16 x 1000, 8 of 64, bf16 11.9, 12.4); more rows go 16 or, bf16 and more than 64, 32 to a wave (64 x 64 x 1000, 8 of 64 25, 30; 64 x 96
+// x 1000 33, 30; 64 x 128 x 1000, 8 of 128 76, 55).
 constexpr int kLoopKeys = 128;                         // two tiles of heads of up to 64
 struct FwdPlan {
   int qt, wk, rows, tiles, splits, chunk, reps;
@@ -426,22 +429,28 @@ extern "C" int stacklstm_attend_fwd(const slstm_attend_dims* d, const void* q, c
       if constexpr (DMA || sizeof(T) * DP <= 512) {
         if (p.wk == 4) {
           static std::atomic<uint64_t> dev;
-          return attend_launch(k_attend_fwd<T, DP, 1, 4, DMA, false>, a, groups, Fwd<T, DP, 4, DMA>::LDS, dev, st);
+          return attend_launch(k_attend_fwd<T, DP, 1, 4, DMA, false, false>, a, groups, Fwd<T, DP, 4, DMA>::LDS, dev, st);
         }
       }
       if constexpr (DP <= 64) {
         static_assert(2 * Fwd<T, DP, 1, DMA>::KT >= kLoopKeys && Fwd<T, DP, 1, DMA>::STAGES == 2, "all keys stay");
         if (p.reps > 1) {
           static std::atomic<uint64_t> dev;
-          return attend_launch(k_attend_fwd<T, DP, (sizeof(T) == 4 ? 1 : 2), 1, DMA, true>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+          return attend_launch(k_attend_fwd<T, DP, (sizeof(T) == 4 ? 1 : 2), 1, DMA, true, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+        }
+      }
+      if constexpr (sizeof(T) * DP > 512) {
+        if (std::min(p.chunk, d->Tk) <= kChain) {
+          static std::atomic<uint64_t> dev;
+          return attend_launch(k_attend_fwd<T, DP, 1, 1, DMA, false, true>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
         }
       }
       if (DP > 128 || p.qt == 1) {
         static std::atomic<uint64_t> dev;
-        return attend_launch(k_attend_fwd<T, DP, 1, 1, DMA, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+        return attend_launch(k_attend_fwd<T, DP, 1, 1, DMA, false, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
       }
       static std::atomic<uint64_t> dev;
-      return attend_launch(k_attend_fwd<T, DP, (DP > 128 || sizeof(T) == 4 ? 1 : 2), 1, DMA, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
+      return attend_launch(k_attend_fwd<T, DP, (DP > 128 || sizeof(T) == 4 ? 1 : 2), 1, DMA, false, false>, a, groups, Fwd<T, DP, 1, DMA>::LDS, dev, st);
     };
     hipError_t e = dma_ok(d, k, a.sk) && dma_ok(d, v, a.sv) ? run(std::true_type()) : run(std::false_type());
     if (e == hipSuccess && p.splits > 1) {

@@ -40,7 +40,7 @@ def test_rows_up_to_31_bits(dtype):
 SIZES = [(2, 1, 300, 8, 2, 128), (1, 4, 500, 2, 1, 100), (1, 3, 200, 2, 2, 131), (2, 2, 300, 2, 1, 256), (3, 2, 150, 8, 1, 27), (2, 5, 400, 3, 3, 32), (1, 16, 170, 1, 1, 61),
          (2, 3, 290, 4, 1, 64), (2, 70, 90, 2, 2, 50), (2, 90, 70, 2, 1, 30), (1, 50, 150, 2, 1, 63), (2, 40, 140, 2, 2, 29), (1, 80, 300, 2, 1, 121), (1, 60, 150, 1, 1, 250), (2, 34, 135, 1, 1, 32),
          (2, 100, 140, 2, 2, 64), (1, 65, 129, 1, 1, 24), (1, 20, 130, 4, 1, 160), (2, 3, 180, 2, 1, 101),
-         (1, 20, 100, 2, 1, 121), (2, 24, 100, 2, 2, 40)]
+         (1, 20, 100, 2, 1, 121), (2, 24, 100, 2, 2, 40), (3, 300, 300, 90, 90, 132), (3, 290, 310, 90, 90, 131)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
