@@ -101,3 +101,62 @@ def test_best_tokens(R, V, G, N, dtype):
     _check(r, few, want, dtype, a[few], h[few])
     r.forward(), r.backward()
     _check(r, few, want, dtype, a[few], h[few])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(3, 50, 70, 4, 2, 64), (2, 9, 300, 4, 1, 48), (2, 33, 90, 2, 2, 160)])
+def test_mixed_layouts(size, dtype):
+    """Every matrix in a layout of its own: queries and dy in wider buffers, keys steps first, values heads first, gradients in other orders."""
+    ly = _ly()
+    rng = rng_for("mixed", *size, dtype)
+    B, Tq, Tk, Hq, Hk, D = size
+    s, q_len, k_len, m = inputs(rng, *size, dtype, lens=True, mask=True)
+    v = heads(s["v"], dtype).permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3)
+    big = torch.full((Tq, B, Hq, D + 5), 5.0, dtype=DT[dtype], device="cuda")
+    y = big[..., 2:2 + D].transpose(0, 1)
+    r = ly.AttendRun.of(heads(s["q"], dtype, pad=3), heads(s["k"], dtype, steps_first=True), v, dev(q_len), dev(k_len), dev(m), None,
+                        heads(s["dy"], dtype, pad=1, steps_first=True), y)
+    r.dk = torch.full((Hk, Tk, B, D), 7.0, dtype=DT[dtype], device="cuda").permute(2, 1, 0, 3)
+    r.dims.dk = ly.strides_of(r.dk)
+    r.forward(), r.backward()
+    want, off = ref.attend(s["q"], s["k"], s["v"], ref.seen(B, Tq, Tk, q_len, k_len, m), D ** -0.5, s["dy"], dtype, bounds=True)
+    for n, x in (("y", r.y), ("dq", r.dq), ("dk", r.dk), ("dv", r.dv)):
+        within(x, want[n], off[n], n)
+    assert (big[..., :2] == 5).all() and (big[..., 2 + D:] == 5).all()
+
+
+def test_graphs_of_split_calls():
+    """Calls that go through a work space, and of more than 64 KB of LDS, captured together and replayed with other inputs and lengths."""
+    ly = _ly()
+    g = torch.Generator(device="cuda").manual_seed(11)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    runs = []
+    for D, dtype in ((256, "f32"), (128, "bf16"), (50, "f32")):
+        e = lambda T, H: rand(2, T, H, D).to(DT[dtype])
+        k_len = torch.tensor([700, 333], dtype=torch.int32, device="cuda")
+        runs.append(ly.AttendRun.of(e(40, 4), e(700, 2), e(700, 2), k_len=k_len, dy=e(40, 4)))
+    lp = ly.LogProbRun.of(rand(3, 70000), torch.zeros(3, 1, dtype=torch.int32, device="cuda"), top=4, dlogp=rand(3, 1))
+
+    def step():
+        for r in runs:
+            r.forward(), r.backward()
+        lp.step()
+    outputs = lambda: [t for r in runs for t in (r.y, r.dq, r.dk, r.dv)] + [lp.logp, lp.entropy, lp.index, lp.value, lp.dlogits]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        for r in runs:
+            r.q.copy_(rand(*r.q.shape))
+            r.k_len.copy_(torch.randint(0, 701, (2,), generator=g, device="cuda"))
+        lp.logits.copy_(rand(3, 70000))
+        step()
+        want = [t.clone() for t in outputs()]
+        for t in outputs() + [r.workspace for r in runs] + [lp.workspace]:
+            t.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outputs())), i
